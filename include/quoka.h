@@ -10,7 +10,8 @@
  *   3. keeps the B_SA best keys per KV head               (Alg. 1, topk step; Eq. 3),
  *   4. attends the chunk over [gathered keys | chunk keys] with a causal mask inside the chunk
  *                                                         (Alg. 2, attention step; Eq. 2-3).
- * A dense chunked-prefill attention (Eq. 2) is provided as the baseline.
+ * A dense chunked-prefill attention (Eq. 2) is provided as the baseline, and for caches kept in pages, in 8 bits or as they
+ * are, the write of a chunk's rows, their way back and the attention over them (quoka_cache_write and what follows it).
  *
  * Conventions that hold for every entry point
  *   - `shape` is a host pointer, read during the call, never retained.
@@ -205,6 +206,71 @@ quoka_status quoka_prefill_attn(const quoka_shape* shape, int sparse, const void
                                 const int32_t* kv_lens_all, const int32_t* budgets_all, int32_t* q_idx, float* qbar,
                                 float* scores, int32_t* k_idx, int32_t* k_cnt, void* out, void* workspace,
                                 size_t workspace_bytes, void* stream);
+
+/* ---- Caches in pages ------------------------------------------------------------------------------------------------
+ * A pool of pages of page_len tokens each holds the keys and values of many sequences; page_table names the pages of every
+ * sequence in order: the row of KV head kv at position t of sequence b is
+ *   page = page_table[b, t / page_len],  k[page, kv, t % page_len, :]   (v likewise).
+ * The convention of lengths is the library's: kv_lens[b] tokens are cached before the chunk, and the chunk's token i has position
+ * kv_lens[b] + i.  chunk_lens[b] <= chunk_len is the number of tokens that sequence b really has in this chunk (NULL: chunk_len
+ * for all; 0 is legal).  kv_lens is cut to [0, max_kv_len], chunk_lens to [0, chunk_len].
+ *   QUOKA_PAGES_RAW  rows are kept in shape.dtype; k_scale and v_scale are ignored
+ *   QUOKA_PAGES_FP8  rows are d elements of e4m3 (OCP, no infinities) times one power of two per row, kept as its biased
+ *                    exponent (2^(scale - 127), scale 1..254): the smallest one that brings the row's largest magnitude to 448 or
+ *                    less, at least 2^-126.  Elements are rounded to nearest, ties to even.  A power of two costs no precision
+ *                    (the elements have exponents of their own) and lets a row come back in bfloat16 without a second rounding.
+ * Pages that no position below a sequence's length lies in are never touched, whatever their table entries are, and rows of the
+ * pool past a length are never used, whatever they hold (NaN included).  Entries that are used must be in [0, n_pages); others
+ * are harmless: a write drops the row, everything else takes some row of the pool in its place.  The same goes for positions
+ * from max_pages * page_len on.  Sequences may share pages that are only read.                                                    */
+typedef enum { QUOKA_PAGES_RAW = 0, QUOKA_PAGES_FP8 = 1 } quoka_page_format;
+
+typedef struct quoka_pages {
+  void* k;                   /* device: K pages [n_pages, n_KV, page_len, d], 16-byte aligned                      */
+  void* v;                   /* device: V pages, the same layout                                                   */
+  uint8_t* k_scale;          /* device: [n_pages, n_KV, page_len], dense (FP8 only)                                */
+  uint8_t* v_scale;
+  const int32_t* page_table; /* device: [b, max_pages]                                                             */
+  int64_t stride[3];         /* page, head and token strides of K and V in elements: multiples of 16, token >= d   */
+  int32_t n_pages;           /* pages of the pool                                                                  */
+  int32_t page_len;          /* tokens of a page: a power of two, at most 65536                                    */
+  int32_t max_pages;         /* extent of page_table's last axis; max_pages * page_len >= shape.max_kv_len         */
+  int32_t format;            /* quoka_page_format                                                                  */
+} quoka_pages;
+
+/* The chunk's keys and values into their pages (the append step of Alg. 2 for a cache in pages).
+ *   k_chunk, v_chunk  in  [b, n_KV, C, d] (shape.dtype, shape.ck_stride)
+ *   pages             rows kv_lens[b] .. kv_lens[b] + chunk_lens[b] - 1 of every sequence are written, and their scales; no other
+ *                     byte of the pool is
+ * No two of the rows written may be the same row of the pool.  Needs no workspace. */
+quoka_status quoka_cache_write(const quoka_shape* shape, const quoka_pages* pages, const void* k_chunk, const void* v_chunk,
+                               const int32_t* kv_lens, const int32_t* chunk_lens, void* stream);
+
+/* Rows 0 .. kv_lens[b] - 1 of every sequence as contiguous tensors, what they stand for in shape.dtype.
+ *   k_out, v_out  out  [b, n_KV, T_max, d] (shape.dtype, shape.kv_stride); either may be NULL (a selection of keys needs K
+ *                      alone).  Rows from kv_lens[b] on are left as they are.
+ * Exact, but for 8-bit rows so small that bfloat16 has no normal number for them.  Needs no workspace. */
+quoka_status quoka_cache_read(const quoka_shape* shape, const quoka_pages* pages, const int32_t* kv_lens, void* k_out,
+                              void* v_out, void* stream);
+
+/* Attention of a chunk over the pages, the chunk's own rows among them (quoka_cache_write has put them there).  For q-head h (KV
+ * head kv) and chunk position i < chunk_lens[b]:
+ *   O[b,h,i] = sum_j softmax_j(<Q[b,h,i], K_j> / sqrt(d)) V_j,
+ *   j over the positions kv_lens[b] + c, c <= i, and
+ *     k_idx == NULL: every position t < kv_lens[b]                    (quoka_dense_attn over pages)
+ *     otherwise:     k_idx[b,kv,0..k_cnt[b,kv])                       (quoka_sparse_attn over pages; any order; entries are positions
+ *                    below kv_lens[b]; others are cut to [0, max_kv_len) and give a wrong result, never an access outside the pool)
+ * Rows i >= chunk_lens[b] are written as zeros, their lse as -infinity.
+ *   q, out   [b, n_Q, C, d] (shape.dtype);  k_idx [b, n_KV, B_max], k_cnt [b, n_KV] as written by quoka_topk_keys
+ *   lse      optional [b, n_Q, C] float32: natural-log softmax normaliser
+ * bf16: products on bf16 MFMA with float32 accumulation and softmax state; 8-bit rows are widened to bfloat16, which is exact; the
+ *   softmax scale is applied to the float32 products (as with QUOKA_ATTN_SCALE_F32, which changes nothing here), so that P and
+ *   the output are rounded once each and Q is not.   f32: all arithmetic in float32, 8-bit rows widened exactly.
+ * The other score_flags, kv_stride and ck_stride do not matter here, but have to be valid. */
+quoka_status quoka_paged_workspace_bytes(const quoka_shape* shape, size_t* out_bytes);
+quoka_status quoka_paged_attn(const quoka_shape* shape, const quoka_pages* pages, const void* q, const int32_t* kv_lens,
+                              const int32_t* chunk_lens, const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse,
+                              void* workspace, size_t workspace_bytes, void* stream);
 
 /* quoka_topk_keys for callers that cannot allocate device memory and have no workspace to pass: code under HIP
  * graph capture, tight serving loops, harnesses that forbid hipMalloc.  Same arguments minus the workspace, same

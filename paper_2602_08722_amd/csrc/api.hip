@@ -589,6 +589,96 @@ quoka_status quoka_topk_keys_noalloc(const quoka_shape* shape, const float* scor
       quoka::launch_topk_keys(dm, scores, kv_lens, budgets, k_idx, k_cnt, ws, static_cast<hipStream_t>(stream)));
 }
 
+// ---- caches in pages -----------------------------------------------------------------------------------------------
+static quoka_status check_pages(const quoka_shape& s, const quoka_pages* p, quoka::Pages* out) {
+  if (p == nullptr || p->k == nullptr || p->v == nullptr || p->page_table == nullptr) return QUOKA_EINVAL;
+  if (p->n_pages < 1 || p->max_pages < 1 || p->page_len < 1 || (p->page_len & (p->page_len - 1)) != 0) return QUOKA_EINVAL;
+  if (p->format != QUOKA_PAGES_RAW && p->format != QUOKA_PAGES_FP8) return QUOKA_EUNSUPPORTED;
+  if (p->page_len > 65536) return QUOKA_EUNSUPPORTED;
+  if (p->format == QUOKA_PAGES_FP8 && (p->k_scale == nullptr || p->v_scale == nullptr)) return QUOKA_EINVAL;
+  if (!aligned16(p->k) || !aligned16(p->v)) return QUOKA_EINVAL;
+  for (int i = 0; i < 3; ++i)
+    if (p->stride[i] < 0 || p->stride[i] % 16 != 0) return QUOKA_EINVAL;
+  if (p->stride[2] < s.head_dim) return QUOKA_EINVAL;
+  if ((long long)p->max_pages * p->page_len < s.max_kv_len) return QUOKA_EINVAL;
+  out->k = p->k;
+  out->v = p->v;
+  out->k_scale = p->k_scale;
+  out->v_scale = p->v_scale;
+  out->table = p->page_table;
+  for (int i = 0; i < 3; ++i) out->st[i] = p->stride[i];
+  out->n_pages = p->n_pages;
+  out->max_pages = p->max_pages;
+  out->n_kv = s.n_kv_heads;
+  out->shift = __builtin_ctz((unsigned)p->page_len);
+  return QUOKA_OK;
+}
+
+quoka_status quoka_cache_write(const quoka_shape* shape, const quoka_pages* pages, const void* k_chunk, const void* v_chunk,
+                               const int32_t* kv_lens, const int32_t* chunk_lens, void* stream) {
+  Dims dm;
+  quoka::Pages pg;
+  quoka_status st = check_shape(shape, &dm);
+  if (st != QUOKA_OK) return st;
+  st = check_pages(*shape, pages, &pg);
+  if (st != QUOKA_OK) return st;
+  if (k_chunk == nullptr || v_chunk == nullptr || kv_lens == nullptr || !aligned16(k_chunk) || !aligned16(v_chunk)) return QUOKA_EINVAL;
+  return from_hip(quoka::launch_cache_write(dm, shape->dtype, pages->format == QUOKA_PAGES_FP8, pg, k_chunk, v_chunk, kv_lens,
+                                            chunk_lens, static_cast<hipStream_t>(stream)));
+}
+
+quoka_status quoka_cache_read(const quoka_shape* shape, const quoka_pages* pages, const int32_t* kv_lens, void* k_out,
+                              void* v_out, void* stream) {
+  Dims dm;
+  quoka::Pages pg;
+  quoka_status st = check_shape(shape, &dm);
+  if (st != QUOKA_OK) return st;
+  st = check_pages(*shape, pages, &pg);
+  if (st != QUOKA_OK) return st;
+  if (kv_lens == nullptr || (k_out == nullptr && v_out == nullptr) || !aligned16(k_out) || !aligned16(v_out)) return QUOKA_EINVAL;
+  if (dm.T_max == 0) return QUOKA_OK;
+  return from_hip(quoka::launch_cache_read(dm, shape->dtype, pages->format == QUOKA_PAGES_FP8, pg, kv_lens, k_out, v_out,
+                                           static_cast<hipStream_t>(stream)));
+}
+
+quoka_status quoka_paged_workspace_bytes(const quoka_shape* shape, size_t* out_bytes) {
+  Dims dm;
+  const quoka_status st = check_shape(shape, &dm);
+  if (st != QUOKA_OK) return st;
+  if (out_bytes == nullptr) return QUOKA_EINVAL;
+  const size_t bytes = round_up(quoka::paged_attn_ws_floats(dm, shape->dtype) * sizeof(float), kAlign);
+  *out_bytes = bytes > 0 ? bytes : kAlign;
+  return QUOKA_OK;
+}
+
+quoka_status quoka_paged_attn(const quoka_shape* shape, const quoka_pages* pages, const void* q, const int32_t* kv_lens,
+                              const int32_t* chunk_lens, const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  Dims dm;
+  quoka::PagedArgs a;
+  quoka_status st = check_shape(shape, &dm);
+  if (st != QUOKA_OK) return st;
+  st = check_pages(*shape, pages, &a.pg);
+  if (st != QUOKA_OK) return st;
+  if (q == nullptr || out == nullptr || kv_lens == nullptr || !aligned16(q) || !aligned16(out)) return QUOKA_EINVAL;
+  if (k_idx != nullptr && k_cnt == nullptr) return QUOKA_EINVAL;
+  if (workspace == nullptr) return QUOKA_EINVAL;
+  size_t need = 0;
+  st = quoka_paged_workspace_bytes(shape, &need);
+  if (st != QUOKA_OK) return st;
+  if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0 || workspace_bytes < need) return QUOKA_EWORKSPACE;
+  a.q = q;
+  a.kv_lens = kv_lens;
+  a.chunk_lens = chunk_lens;
+  // (a list without room for entries: kernels fetch entry 0 before they know a list's length, so they are given k_cnt in its place)
+  a.k_idx = k_idx != nullptr && dm.B_max == 0 ? k_cnt : k_idx;
+  a.k_cnt = k_cnt;
+  a.out = out;
+  a.lse = lse;
+  return from_hip(quoka::launch_paged_attn(dm, shape->dtype, pages->format == QUOKA_PAGES_FP8, a, static_cast<float*>(workspace),
+                                           static_cast<hipStream_t>(stream)));
+}
+
 quoka_status quoka_probe_mfma(int blocks, int iters, float* sink, void* stream) {
   if (blocks < 1 || blocks > 65535 || iters < 1 || sink == nullptr) return QUOKA_EINVAL;
   return from_hip(quoka::launch_probe_mfma(blocks, iters, sink, static_cast<hipStream_t>(stream)));
@@ -625,6 +715,6 @@ const char* quoka_status_string(quoka_status status) {
   return "unknown status";
 }
 
-int quoka_version(void) { return 100; }
+int quoka_version(void) { return 200; }
 
 }  // extern "C"

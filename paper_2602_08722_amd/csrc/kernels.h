@@ -124,6 +124,31 @@ hipError_t launch_attn_decode_bf16(const Dims& dm, const AttnArgs& a, float* par
 size_t attn_f32_ws_floats(const Dims& dm);
 hipError_t launch_attn_f32(const Dims& dm, const AttnArgs& a, float* part, hipStream_t st);
 
+// --- caches in pages (pages.hip, paged_*.hip) -------------------------------------------------------
+// Kernel-side view of quoka_pages.
+struct Pages {
+  void *k, *v;
+  uint8_t *k_scale, *v_scale;
+  const int32_t* table;
+  long long st[3];   // page, head, token
+  int n_pages, shift, max_pages;   // page_len == 1 << shift
+  int n_kv;
+};
+hipError_t launch_cache_write(const Dims& dm, int dtype, bool fp8, const Pages& pg, const void* k, const void* v, const int32_t* kv_lens,
+                              const int32_t* chunk_lens, hipStream_t st);
+hipError_t launch_cache_read(const Dims& dm, int dtype, bool fp8, const Pages& pg, const int32_t* kv_lens, void* k, void* v,
+                             hipStream_t st);
+struct PagedArgs {
+  const void* q;
+  const int32_t *kv_lens, *chunk_lens;   // chunk_lens: nullptr where every sequence has C tokens
+  const int32_t *k_idx, *k_cnt;          // nullptr for dense
+  void* out;
+  float* lse;                            // may be nullptr
+  Pages pg;
+};
+size_t paged_attn_ws_floats(const Dims& dm, int dtype);
+hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float* part, hipStream_t st);
+
 // --- measurement aids (probes.hip) ------------------------------------------------------------------
 hipError_t launch_probe_mfma(int blocks, int iters, float* sink, hipStream_t st);
 hipError_t launch_probe_attn_mix(int blocks, int steps, float* sink, hipStream_t st);

@@ -1,0 +1,510 @@
+"""Caches in pages on the GPU against plain float64: what a write leaves, what comes back, and attention over the pages."""
+import numpy as np
+import pytest
+import torch
+
+from tests import paged_plain as P
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+def _pk():
+    import paper_2602_08722_amd as pk
+    pk.load_library()
+    return pk
+
+
+def _ids(c):
+    return "-".join(f"{k}{v}" for k, v in c.items()).replace(" ", "")
+
+
+def _rows(rng, n, n_kv, d, dtype):
+    return P.store(rng.standard_normal((n, n_kv, d)), dtype).astype(np.float64)
+
+
+# ---- write ---------------------------------------------------------------------------------------------------------
+
+WRITE_CASES = [
+    dict(dtype="bf16", fp8=True, n_kv=2, d=128, page_len=16, C=40, lens=[0, 7, 16], chunks=[40, 33, 1]),
+    dict(dtype="bf16", fp8=True, n_kv=3, d=64, page_len=64, C=130, lens=[63, 64], chunks=None),
+    dict(dtype="bf16", fp8=False, n_kv=2, d=128, page_len=32, C=35, lens=[31, 5], chunks=[0, 35]),
+    dict(dtype="bf16", fp8=False, n_kv=1, d=64, page_len=1, C=9, lens=[3], chunks=None),
+    dict(dtype="f32", fp8=True, n_kv=2, d=128, page_len=8, C=21, lens=[2, 9], chunks=[21, -4]),
+    dict(dtype="f32", fp8=True, n_kv=1, d=64, page_len=256, C=300, lens=[100], chunks=None),
+    dict(dtype="f32", fp8=False, n_kv=2, d=64, page_len=16, C=50, lens=[0, 1], chunks=[50, 17]),
+    dict(dtype="f32", fp8=False, n_kv=2, d=128, page_len=16, C=3, lens=[14, 15, 16], chunks=None),
+    dict(dtype="bf16", fp8=True, n_kv=8, d=128, page_len=16, C=1, lens=[0, 15, 16, 17, 31, 100], chunks=None),
+    dict(dtype="bf16", fp8=True, n_kv=2, d=128, page_len=128, C=2100, lens=[77], chunks=[2050]),   # many blocks
+]
+
+
+@pytest.mark.parametrize("layout", ["heads", "tokens"])
+@pytest.mark.parametrize("case", WRITE_CASES, ids=_ids)
+def test_write_leaves_the_rows_and_nothing_else(case, layout):
+    pk = _pk()
+    rng = np.random.default_rng(5)
+    n_kv, d, C, lens, b = case["n_kv"], case["d"], case["C"], case["lens"], len(case["lens"])
+    chunks = [C] * b if case["chunks"] is None else [max(c, 0) for c in case["chunks"]]
+    pool = P.Pool(rng, [_rows(rng, n, n_kv, d, case["dtype"]) for n in lens], [_rows(rng, n, n_kv, d, case["dtype"]) for n in lens],
+                  n_kv, d, case["page_len"], case["dtype"], case["fp8"], layout=layout, reserve=[t + c for t, c in zip(lens, chunks)])
+    k_new, v_new = (P.store(rng.standard_normal((b, n_kv, C, d)) * np.exp2(rng.integers(-20, 20, (b, n_kv, C, 1))), case["dtype"])
+                    for _ in range(2))
+    k_new[:, :, -1] = 0.0   # a row of zeros
+    given = [P.to_dev(x, case["dtype"], DEV) for x in (k_new, v_new)]
+    if layout == "tokens":   # a chunk whose heads lie inside its tokens
+        given = [x.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3) for x in given]
+
+    def bits():
+        got = []
+        for t in (pool.k_pages, pool.v_pages, pool.k_scale, pool.v_scale):
+            if t is not None:
+                got.append((t.view(torch.uint8) if t.element_size() == 1 else t.view(torch.int16 if t.element_size() == 2 else torch.int32))
+                           .cpu().numpy().copy())
+        return got
+
+    before = bits()
+    buf = pk.PagedBuffers(pool.cache(), lens, max(lens), k_chunk=given[0], v_chunk=given[1],
+                          chunk_lens=case["chunks"])
+    buf.write()
+    torch.cuda.synchronize()
+    after = bits()
+    touched = np.zeros(before[0].shape[:3], dtype=bool)
+    for i in range(b):
+        for c in range(chunks[i]):
+            p = lens[i] + c
+            touched[pool.table[i, p // case["page_len"]], :, p % case["page_len"]] = True
+    for x, y in zip(before, after):
+        assert np.array_equal(x[~touched], y[~touched]), "a row that is not the chunk's changed"
+    for which, pages, scale, new in (("k", pool.k_pages, pool.k_scale, k_new), ("v", pool.v_pages, pool.v_scale, v_new)):
+        got = pages.float().cpu().numpy().astype(np.float64)
+        exps = None if scale is None else scale.cpu().numpy().astype(np.int64)
+        for i in range(b):
+            p = lens[i] + np.arange(chunks[i])
+            page, slot = pool.table[i][p // case["page_len"]], p % case["page_len"]
+            want = new[i].transpose(1, 0, 2)[:chunks[i]].astype(np.float64)
+            if scale is not None:
+                want, e = P.quantise(want)
+                assert np.array_equal(exps[page, :, slot], e), f"{which}{i}: exponents"
+            assert np.array_equal(got[page, :, slot], want), f"{which}{i}: rows"
+
+
+def test_write_rounds_every_kind_of_row_as_the_format_says():
+    """Rows at the edges of the format: the largest magnitude at, just below and just above 448 times a power of two, halves between two
+    elements, elements below the smallest normal one, rows of the smallest and largest numbers of the dtype, negative zeros."""
+    pk = _pk()
+    rng = np.random.default_rng(6)
+    for dtype, d in (("bf16", 128), ("f32", 64)):
+        rows = []
+        eps = 2.0 ** -7 if dtype == "bf16" else 2.0 ** -23
+        for e in (-130, -127, -126, -125, -118, -117, -60, -1, 0, 1, 7, 8, 9, 100, 119):
+            for lead in (1.0, 1.75, 1.75 * (1 + eps), 1.75 * (1 - eps), 1.9921875):
+                x = rng.standard_normal(d) * 0.2
+                x[::5] *= np.exp2(rng.integers(-18, 0, x[::5].shape))
+                # halves between neighbouring elements: odd multiples of half a step
+                x[1:17] = (8 + np.arange(16) % 8 + 0.5) / 8 * np.exp2(-(np.arange(16) // 8 + 4.0))
+                x = np.clip(x, -0.99, 0.99)
+                x[0] = lead
+                rows.append(np.ldexp(x, e))
+        rows.append(np.zeros(d))
+        rows.append(-np.zeros(d))
+        big = np.zeros(d)
+        big[3] = 3.3895313892515355e38   # the largest bfloat16
+        rows.append(-big)
+        tiny = np.zeros(d)
+        tiny[5] = 2.0 ** -133            # the smallest bfloat16
+        rows.append(tiny)
+        x = P.store(np.stack(rows)[None, None], dtype)   # [1, 1, C, d]
+        C = x.shape[2]
+        pool = P.Pool(rng, [np.zeros((0, 1, d))], [np.zeros((0, 1, d))], 1, d, 16, dtype, True, reserve=[C])
+        t = P.to_dev(x, dtype, DEV)
+        buf = pk.PagedBuffers(pool.cache(), [0], 0, k_chunk=t, v_chunk=t.clone())
+        buf.write()
+        torch.cuda.synchronize()
+        want, e = P.quantise(x[0, 0].astype(np.float64))
+        p = np.arange(C)
+        for pages, scale in ((pool.k_pages, pool.k_scale), (pool.v_pages, pool.v_scale)):
+            got = pages.float().cpu().numpy()[pool.table[0][p // 16], 0, p % 16]
+            assert np.array_equal(scale.cpu().numpy()[pool.table[0][p // 16], 0, p % 16].astype(np.int64), e)
+            assert np.array_equal(got.astype(np.float64), want)
+            assert np.all(np.abs(got) <= 448)
+
+
+def test_write_drops_rows_that_have_no_page():
+    """Entries outside the pool and positions past the table: nothing is written for them, the others are."""
+    pk = _pk()
+    rng = np.random.default_rng(7)
+    n_kv, d, page_len = 2, 128, 16
+    pool = P.Pool(rng, [np.zeros((0, n_kv, d))], [np.zeros((0, n_kv, d))], n_kv, d, page_len, "bf16", True, reserve=[48])
+    pool.dev_table[0, 1] = pool.k_pages.shape[0] + 5
+    good = [int(pool.table[0, 0]), int(pool.table[0, 2])]
+    t = P.to_dev(rng.standard_normal((1, n_kv, 70, d)), "bf16", DEV)   # 48 positions have a place in the table
+    buf = pk.PagedBuffers(pool.cache(), [0], 48, k_chunk=t, v_chunk=t.clone())
+    buf.write()
+    torch.cuda.synchronize()
+    written = (pool.k_scale != 255).all(-1).all(-1).cpu().numpy()
+    assert sorted(np.nonzero(written)[0].tolist()) == sorted(good)
+    assert not (pool.k_scale != 255).any(-1).any(-1).cpu().numpy()[~written].any()
+
+
+# ---- read ----------------------------------------------------------------------------------------------------------
+
+READ_CASES = [
+    dict(dtype="bf16", fp8=True, n_kv=2, d=128, page_len=16, lens=[1, 100, 33]),
+    dict(dtype="bf16", fp8=True, n_kv=3, d=64, page_len=64, lens=[0, 129]),
+    dict(dtype="bf16", fp8=False, n_kv=2, d=128, page_len=8, lens=[77]),
+    dict(dtype="bf16", fp8=False, n_kv=2, d=64, page_len=32, lens=[5, 64]),
+    dict(dtype="f32", fp8=True, n_kv=2, d=128, page_len=16, lens=[31, 2]),
+    dict(dtype="f32", fp8=False, n_kv=1, d=64, page_len=1, lens=[13]),
+    dict(dtype="f32", fp8=False, n_kv=2, d=128, page_len=128, lens=[500, 1]),
+    dict(dtype="bf16", fp8=True, n_kv=2, d=128, page_len=256, lens=[5003]),
+]
+
+
+@pytest.mark.parametrize("layout", ["heads", "tokens"])
+@pytest.mark.parametrize("case", READ_CASES, ids=_ids)
+def test_read_returns_what_the_rows_stand_for(case, layout):
+    pk = _pk()
+    rng = np.random.default_rng(8)
+    n_kv, d, lens, b = case["n_kv"], case["d"], case["lens"], len(case["lens"])
+    scale = lambda n: np.exp2(rng.integers(-30, 30, (n, n_kv, 1)))  # noqa: E731
+    pool = P.Pool(rng, [P.store(_rows(rng, n, n_kv, d, case["dtype"]) * scale(n), case["dtype"]).astype(np.float64) for n in lens],
+                  [_rows(rng, n, n_kv, d, case["dtype"]) for n in lens], n_kv, d, case["page_len"], case["dtype"], case["fp8"], layout=layout)
+    T = max(lens) + 3
+    buf = pk.PagedBuffers(pool.cache(), lens, T if T <= pool.table.shape[1] * case["page_len"] else max(lens))
+    T = buf.max_kv_len
+    for want_k, want_v in ((True, True), (True, False), (False, True)):
+        outs = []
+        for want in (want_k, want_v):
+            t = torch.full((b, n_kv, T, d), 7.0, dtype=P.TORCH[case["dtype"]], device=DEV)
+            if layout == "tokens":
+                t = t.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)
+            outs.append(t if want else None)
+        buf.read(*outs)
+        torch.cuda.synchronize()
+        for got, want in zip(outs, (pool.k, pool.v)):
+            if got is None:
+                continue
+            got = got.float().cpu().numpy().astype(np.float64)
+            for i in range(b):
+                assert np.array_equal(got[i, :, :lens[i]], want[i].transpose(1, 0, 2))   # exact
+                assert np.all(got[i, :, lens[i]:] == 7.0)
+
+
+# ---- attention -----------------------------------------------------------------------------------------------------
+
+def _attn_problem(case, seed, layout="heads", q_scale=1.0, tail_entries=-1, n_pages=None, table_cols=None):
+    rng = np.random.default_rng(seed)
+    n_q, n_kv, d, C, lens, dtype = (case[k] for k in ("n_q", "n_kv", "d", "C", "lens", "dtype"))
+    b = len(lens)
+    chunks = [C] * b if case.get("chunks") is None else [max(c, 0) for c in case["chunks"]]
+    held = [t + c for t, c in zip(lens, chunks)]
+    pool = P.Pool(rng, [_rows(rng, n, n_kv, d, dtype) for n in held], [_rows(rng, n, n_kv, d, dtype) for n in held], n_kv, d,
+                  case["page_len"], dtype, case["fp8"], layout=layout, tail_entries=tail_entries, n_pages=n_pages, table_cols=table_cols)
+    q = P.store(rng.standard_normal((b, n_q, C, d)) * q_scale, dtype)
+    lists = None
+    if case.get("budgets") is not None:
+        lists = [[np.sort(rng.choice(t, size=min(n, t), replace=False)) if t else np.zeros(0, int) for _ in range(n_kv)]
+                 for t, n in zip(lens, case["budgets"])]
+    return rng, pool, q, chunks, lists
+
+
+def _buffers(pk, case, pool, q, lists, q_layout="heads"):
+    tq = P.to_dev(q, case["dtype"], DEV)
+    if q_layout == "tokens":
+        tq = tq.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)
+    how = {}
+    if lists is not None:
+        B = max(max(case["budgets"]), 1)
+        # entries past a list's length must not matter
+        idx = np.full((len(lists), case["n_kv"], B), -7, dtype=np.int32)
+        for i, per_head in enumerate(lists):
+            for kv, x in enumerate(per_head):
+                idx[i, kv, :len(x)] = x
+        how = dict(k_idx=torch.from_numpy(idx).to(DEV),
+                   k_cnt=torch.tensor([[len(x) for x in per] for per in lists], dtype=torch.int32, device=DEV))
+    max_kv = max(max(case["lens"]), how["k_idx"].shape[2] if how else 0)
+    buf = pk.PagedBuffers(pool.cache(), case["lens"], max_kv, q=tq, chunk_lens=case.get("chunks"), **how)
+    buf.out.fill_(float("nan"))
+    buf.lse.fill_(float("nan"))
+    buf.workspace.fill_(0xFF)   # NaN, whatever it is read as
+    return buf
+
+
+def _check(case, buf, pool, q, chunks, lists, what=""):
+    """bf16: every probability, and the output, is rounded once (relative 2^-9): |error| <= 2^-9 (P |V| + |O|), and a few units of
+    float32 rounding on top (2^-9 * 1.05 holds them).  f32: a logit of d products is off by d * 2^-24 * sum |q k| / sqrt(d) at most,
+    here below 5e-5, and a probability by as much relatively.  lse: of unrounded probabilities in float32 in either case."""
+    got = buf.out.float().cpu().numpy().astype(np.float64)
+    got_lse = buf.lse.cpu().numpy().astype(np.float64)
+    for i in range(len(chunks)):
+        n = chunks[i]
+        want, lse, weight = P.attention(q[i, :, :n].astype(np.float64), pool.k[i], pool.v[i], case["lens"][i],
+                                        None if lists is None else lists[i])
+        bound = 1.05 * 2.0 ** -9 * (weight + np.abs(want)) + 1e-6 if case["dtype"] == "bf16" else 1e-4 * weight + 1e-7
+        err = np.abs(got[i, :, :n] - want)
+        assert np.all(err <= bound), f"{what} sequence {i}: {np.nanmax(err)} (NaN: {np.isnan(err).sum()}), {np.argwhere(~(err <= bound))[:4].tolist()}"
+        e = np.abs(got_lse[i, :, :n] - lse)
+        assert np.all(e <= 1e-4), f"{what} sequence {i}: lse {np.nanmax(e)}"
+        assert np.all(got[i, :, n:] == 0.0), f"{what} sequence {i}: rows past the chunk"
+        assert np.all(np.isneginf(got_lse[i, :, n:])), f"{what} sequence {i}: lse past the chunk"
+
+
+ATTN_CASES = [
+    # single tokens and a few, lists of one and of none, lengths at the ends of pages and tiles
+    dict(dtype="bf16", fp8=True, n_q=32, n_kv=8, d=128, page_len=64, C=1, lens=[500]),
+    dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=16, C=1, lens=[0, 1, 15, 16, 17, 31, 32, 33, 63, 64]),
+    dict(dtype="bf16", fp8=False, n_q=8, n_kv=2, d=128, page_len=16, C=1, lens=[0, 1, 31, 32, 2000]),
+    dict(dtype="bf16", fp8=True, n_q=4, n_kv=4, d=64, page_len=32, C=2, lens=[129, 0, 3000]),
+    dict(dtype="bf16", fp8=False, n_q=7, n_kv=1, d=64, page_len=8, C=4, lens=[777]),
+    dict(dtype="bf16", fp8=True, n_q=16, n_kv=1, d=128, page_len=128, C=2, lens=[5000, 40]),
+    dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=64, C=8, lens=[1000, 5], chunks=[8, 3]),
+    dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=64, C=5, lens=[300, 20, 0, 9], chunks=[0, 5, 2, -1]),
+    dict(dtype="bf16", fp8=True, n_q=2, n_kv=2, d=128, page_len=1, C=1, lens=[70]),
+    dict(dtype="bf16", fp8=True, n_q=32, n_kv=8, d=128, page_len=16, C=1, lens=[100 + 13 * i for i in range(70)]),
+    # chunks
+    dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=64, C=200, lens=[700]),
+    dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=64, page_len=16, C=77, lens=[0, 130]),
+    dict(dtype="bf16", fp8=False, n_q=8, n_kv=2, d=128, page_len=32, C=129, lens=[1, 511]),
+    dict(dtype="bf16", fp8=False, n_q=12, n_kv=4, d=64, page_len=16, C=100, lens=[1237, 999, 63], chunks=[100, 31, 65]),
+    dict(dtype="bf16", fp8=True, n_q=6, n_kv=2, d=128, page_len=256, C=64, lens=[3000, 10, 0], chunks=[1, 64, 0]),
+    dict(dtype="bf16", fp8=True, n_q=32, n_kv=2, d=128, page_len=64, C=300, lens=[260]),
+    dict(dtype="bf16", fp8=True, n_q=16, n_kv=16, d=64, page_len=64, C=640, lens=[129]),
+    dict(dtype="bf16", fp8=False, n_q=32, n_kv=8, d=128, page_len=16, C=333, lens=[65, 64]),
+    dict(dtype="bf16", fp8=True, n_q=32, n_kv=8, d=64, page_len=16, C=1100, lens=[100]),       # more than 1024 row blocks
+    dict(dtype="bf16", fp8=True, n_q=32, n_kv=8, d=128, page_len=16, C=1100, lens=[100]),
+    # float32
+    dict(dtype="f32", fp8=False, n_q=4, n_kv=2, d=64, page_len=16, C=1, lens=[0, 100, 16]),
+    dict(dtype="f32", fp8=True, n_q=4, n_kv=2, d=128, page_len=32, C=1, lens=[2000]),
+    dict(dtype="f32", fp8=False, n_q=8, n_kv=2, d=128, page_len=64, C=100, lens=[333, 0], chunks=[100, 37]),
+    dict(dtype="f32", fp8=True, n_q=6, n_kv=2, d=64, page_len=16, C=70, lens=[64, 900], chunks=[0, 70]),
+    dict(dtype="f32", fp8=False, n_q=16, n_kv=1, d=64, page_len=8, C=33, lens=[31]),
+]
+
+
+@pytest.mark.parametrize("case", ATTN_CASES, ids=_ids)
+def test_attention_over_whole_sequences(case):
+    _, pool, q, chunks, lists = _attn_problem(case, 21)
+    buf = _buffers(_pk(), case, pool, q, lists)
+    buf.attn()
+    torch.cuda.synchronize()
+    _check(case, buf, pool, q, chunks, lists)
+
+
+SPARSE_CASES = [
+    dict(dtype="bf16", fp8=True, n_q=32, n_kv=8, d=128, page_len=64, C=1, lens=[3000], budgets=[360]),
+    dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=16, C=1, lens=[0, 5, 400], budgets=[10, 10, 33]),
+    dict(dtype="bf16", fp8=False, n_q=4, n_kv=2, d=64, page_len=16, C=3, lens=[1000, 300], budgets=[1, 0]),
+    dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=64, C=200, lens=[2000], budgets=[240]),
+    dict(dtype="bf16", fp8=False, n_q=12, n_kv=4, d=64, page_len=16, C=100, lens=[1500, 0, 700], budgets=[400, 5, 64],
+         chunks=[100, 77, 32]),
+    dict(dtype="bf16", fp8=True, n_q=32, n_kv=8, d=128, page_len=32, C=1100, lens=[500], budgets=[130]),
+    dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=64, page_len=32, C=70, lens=[9000], budgets=[5000]),
+    dict(dtype="f32", fp8=False, n_q=4, n_kv=2, d=64, page_len=16, C=1, lens=[300], budgets=[40]),
+    dict(dtype="f32", fp8=True, n_q=8, n_kv=2, d=128, page_len=64, C=90, lens=[800, 50], budgets=[200, 0], chunks=[90, 5]),
+]
+
+
+@pytest.mark.parametrize("case", SPARSE_CASES, ids=_ids)
+def test_attention_over_lists(case):
+    _, pool, q, chunks, lists = _attn_problem(case, 22)
+    buf = _buffers(_pk(), case, pool, q, lists)
+    buf.sparse_attn()
+    torch.cuda.synchronize()
+    _check(case, buf, pool, q, chunks, lists)
+
+
+LAYOUT_CASES = [
+    dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=16, C=1, lens=[300, 77]),
+    dict(dtype="bf16", fp8=False, n_q=8, n_kv=2, d=64, page_len=16, C=90, lens=[300, 77]),
+    dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=64, C=90, lens=[300, 77], budgets=[40, 7]),
+    dict(dtype="f32", fp8=True, n_q=8, n_kv=2, d=128, page_len=16, C=40, lens=[300, 77]),
+    dict(dtype="f32", fp8=False, n_q=8, n_kv=2, d=64, page_len=16, C=2, lens=[300, 77]),
+]
+
+
+@pytest.mark.parametrize("case", LAYOUT_CASES, ids=_ids)
+def test_attention_over_other_strides_and_entries(case):
+    """Heads inside tokens, gaps between rows, and table entries past a sequence's length that name no page."""
+    _, pool, q, chunks, lists = _attn_problem(case, 23, layout="tokens", tail_entries=2 ** 31 - 1,
+                                              table_cols=-(-(max(case["lens"]) + case["C"]) // case["page_len"]) + 9)
+    buf = _buffers(_pk(), case, pool, q, lists, q_layout="tokens")
+    buf.attn() if lists is None else buf.sparse_attn()
+    torch.cuda.synchronize()
+    _check(case, buf, pool, q, chunks, lists)
+
+
+@pytest.mark.parametrize("case", [
+    dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=64, C=1, lens=[900]),
+    dict(dtype="bf16", fp8=False, n_q=8, n_kv=2, d=64, page_len=64, C=150, lens=[900]),
+    dict(dtype="f32", fp8=False, n_q=4, n_kv=2, d=128, page_len=64, C=20, lens=[200]),
+], ids=_ids)
+def test_attention_of_large_logits(case):
+    """Queries of eight times unit variance: nearly all weight on a few keys, references that move."""
+    _, pool, q, chunks, lists = _attn_problem(case, 24, q_scale=8.0)
+    buf = _buffers(_pk(), case, pool, q, lists)
+    buf.attn()
+    torch.cuda.synchronize()
+    got = buf.out.float().cpu().numpy().astype(np.float64)
+    want, lse, weight = P.attention(q[0].astype(np.float64), pool.k[0], pool.v[0], case["lens"][0])
+    # float32 logits of eight times the size: 8 * 5e-5 relative in a probability on top of the roundings
+    bound = (1.05 * 2.0 ** -9 * (weight + np.abs(want)) if case["dtype"] == "bf16" else 0.0) + 8e-4 * weight + 1e-6
+    assert np.all(np.abs(got[0] - want) <= bound)
+    assert np.all(np.abs(buf.lse[0].cpu().numpy() - lse) <= 8e-4)
+
+
+def test_malformed_lists_and_entries_stay_inside_the_pool():
+    """Entries of a list outside the cache and of a table outside the pool are cut to some row: finite values, no fault."""
+    pk = _pk()
+    for dtype, C in (("bf16", 1), ("bf16", 70), ("f32", 5)):
+        case = dict(dtype=dtype, fp8=False, n_q=4, n_kv=2, d=64, page_len=16, C=C, lens=[200], budgets=[50])
+        _, pool, q, chunks, lists = _attn_problem(case, 25)
+        pool.k_pages.fill_(0.5)
+        pool.v_pages.fill_(0.25)
+        buf = _buffers(pk, case, pool, q, lists)
+        buf.k_idx[0, 0, ::3] = 2 ** 31 - 1
+        buf.k_idx[0, 1, ::2] = -5
+        pool.dev_table[0, 1::2] = -9
+        pool.dev_table[0, 2::4] = 10 ** 9
+        for run in (buf.attn, buf.sparse_attn):
+            out = run()
+            torch.cuda.synchronize()
+            assert torch.all(torch.abs(out.float() - 0.25) <= 1e-3)
+
+
+def test_rows_beyond_four_gib_of_a_pool():
+    """A pool of more than 2^32 bytes whose last pages are the sequence's: write, read and attend."""
+    pk = _pk()
+    n_kv, d, page_len, C, T = 8, 128, 64, 40, 100
+    n_pages = (1 << 32) // (n_kv * page_len * d * 2) + 7
+    rng = np.random.default_rng(26)
+    pages = [torch.zeros(n_pages, n_kv, page_len, d, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    table = torch.tensor([[n_pages - 1, n_pages - 5, n_pages - 2]], dtype=torch.int32, device=DEV)
+    k, v = (_rows(rng, T + C, n_kv, d, "bf16") for _ in range(2))
+    q = P.store(rng.standard_normal((1, 16, C, d)), "bf16")
+    whole = [P.to_dev(x.transpose(1, 0, 2)[None], "bf16", DEV) for x in (k, v)]
+    cache = pk.PagedCache(pages[0], pages[1], table)
+    pk.PagedBuffers(cache, [0], 0, k_chunk=whole[0], v_chunk=whole[1]).write()
+    out = [torch.empty_like(x) for x in whole]
+    pk.PagedBuffers(cache, [T + C], T + C).read(*out)
+    assert all(torch.equal(x, y) for x, y in zip(out, whole))
+    want, _, weight = P.attention(q[0].astype(np.float64), k, v, T)
+    for n in (C, 1):
+        buf = pk.PagedBuffers(cache, [T + C - n], T + C - n, q=P.to_dev(q[:, :, C - n:], "bf16", DEV))
+        got = buf.attn()[0].float().cpu().numpy()
+        w, a = want[:, C - n:], weight[:, C - n:]
+        assert np.all(np.abs(got - w) <= 1.05 * 2.0 ** -9 * (a + np.abs(w)) + 1e-6)
+
+
+# ---- as a program uses them ----------------------------------------------------------------------------------------
+
+def test_a_prompt_and_tokens_through_pages_match_the_contiguous_path():
+    """Chunks of a prompt and then single tokens, written and attended; 16-bit pages against quoka_dense_attn on contiguous tensors."""
+    pk = _pk()
+    rng = np.random.default_rng(27)
+    n_q, n_kv, d, L, C, page_len = 8, 2, 128, 300, 128, 16
+    q, k, v = (P.to_dev(rng.standard_normal((1, n, L, d)), "bf16", DEV) for n in (n_q, n_kv, n_kv))
+    table = torch.from_numpy(rng.permutation(40)[:19].astype(np.int32)).to(DEV)[None]
+    cache = pk.PagedCache.allocate(40, page_len, n_kv, d, table, dtype=torch.bfloat16)
+    at = 0
+    while at < L:
+        n = C if at + C <= 296 else (296 - at if at < 296 else 1)
+        qs, ks, vs = (x[:, :, at:at + n] for x in (q, k, v))
+        buf = pk.PagedBuffers(cache, [at], at, q=qs, k_chunk=ks, v_chunk=vs)
+        buf.write()
+        got = buf.attn()
+        ref = pk.ChunkBuffers(qs, k, v, ks, vs, [at], [0], 1, score_flags=pk.QUOKA_ATTN_SCALE_F32)
+        want = ref.dense_attn()
+        torch.cuda.synchronize()
+        # both round P and the output once: twice the bound of one, with P |V| <= 4.5 and |O| <= 4.5
+        assert torch.all(torch.abs(got.float() - want.float()) <= 2 * 2.0 ** -9 * 9.0)
+        # (the other path sums rounded probabilities)
+        assert torch.all(torch.abs(buf.lse - ref.lse) <= 2.0 ** -8)
+        at += n
+
+
+@pytest.mark.parametrize("dtype,fp8", [("bf16", True), ("bf16", False), ("f32", True)])
+def test_selection_over_pages_selects_what_the_contiguous_path_selects(dtype, fp8):
+    """The method's step over pages: the same lists as quoka_chunk_attn on the rows as the pages stand for them, and attention over
+    those lists as plain float64 has it."""
+    pk = _pk()
+    case = dict(dtype=dtype, fp8=fp8, n_q=8, n_kv=2, d=128, page_len=32, C=96, lens=[1500, 700])
+    rng, pool, q, chunks, _ = _attn_problem(case, 28)
+    budgets, n_retain = [180, 90], 32
+    tq = P.to_dev(q, dtype, DEV)
+    # the chunk's rows as the caller has them: already what the pages hold, so that they stay
+    new = [P.to_dev(np.stack([x[i][case["lens"][i]:].transpose(1, 0, 2) for i in range(2)]), dtype, DEV) for x in (pool.k, pool.v)]
+    buf = pk.PagedBuffers(pool.cache(), case["lens"], max(case["lens"]), q=tq, k_chunk=new[0], v_chunk=new[1], budgets=budgets,
+                          n_retain=n_retain)
+    buf.chunk_attn()
+    T = max(case["lens"])
+    whole = []
+    for x in (pool.k, pool.v):
+        y = np.zeros((2, 2, T, 128))
+        for i, n in enumerate(case["lens"]):
+            y[i, :, :n] = x[i][:n].transpose(1, 0, 2)
+        whole.append(P.to_dev(y, dtype, DEV))
+    ref = pk.ChunkBuffers(tq, whole[0], whole[1], new[0], new[1], case["lens"], budgets, n_retain)
+    ref.chunk_attn()
+    torch.cuda.synchronize()
+    assert torch.equal(buf.k_cnt, ref.k_cnt) and torch.equal(buf.q_idx, ref.q_idx)
+    lists = []
+    for i in range(2):
+        n = int(ref.k_cnt[i, 0])
+        assert torch.equal(buf.k_idx[i, :, :n], ref.k_idx[i, :, :n])
+        lists.append([buf.k_idx[i, kv, :n].cpu().numpy() for kv in range(2)])
+    _check(case, buf, pool, q, chunks, lists)
+
+
+def test_calls_on_another_stream_and_from_a_graph():
+    """Write, attention (decode-sized, chunk-sized, ragged) and read on a side stream, recorded and replayed on fresh inputs."""
+    pk = _pk()
+    for C, chunks in ((1, None), (80, None), (80, [80, 3])):
+        case = dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=16, C=C, lens=[400, 90], chunks=chunks)
+        _, pool, q, _, _ = _attn_problem(case, 29)
+        tq = P.to_dev(q, "bf16", DEV)
+        new = [torch.randn(2, 2, C, 128, device=DEV).bfloat16() for _ in range(2)]
+        buf = pk.PagedBuffers(pool.cache(), case["lens"], 400, q=tq, k_chunk=new[0], v_chunk=new[1], chunk_lens=chunks)
+        k_out, v_out = (torch.zeros(2, 2, 400, 128, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+
+        def step():
+            buf.write()
+            buf.attn()
+            buf.read(k_out, v_out)
+
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+        torch.cuda.synchronize()
+        for rep in range(3):
+            tq.copy_(torch.randn_like(tq))
+            new[0].copy_(torch.randn_like(new[0]))
+            new[1].copy_(torch.randn_like(new[1]))
+            buf.out.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            got = [x.clone() for x in (buf.out, buf.lse, k_out, v_out, pool.k_scale)]
+            float(torch.randn(1 << 16, device=DEV).sum())
+            torch.cuda.synchronize()
+            buf.out.zero_()
+            step()
+            torch.cuda.synchronize()
+            for x, y in zip(got, (buf.out, buf.lse, k_out, v_out, pool.k_scale)):
+                assert torch.equal(x, y), f"replay {rep}"
+
+
+def test_the_example_runs():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "paged_generation.py")
+    spec = importlib.util.spec_from_file_location("paged_generation", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    # an 8-bit element is off by 2^-4 at most, 0.027 (root mean square) of itself: K's and V's errors add up to 0.04 or so
+    assert mod.main(prompt=700, tokens=5, chunk=256) < 0.06

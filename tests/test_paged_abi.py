@@ -1,0 +1,121 @@
+"""What the entry points for caches in pages refuse, and what their structure looks like, without a GPU: nothing is launched."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2602_08722_amd as pk
+from tests.test_abi import _shape
+
+AT, WS, BIG = ctypes.c_void_p(0x1000), ctypes.c_void_p(0x10000), ctypes.c_size_t(1 << 40)   # never followed
+
+
+def _pages(**kw):
+    p = pk.QuokaPages()
+    vals = dict(k=0x1000, v=0x2000, k_scale=0x3000, v_scale=0x3001, page_table=0x4000, n_pages=100, page_len=16, max_pages=80,
+                format=pk.QUOKA_PAGES_FP8)
+    stride = kw.pop("stride", (2 * 16 * 128, 16 * 128, 128))
+    vals.update(kw)
+    for k, v in vals.items():
+        setattr(p, k, v)
+    p.stride = (ctypes.c_int64 * 3)(*stride)
+    return p
+
+
+def _calls(shape, pages):
+    """Status of each entry point with otherwise valid arguments that lead to a refusal."""
+    lib = pk.load_library()
+    s, p = ctypes.byref(shape), None if pages is None else ctypes.byref(pages)
+    return (lib.quoka_cache_write(s, p, AT, AT, AT, None, None), lib.quoka_cache_read(s, p, AT, AT, AT, None),
+            lib.quoka_paged_attn(s, p, AT, AT, None, None, None, AT, None, WS, BIG, None))
+
+
+def test_struct_layout():
+    # five pointers, three int64, four int32
+    assert ctypes.sizeof(pk.QuokaPages) == 5 * 8 + 3 * 8 + 4 * 4
+    assert pk.QuokaPages.stride.offset == 40 and pk.QuokaPages.n_pages.offset == 64
+    lib = pk.load_library()
+    assert lib.quoka_version() >= 200
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(k=0), 1), (dict(v=0), 1), (dict(page_table=0), 1), (dict(k_scale=0), 1), (dict(v_scale=0), 1),
+    (dict(k=0x1008), 1), (dict(v=0x1004), 1),
+    (dict(n_pages=0), 1), (dict(max_pages=0), 1), (dict(page_len=0), 1), (dict(page_len=48), 1), (dict(page_len=-16), 1),
+    (dict(page_len=131072), 2), (dict(format=2), 2), (dict(format=-1), 2),
+    (dict(max_pages=62), 1),                                          # 62 * 16 tokens for 1000
+    (dict(stride=(4096, 2048, 64)), 1), (dict(stride=(4096, 2048, 136)), 1), (dict(stride=(4104, 2048, 128)), 1),
+    (dict(stride=(4096, -2048, 128)), 1),
+])
+def test_bad_pages_are_refused(kw, code):
+    assert _calls(_shape(pk), _pages(**kw)) == (code,) * 3
+
+
+def test_no_pages_and_bad_shapes_are_refused():
+    assert _calls(_shape(pk), None) == (1,) * 3
+    for kw, code in ((dict(head_dim=96), 2), (dict(dtype=7), 2), (dict(batch=0), 1), (dict(n_q_heads=7), 1), (dict(chunk_len=8193), 2)):
+        assert _calls(_shape(pk, **kw), _pages()) == (code,) * 3
+    n = ctypes.c_size_t(0)
+    assert pk.load_library().quoka_paged_workspace_bytes(ctypes.byref(_shape(pk, head_dim=32)), ctypes.byref(n)) == 2
+    assert pk.load_library().quoka_paged_workspace_bytes(ctypes.byref(_shape(pk)), None) == 1
+
+
+def test_bad_pointers_and_workspaces_are_refused():
+    lib, p = pk.load_library(), ctypes.byref(_pages())
+    odd, null = ctypes.c_void_p(0x1004), None
+    s = ctypes.byref(_shape(pk))
+    for args in ((null, AT, AT), (AT, null, AT), (AT, AT, null), (odd, AT, AT), (AT, odd, AT)):
+        assert lib.quoka_cache_write(s, p, *args, None, None) == 1
+    for args in ((null, AT, AT), (AT, null, null), (AT, odd, AT), (AT, AT, odd)):
+        assert lib.quoka_cache_read(s, p, *args, None) == 1
+    for q, lens, idx, cnt, out, ws, code in ((null, AT, null, null, AT, WS, 1), (AT, null, null, null, AT, WS, 1),
+                                             (AT, AT, AT, null, AT, WS, 1), (AT, AT, null, null, null, WS, 1),
+                                             (odd, AT, null, null, AT, WS, 1), (AT, AT, null, null, odd, WS, 1),
+                                             (AT, AT, null, null, AT, null, 1), (AT, AT, null, null, AT, ctypes.c_void_p(0x10010), 3)):
+        assert lib.quoka_paged_attn(s, p, q, lens, None, idx, cnt, out, None, ws, BIG, None) == code
+    need = ctypes.c_size_t(0)
+    assert lib.quoka_paged_workspace_bytes(s, ctypes.byref(need)) == 0 and need.value > 0 and need.value % 256 == 0
+    assert lib.quoka_paged_attn(s, p, AT, AT, None, None, None, AT, None, WS, ctypes.c_size_t(need.value - 1), None) == 3
+
+
+def _cache(dtype=torch.float8_e4m3fn, batch=2, n_kv=2, d=64, page_len=16, cols=4):
+    return pk.PagedCache.allocate(10, page_len, n_kv, d, torch.zeros((batch, cols), dtype=torch.int32), dtype=dtype)
+
+
+def test_the_binding_refuses_tensors_that_do_not_fit(monkeypatch):
+    monkeypatch.setattr(pk.binding, "_stream", lambda stream: None)   # (no GPU to ask; every call below is refused ahead of it)
+    pool = torch.zeros(10, 2, 16, 64, dtype=torch.bfloat16)
+    table = torch.zeros(2, 4, dtype=torch.int32)
+    scale = torch.zeros(10, 2, 16, dtype=torch.uint8)
+    with pytest.raises(TypeError):
+        pk.make_pages(pool.half(), pool.half(), table)
+    for args in ((pool, pool[:5], table), (pool, pool.float(), table), (pool, pool, table.long()), (pool, pool, table[0]),
+                 (pool.to(torch.float8_e4m3fn),) * 2 + (table,), (pool.to(torch.float8_e4m3fn),) * 2 + (table, scale, scale[:, :, :8])):
+        with pytest.raises(ValueError):
+            pk.make_pages(*args)
+    cache = _cache()
+    q, kc = torch.zeros(2, 4, 3, 64, dtype=torch.bfloat16), torch.zeros(2, 2, 3, 64, dtype=torch.bfloat16)
+    pk.PagedBuffers(cache, [1, 2], 60, q=q, k_chunk=kc, v_chunk=kc)
+    with pytest.raises(TypeError):   # 16-bit pages with a float32 chunk
+        pk.PagedBuffers(_cache(torch.bfloat16), [1, 2], 60, q=q.float())
+    idx, cnt = torch.zeros(2, 2, 5, dtype=torch.int32), torch.zeros(2, 2, dtype=torch.int32)
+    for how in (dict(k_chunk=kc), dict(q=q[:1]), dict(q=q, k_chunk=kc[:, :, :2], v_chunk=kc[:, :, :2]), dict(q=q, k_chunk=q, v_chunk=q),
+                dict(q=q, chunk_lens=[1]), dict(q=q, k_idx=idx), dict(q=q, k_idx=idx.long(), k_cnt=cnt), dict(q=q, k_idx=idx[:, :, ::2], k_cnt=cnt),
+                dict(q=q, budgets=[3, 3]), dict(q=q, k_chunk=kc, v_chunk=kc, budgets=[3, 3], chunk_lens=[1, 1]),
+                dict(k_chunk=kc, v_chunk=kc.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3))):
+        with pytest.raises(ValueError):
+            pk.PagedBuffers(cache, [1, 2], 60, **how)
+    with pytest.raises(ValueError):
+        pk.PagedBuffers(cache, [1, 2, 3], 60)
+    with pytest.raises(pk.QuokaError):   # a table of 64 positions
+        pk.PagedBuffers(cache, [1, 2], 65, k_chunk=kc, v_chunk=kc).write()
+    bare = pk.PagedBuffers(cache, [1, 2], 60)
+    for call in (bare.write, bare.attn, bare.sparse_attn, bare.chunk_attn):
+        with pytest.raises(ValueError):
+            call()
+    out = torch.zeros(2, 2, 60, 64, dtype=torch.bfloat16)
+    for args, error in (((out.half(),), TypeError), ((out[:, :, :59],), ValueError), ((out, out.float()), ValueError)):
+        with pytest.raises(error):
+            bare.read(*args)
+    with pytest.raises(TypeError):
+        pk.PagedBuffers(_cache(torch.float32), [1, 2], 60).read(out)
