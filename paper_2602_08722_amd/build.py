@@ -13,7 +13,7 @@ OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libquoka.so")
 
 SOURCES = ["api.hip", "select_queries.hip", "score_keys.hip", "topk_keys.hip", "select_keys.hip", "score_stream.hip", "attn_mfma.hip", "attn_decode.hip", "attn_f32.hip",
-           "pages.hip", "paged_attn.hip", "probes.hip"]
+           "pages.hip", "paged_attn.hip", "attn_mfma_paged.hip", "probes.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -25,7 +25,7 @@ FLAGS = [
 ]
 
 # Where the attention kernel's loop begins in a 64-byte line of code moves its time by 1 % either way with every change before it.
-SOURCE_FLAGS = {"attn_mfma.hip": ["-falign-loops=64"]}
+SOURCE_FLAGS = {src: ["-falign-loops=64"] for src in ("attn_mfma.hip", "attn_mfma_paged.hip")}
 
 
 def _compile(src: str, extra) -> str:
@@ -40,7 +40,7 @@ def _compile(src: str, extra) -> str:
     return obj
 
 
-def build(extra_flags=(), jobs: int = 6) -> str:
+def build(extra_flags=(), jobs: int = 8) -> str:
     os.makedirs(OBJ, exist_ok=True)
     with ThreadPoolExecutor(max_workers=jobs) as ex:
         objs = list(ex.map(lambda s: _compile(s, list(extra_flags)), SOURCES))

@@ -1,0 +1,38 @@
+// The bf16 attention kernel (attn_mfma.hip.h) over a cache in pages.
+#include "attn_mfma.hip.h"
+
+namespace quoka {
+
+template <int D, bool SPLIT, int SRC>
+static hipError_t launch_paged_ds(const Dims& dm, const PagedAttnArgs& a, hipStream_t st) {
+  if (a.n_splits > 1) return launch_variant<D, SPLIT, true, true, false, SRC>(dm, a, st);
+  return launch_variant<D, SPLIT, true, false, SPLIT || D == 128, SRC>(dm, a, st);
+}
+
+hipError_t launch_paged_attn_bf16(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st) {
+  const AttnPlan p = attn_plan(dm, a.k_idx != nullptr);
+  PagedAttnArgs aa;
+  aa.q = a.q;
+  aa.k_cache = aa.v_cache = aa.k_chunk = aa.v_chunk = nullptr;
+  aa.k_idx = a.k_idx;
+  aa.n_cache = a.k_idx != nullptr ? a.k_cnt : a.kv_lens;
+  aa.out = a.out;
+  aa.lse = a.lse;
+  aa.part = part;
+  aa.n_splits = p.n_splits;
+  aa.kv_lens = a.kv_lens;
+  aa.chunk_lens = a.chunk_lens;
+  aa.pg = a.pg;
+  auto launch = [&](auto d, auto src) {
+    constexpr int D = decltype(d)::value, SRC = decltype(src)::value;
+    return p.split_tile ? launch_paged_ds<D, true, SRC>(dm, aa, st) : launch_paged_ds<D, false, SRC>(dm, aa, st);
+  };
+  using d64 = std::integral_constant<int, 64>;
+  using d128 = std::integral_constant<int, 128>;
+  using raw = std::integral_constant<int, kRawPages>;
+  using eight_bit = std::integral_constant<int, kFp8Pages>;
+  if (dm.d == 64) return fp8 ? launch(d64{}, eight_bit{}) : launch(d64{}, raw{});
+  return fp8 ? launch(d128{}, eight_bit{}) : launch(d128{}, raw{});
+}
+
+}  // namespace quoka

@@ -146,6 +146,7 @@ struct PagedArgs {
   float* lse;                            // may be nullptr
   Pages pg;
 };
+hipError_t launch_paged_attn_bf16(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st);   // (partials as attn_bf16)
 size_t paged_attn_ws_floats(const Dims& dm, int dtype);
 hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float* part, hipStream_t st);
 

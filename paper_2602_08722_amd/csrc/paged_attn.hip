@@ -8,9 +8,9 @@ constexpr int kPaThreads = 256;
 template <typename T, bool FP8>
 __device__ __forceinline__ void load_row8(const void* pages, long long row, int e0, float scale, float (&x)[8]) {
   if constexpr (FP8) {
-    const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(pages) + row + e0);
-    widen_f32(w.x, scale, x);
-    widen_f32(w.y, scale, x + 4);
+    const u32x2 w = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(pages) + row + e0);
+    widen_f32(w[0], scale, x);
+    widen_f32(w[1], scale, x + 4);
   } else {
     Elem<T>::load8(static_cast<const T*>(pages) + row + e0, x);
   }
@@ -37,7 +37,8 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_rows(Dims dm, PagedArgs
   const int n_list = a.k_idx == nullptr ? T_b : min(max(a.k_cnt[b * dm.n_kv + kv], 0), dm.B_max);
   const int32_t* list = a.k_idx == nullptr ? nullptr : a.k_idx + (long long)(b * dm.n_kv + kv) * dm.B_max;
   const int32_t* table = pg.table + (long long)b * pg.max_pages;
-  const int total = i < C ? n_list + i + 1 : 0;
+  if (i >= C) return;
+  const int total = n_list + i + 1;
   const float scale = 1.0f / sqrtf((float)D);
   float m_run = -INFINITY, l_run = 0.f, acc[EPL];
 #pragma unroll
@@ -82,16 +83,37 @@ __global__ __launch_bounds__(kPaThreads) void paged_attn_rows(Dims dm, PagedArgs
   T* out = static_cast<T*>(a.out) + b * dm.os[0] + h * dm.os[1] + i * dm.os[2];
 #pragma unroll
   for (int e = 0; e < EPL; ++e) {
-    const float o = total > 0 ? acc[e] / l_run : 0.f;
+    const float o = acc[e] / l_run;
     if constexpr (sizeof(T) == 2) out[lane + 64 * e] = (T)f32_to_bf16_bits(o);
     else out[lane + 64 * e] = o;
   }
-  if (a.lse != nullptr && lane == 0) a.lse[(long long)(b * dm.n_q + h) * dm.C + i] = total > 0 ? m_run + logf(l_run) : -INFINITY;
+  if (a.lse != nullptr && lane == 0) a.lse[(long long)(b * dm.n_q + h) * dm.C + i] = m_run + logf(l_run);
 }
 
-size_t paged_attn_ws_floats(const Dims&, int) { return 0; }
+// Rows past a sequence's chunk: zeros, and no weight at all.  (A launch of its own, and only where lengths are given, since the attention
+// kernels' grids follow the chunk's row blocks and such rows may be most of a ragged batch.)
+constexpr int kFillRows = 32;
+__global__ __launch_bounds__(256) void paged_fill(Dims dm, PagedArgs a, int row_units) {   // row_units: 16-byte units of a row
+  const int h = blockIdx.y, b = blockIdx.z, C = max(min(a.chunk_lens[b], dm.C), 0);
+  const int i0 = max((int)blockIdx.x * kFillRows, C), i1 = min((int)(blockIdx.x + 1) * kFillRows, dm.C);
+  const long long es = dm.d * 2 == row_units * 16 ? 2 : 4;
+  char* out = static_cast<char*>(a.out) + (b * dm.os[0] + h * dm.os[1]) * es;
+  for (int u = threadIdx.x; u < (i1 - i0) * row_units; u += 256)
+    *reinterpret_cast<u32x4*>(out + (i0 + u / row_units) * dm.os[2] * es + (u % row_units) * 16) = u32x4{0u, 0u, 0u, 0u};
+  if (a.lse != nullptr)
+    for (int i = i0 + threadIdx.x; i < i1; i += 256) a.lse[(long long)(b * dm.n_q + h) * dm.C + i] = -INFINITY;
+}
 
-hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float*, hipStream_t st) {
+size_t paged_attn_ws_floats(const Dims& dm, int dtype) { return dtype == QUOKA_BF16 ? attn_bf16_ws_floats(dm) : 0; }
+
+hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float* part, hipStream_t st) {
+  if (a.chunk_lens != nullptr) {
+    hipLaunchKernelGGL(paged_fill, dim3((dm.C + kFillRows - 1) / kFillRows, dm.n_q, dm.b), dim3(256), 0, st, dm, a,
+                       dm.d * (dtype == QUOKA_BF16 ? 2 : 4) / 16);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (dtype == QUOKA_BF16 && !attn_decode_applies(dm)) return launch_paged_attn_bf16(dm, fp8, a, part, st);
   const dim3 grid((dm.C + 3) / 4, dm.n_q, dm.b);
   auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(kPaThreads), 0, st, dm, a);

@@ -49,16 +49,16 @@ __device__ __forceinline__ void put_row(const Eight<T>& x, void* pages, uint8_t*
     for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x.at(e)));
     const uint32_t ex = row_exponent(row_max<D / 8>(top));
     const float by = row_scale(254u - ex);
-    uint2 q;
+    u32x2 q;
     int lo = 0, hi = 0;
     lo = __builtin_amdgcn_cvt_pk_fp8_f32(x.at(0) * by, x.at(1) * by, lo, false);
     lo = __builtin_amdgcn_cvt_pk_fp8_f32(x.at(2) * by, x.at(3) * by, lo, true);
     hi = __builtin_amdgcn_cvt_pk_fp8_f32(x.at(4) * by, x.at(5) * by, hi, false);
     hi = __builtin_amdgcn_cvt_pk_fp8_f32(x.at(6) * by, x.at(7) * by, hi, true);
-    q.x = (uint32_t)lo;
-    q.y = (uint32_t)hi;
+    q[0] = (uint32_t)lo;
+    q[1] = (uint32_t)hi;
     if (on) {
-      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(pages) + row + 8 * c) = q;
+      *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(pages) + row + 8 * c) = q;
       if (c == 0) scales[scale_row] = (uint8_t)ex;
     }
   }
@@ -126,12 +126,12 @@ __global__ __launch_bounds__(kPgThreads) void cache_read(Dims dm, Pages pg, cons
       if (t < T_b) x[u].store(out + t * dm.kvs[2]);
     }
   } else {
-    uint2 x[U];
+    u32x2 x[U];
     uint32_t e[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int slot = slot_of(pg, min(first + u * RPB + r0, T_b - 1));
-      x[u] = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(pages) + row_at(pg, page[u], kv, slot) + 8 * c);
+      x[u] = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(pages) + row_at(pg, page[u], kv, slot) + 8 * c);
       e[u] = scales[scale_at(pg, page[u], kv, slot)];
     }
 #pragma unroll
@@ -142,8 +142,8 @@ __global__ __launch_bounds__(kPgThreads) void cache_read(Dims dm, Pages pg, cons
         y.w[0] = widen_bf16(x[u], row_scale(e[u]));
       } else {
         float f[8];
-        widen_f32(x[u].x, row_scale(e[u]), f);
-        widen_f32(x[u].y, row_scale(e[u]), f + 4);
+        widen_f32(x[u][0], row_scale(e[u]), f);
+        widen_f32(x[u][1], row_scale(e[u]), f + 4);
 #pragma unroll
         for (int i = 0; i < 8; ++i) y.w[i / 4][i % 4] = __float_as_uint(f[i]);
       }

@@ -6,6 +6,7 @@
 namespace quoka {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // The page of position `pos` of the sequence whose table row starts at `table`, for readers: some page of the pool whatever the entry.
@@ -30,12 +31,12 @@ __device__ __forceinline__ uint32_t row_exponent(float top) {
 }
 
 // Eight 8-bit elements times a power of two.  To bfloat16 (four significant bits and a power of two: exact down to 2^-126), to float.
-__device__ __forceinline__ u32x4 widen_bf16(uint2 x, float scale) {
+__device__ __forceinline__ u32x4 widen_bf16(u32x2 x, float scale) {
   u32x4 r;
-  r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.x, scale, false));
-  r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.x, scale, true));
-  r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.y, scale, false));
-  r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.y, scale, true));
+  r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[0], scale, false));
+  r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[0], scale, true));
+  r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[1], scale, false));
+  r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[1], scale, true));
   return r;
 }
 __device__ __forceinline__ void widen_f32(uint32_t x, float scale, float* v) {
