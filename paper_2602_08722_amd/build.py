@@ -13,7 +13,7 @@ OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libquoka.so")
 
 SOURCES = ["api.hip", "select_queries.hip", "score_keys.hip", "topk_keys.hip", "select_keys.hip", "score_stream.hip", "attn_mfma.hip", "attn_decode.hip", "attn_f32.hip",
-           "pages.hip", "paged_attn.hip", "attn_mfma_paged.hip", "probes.hip"]
+           "pages.hip", "paged_attn.hip", "paged_decode.hip", "attn_mfma_paged.hip", "probes.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

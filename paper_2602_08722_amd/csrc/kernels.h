@@ -147,6 +147,9 @@ struct PagedArgs {
   Pages pg;
 };
 hipError_t launch_paged_attn_bf16(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st);   // (partials as attn_bf16)
+// up to 32 query rows per KV head
+size_t paged_decode_ws_floats(const Dims& dm);
+hipError_t launch_paged_decode(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st);
 size_t paged_attn_ws_floats(const Dims& dm, int dtype);
 hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float* part, hipStream_t st);
 

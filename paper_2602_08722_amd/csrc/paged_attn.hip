@@ -104,7 +104,10 @@ __global__ __launch_bounds__(256) void paged_fill(Dims dm, PagedArgs a, int row_
     for (int i = i0 + threadIdx.x; i < i1; i += 256) a.lse[(long long)(b * dm.n_q + h) * dm.C + i] = -INFINITY;
 }
 
-size_t paged_attn_ws_floats(const Dims& dm, int dtype) { return dtype == QUOKA_BF16 ? attn_bf16_ws_floats(dm) : 0; }
+size_t paged_attn_ws_floats(const Dims& dm, int dtype) {
+  if (dtype != QUOKA_BF16) return 0;
+  return attn_decode_applies(dm) ? paged_decode_ws_floats(dm) : attn_bf16_ws_floats(dm);
+}
 
 hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float* part, hipStream_t st) {
   if (a.chunk_lens != nullptr) {
@@ -113,16 +116,13 @@ hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArg
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (dtype == QUOKA_BF16 && !attn_decode_applies(dm)) return launch_paged_attn_bf16(dm, fp8, a, part, st);
+  if (dtype == QUOKA_BF16)
+    return attn_decode_applies(dm) ? launch_paged_decode(dm, fp8, a, part, st) : launch_paged_attn_bf16(dm, fp8, a, part, st);
   const dim3 grid((dm.C + 3) / 4, dm.n_q, dm.b);
   auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(kPaThreads), 0, st, dm, a);
     return hipGetLastError();
   };
-  if (dtype == QUOKA_BF16) {
-    if (dm.d == 64) return fp8 ? launch(paged_attn_rows<uint16_t, true, 64>) : launch(paged_attn_rows<uint16_t, false, 64>);
-    return fp8 ? launch(paged_attn_rows<uint16_t, true, 128>) : launch(paged_attn_rows<uint16_t, false, 128>);
-  }
   if (dm.d == 64) return fp8 ? launch(paged_attn_rows<float, true, 64>) : launch(paged_attn_rows<float, false, 64>);
   return fp8 ? launch(paged_attn_rows<float, true, 128>) : launch(paged_attn_rows<float, false, 128>);
 }
