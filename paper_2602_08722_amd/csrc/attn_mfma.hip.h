@@ -33,9 +33,7 @@
 // it (two barriers a tile, staging through registers), attention by itself, us: 32/8 heads, d 128, 4096 tokens over 8192 keys 622 -> 551
 // (1.25 PFLOP/s), 2048 over 3932 172 -> 147, 1024 over 983 38.1 -> 31.7, 1024 over 8192 161 -> 135; d 64, 1500 over 2400 70 -> 59.
 #pragma once
-#include "common.hip.h"
-#include "kernels.h"
-#include "pages.hip.h"
+#include "attn_src.hip.h"
 
 #include <type_traits>
 
@@ -88,23 +86,6 @@ __device__ __forceinline__ int v_swizzle(int row) { return D == 128 ? 4 * (row &
 
 template <int D>
 __device__ __forceinline__ int q_swizzle(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
-
-// Where the rows of the cache and the chunk lie: in tensors of their own, or in pages, which hold both, as they are or in 8 bits.
-constexpr int kContiguous = 0, kRawPages = 1, kFp8Pages = 2;
-struct PagedAttnArgs : AttnArgs {   // (n_cache: as in AttnArgs)
-  const int32_t *kv_lens = nullptr, *chunk_lens = nullptr;
-  Pages pg = {};
-};
-template <int SRC>
-using attn_args = std::conditional_t<SRC == kContiguous, AttnArgs, PagedAttnArgs>;
-// tokens of batch entry b's chunk
-__device__ __forceinline__ int chunk_of(const Dims& dm, const AttnArgs&, int b) { return dm.chunk(b); }
-__device__ __forceinline__ int chunk_of(const Dims& dm, const PagedAttnArgs& a, int b) {
-  return a.chunk_lens == nullptr ? dm.C : max(min(a.chunk_lens[b], dm.C), 0);
-}
-// its cached tokens (in pages; elsewhere nothing asks)
-__device__ __forceinline__ int paged_len(const Dims&, const AttnArgs&, int) { return 0; }
-__device__ __forceinline__ int paged_len(const Dims& dm, const PagedAttnArgs& a, int b) { return min(max(a.kv_lens[b], 0), dm.T_max); }
 
 template <int D, bool SPLIT, int SRC = kContiguous>
 struct AttnCfg {
@@ -173,10 +154,10 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   // in a row.
   const int n_given = a.n_cache[sparse ? b * dm.n_kv + kv : b * dm.ls];
   if constexpr (!PAGED)
-  asm volatile("" ::"s"(dm.g), "s"(dm.C), "s"(dm.T_max), "s"(dm.B_max), "s"(dm.C_last),
-               "s"(dm.qs[0]), "s"(dm.qs[1]), "s"(dm.qs[2]), "s"(dm.kvs[0]), "s"(dm.kvs[1]), "s"(dm.kvs[2]), "s"(dm.cks[0]), "s"(dm.cks[1]),
-               "s"(dm.cks[2]), "s"(a.q), "s"(a.k_cache), "s"(a.v_cache), "s"(a.k_chunk), "s"(a.v_chunk), "s"(a.k_idx),
-               "s"(a.n_cache), "s"(a.adjacent), "s"(a.inv_g));
+    asm volatile("" ::"s"(dm.g), "s"(dm.C), "s"(dm.T_max), "s"(dm.B_max), "s"(dm.C_last),
+                 "s"(dm.qs[0]), "s"(dm.qs[1]), "s"(dm.qs[2]), "s"(dm.kvs[0]), "s"(dm.kvs[1]), "s"(dm.kvs[2]), "s"(dm.cks[0]), "s"(dm.cks[1]),
+                 "s"(dm.cks[2]), "s"(a.q), "s"(a.k_cache), "s"(a.v_cache), "s"(a.k_chunk), "s"(a.v_chunk), "s"(a.k_idx),
+                 "s"(a.n_cache), "s"(a.adjacent), "s"(a.inv_g));
   const int tid = threadIdx.x % kSetThreads, lane = tid & 63;                 // position inside the wave set
   // wave-uniform values are pinned to scalar registers so that everything derived from them (tile kind, base
   // pointers, branches) stays scalar too

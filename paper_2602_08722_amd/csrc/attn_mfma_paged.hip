@@ -11,18 +11,8 @@ static hipError_t launch_paged_ds(const Dims& dm, const PagedAttnArgs& a, hipStr
 
 hipError_t launch_paged_attn_bf16(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st) {
   const AttnPlan p = attn_plan(dm, a.k_idx != nullptr);
-  PagedAttnArgs aa;
-  aa.q = a.q;
-  aa.k_cache = aa.v_cache = aa.k_chunk = aa.v_chunk = nullptr;
-  aa.k_idx = a.k_idx;
-  aa.n_cache = a.k_idx != nullptr ? a.k_cnt : a.kv_lens;
-  aa.out = a.out;
-  aa.lse = a.lse;
-  aa.part = part;
+  PagedAttnArgs aa = paged_attn_args(a, part);
   aa.n_splits = p.n_splits;
-  aa.kv_lens = a.kv_lens;
-  aa.chunk_lens = a.chunk_lens;
-  aa.pg = a.pg;
   auto launch = [&](auto d, auto src) {
     constexpr int D = decltype(d)::value, SRC = decltype(src)::value;
     return p.split_tile ? launch_paged_ds<D, true, SRC>(dm, aa, st) : launch_paged_ds<D, false, SRC>(dm, aa, st);
