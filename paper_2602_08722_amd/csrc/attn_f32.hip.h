@@ -64,7 +64,7 @@ __device__ __forceinline__ FaRow fa_row(int r, int g) { return {r / g, r % g}; }
 // stay, and the way through LDS costs 0.5 us (5 tokens over 45 keys 8.9 / 9.4; eight waves of one unit, 60 tokens over 360 keys 18.2 /
 // 16.7), and at d 64, with half the lines, 4 - 7 % throughout: those take the operands as they come.
 // SRC = kRawPages, kFp8Pages: every row is found through the page table, an entry of a list two units ahead of its page and the page a unit
-// ahead of the rows; offsets are numbers of 16 elements.  8-bit rows are widened in registers, exactly, and never staged: a row is one line.
+// ahead of the rows; offsets are numbers of 16 bytes.  8-bit rows are widened in registers, exactly, and never staged: a row is one line.
 template <int D, bool STAGED, int SRC = kContiguous>
 __global__ __launch_bounds__(kFaThreads, 2) void attn_f32(Dims dm, attn_args<SRC> a, float* __restrict__ part, int n_splits) {
   using Cfg = FaCfg<D, SRC>;
@@ -133,11 +133,10 @@ __global__ __launch_bounds__(kFaThreads, 2) void attn_f32(Dims dm, attn_args<SRC
     v_pool = reinterpret_cast<uint64_t>(a.pg.v) + (uint64_t)kv * a.pg.st[1] * es;
     k_scales = a.pg.k_scale + ((size_t)kv << a.pg.shift);
     v_scales = a.pg.v_scale + ((size_t)kv << a.pg.shift);
-    page_units = (uint32_t)(a.pg.st[0] / 16);
-    slot_units = (uint32_t)(a.pg.st[2] / 16);
+    page_units = (uint32_t)(a.pg.st[0] / (16 / es));
+    slot_units = (uint32_t)(a.pg.st[2] / (16 / es));
     page_scales = (uint32_t)a.pg.n_kv << a.pg.shift;
   }
-  constexpr int kUnitShift = FP8 ? 4 : 6;   // bytes of 16 elements
   auto look_up_page = [&](int u) __attribute__((always_inline)) {   // (its entries have been looked up)
     if constexpr (PAGED) {
       u = min(u, units - 1);   // (past the end the last unit again: positions that the sequence has)
@@ -173,7 +172,7 @@ __global__ __launch_bounds__(kFaThreads, 2) void attn_f32(Dims dm, attn_args<SRC
   float k_by = 1.f;   // FP8: the power of two of the K row in kreg8
   auto request_k = [&](int u, uint32_t off) __attribute__((always_inline)) {
     if constexpr (PAGED && !STAGED) {
-      const uint64_t row = k_pool + ((uint64_t)off << kUnitShift) + (FP8 ? 4 : 16) * hf;
+      const uint64_t row = k_pool + ((uint64_t)off << 4) + (FP8 ? 4 : 16) * hf;
       typedef const f32x4 __attribute__((address_space(1))) * global_f4;
       typedef const uint32_t __attribute__((address_space(1))) * global_u;
 #pragma unroll
@@ -196,7 +195,7 @@ __global__ __launch_bounds__(kFaThreads, 2) void attn_f32(Dims dm, attn_args<SRC
 #pragma unroll
       for (int j = 1; j < RPL; ++j) row = lane / CG == j ? (uint32_t)__builtin_amdgcn_readlane((int)off, i * RPL + j) : row;
       if constexpr (PAGED)
-        dma16(reinterpret_cast<const void*>(k_pool + ((uint64_t)row << kUnitShift) + (uint32_t)(lane % CG ^ (r & 15)) * 16u),
+        dma16(reinterpret_cast<const void*>(k_pool + ((uint64_t)row << 4) + (uint32_t)(lane % CG ^ (r & 15)) * 16u),
               kt_lds + (uint32_t)i * 1024u);
       else
         dma16(base, row + (uint32_t)(lane % CG ^ (r & 15)) * 16u, kt_lds + (uint32_t)i * 1024u);
@@ -260,7 +259,7 @@ __global__ __launch_bounds__(kFaThreads, 2) void attn_f32(Dims dm, attn_args<SRC
       typedef const eight_bit __attribute__((address_space(1))) * global_row8;
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
-        const uint64_t at = v_pool + ((uint64_t)voff[v] << kUnitShift) + (FP8 ? DB : DB * 4) * li;
+        const uint64_t at = v_pool + ((uint64_t)voff[v] << 4) + (FP8 ? DB : DB * 4) * li;
         if constexpr (FP8) vreg8[v] = *(global_row8)at;
         else vreg[v] = *(global_row)at;
       }

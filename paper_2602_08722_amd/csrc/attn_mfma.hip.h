@@ -195,7 +195,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
 
   // The tensor this set stages (set 0: K, set 1: V) for this (batch, KV head), as byte pointers: every row is
   // addressed as base + 32-bit byte offset (the host checks that a head's rows span less than 4 GiB).
-  // PAGED: the head's part of the pool, and rows as 32-bit numbers of 16 elements (the host checks that they fit).
+  // PAGED: the head's part of the pool, and rows as 32-bit numbers of 16 bytes (the host checks that they fit).
   const void* cache_t = set == 0 ? a.k_cache : a.v_cache;
   const void* chunk_t = set == 0 ? a.k_chunk : a.v_chunk;
   const char* cache_base = reinterpret_cast<const char*>(static_cast<const uint16_t*>(cache_t) + b * dm.kvs[0] + kv * dm.kvs[1]);
@@ -212,10 +212,11 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   const uint32_t cg_src = (uint32_t)(tid % CG ^ (set == 0 ? k_swizzle<D>(lane / CG) : v_swizzle<D>(lane / CG))) * 16u;
   const uint32_t idx_max = (uint32_t)max(dm.T_max - 1, 0);
   uint32_t src[NI];     // rows of the tile to be requested next, as looked up (PAGED: the list's entries of the tile after it)
-  uint32_t off[NI];     // the same as byte offsets, of the tile being requested (PAGED: in 16 elements)
+  uint32_t off[NI];     // the same as byte offsets, of the tile being requested (PAGED: in 16 bytes)
   using Row = std::conditional_t<FP8, u32x2, u32x4>;   // eight elements
   Row R[DMA ? 1 : NLD];   // the tile in flight (not DMA)
-  // PAGED: positions and pages of the tile to be requested next; FP8: exponents of the rows of the tile in flight, and of the one before
+  // PAGED: positions and pages of the tile to be requested next; FP8: exponents of the rows of the tile in flight, and powers of two of the
+  // one before
   uint32_t pos[PAGED ? NI : 1], page[PAGED ? NI : 1], ex[FP8 ? NI : 1], ex_old[FP8 ? NI : 1];
   const int n_before = PAGED ? paged_len(dm, a, b) : 0;   // cached tokens, all of them
   const int32_t* table = nullptr;
@@ -227,8 +228,8 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
     constexpr int es = FP8 ? 1 : 2;
     pool = reinterpret_cast<uint64_t>(set == 0 ? a.pg.k : a.pg.v) + (uint64_t)kv * a.pg.st[1] * es;
     scales = (set == 0 ? a.pg.k_scale : a.pg.v_scale) + ((size_t)kv << a.pg.shift);
-    page_units = (uint32_t)(a.pg.st[0] / 16);
-    slot_units = (uint32_t)(a.pg.st[2] / 16);
+    page_units = (uint32_t)(a.pg.st[0] / (16 / es));
+    slot_units = (uint32_t)(a.pg.st[2] / (16 / es));
     page_scales = (uint32_t)a.pg.n_kv << a.pg.shift;
   }
   const char* req_base = nullptr;   // of the tile being requested
@@ -240,7 +241,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   auto request = [&](int t, int k) __attribute__((always_inline)) {   // chunk k of tile t
     if constexpr (PAGED) {
       const uint32_t o = kShare ? row16_lane(off[0], k) : off[k % NI];
-      const uint64_t at = pool_mine + ((uint64_t)o << (FP8 ? 4 : 5));
+      const uint64_t at = pool_mine + ((uint64_t)o << 4);
       if constexpr (DMA) {
         dma16(reinterpret_cast<const void*>(at), dst_mine + (uint32_t)stage_of(t) + 4u * k * group_mine);
       } else {
@@ -328,20 +329,24 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   };
   // PAGED: an entry of the list is fetched a step ahead of its page, and the page a step ahead of the rows.
   auto look_up_entries = [&](int t) __attribute__((always_inline)) {
-    t = min(t, t_end - 1);
     if (!sparse) return;
+    const int base = max(min(t, t_end - 1), 0) * KT;
 #pragma unroll
     for (int i = 0; i < NI; ++i)
-      src[i] = *reinterpret_cast<const uint32_t*>(kidx + (uint32_t)min(max(t, 0) * KT + r0 + RPI * (kShare ? lane % NLD : i), list_last) * 4u);
+      src[i] = *reinterpret_cast<const uint32_t*>(kidx + (uint32_t)min(base + r0 + RPI * (kShare ? lane % NLD : i), list_last) * 4u);
   };
   auto look_up_pages = [&](int t) __attribute__((always_inline)) {
     if constexpr (PAGED) {
       t = min(t, t_end - 1);
+      const bool cache = is_cache(t);
+      const int past = __builtin_amdgcn_readfirstlane(t);   // (or `cache` and the maximum become one subtraction with a carry, in vector registers)
+      const int base = (cache ? t : max(past - (n_ct - 1), 0)) * KT, last = (cache ? n_cache : C) - 1, first_pos = cache ? 0 : n_before;
+      const char* entries = reinterpret_cast<const char*>(table);
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const uint32_t row = row_of(t, i);
-        pos[i] = !is_cache(t) ? (uint32_t)n_before + row : sparse ? min(src[i], idx_max) : row;
-        page[i] = (uint32_t)table[min((int)(pos[i] >> a.pg.shift), a.pg.max_pages - 1)];
+        const int row = min(base + r0 + RPI * (kShare ? lane % NLD : i), last) + first_pos;   // tail slots repeat a real row
+        pos[i] = cache && sparse ? min(src[i], idx_max) : (uint32_t)row;
+        page[i] = *reinterpret_cast<const uint32_t*>(entries + min(pos[i] >> a.pg.shift, (uint32_t)(a.pg.max_pages - 1)) * 4u);
       }
     }
   };
@@ -374,7 +379,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
         const uint32_t pg = min(page[i], (uint32_t)(a.pg.n_pages - 1)), slot = pos[i] & ((1u << a.pg.shift) - 1u);
         off[i] = pg * page_units + slot * slot_units;
         if constexpr (FP8) {
-          ex_old[i] = ex[i];
+          ex_old[i] = ex[i] << 23;
           ex[i] = scales[pg * page_scales + slot];
         }
       }
@@ -395,7 +400,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   };
   auto store = [&](int t, int k, Row row) __attribute__((always_inline)) {   // (not DMA)
     u32x4 r;
-    if constexpr (FP8) r = widen_bf16(row, row_scale(kShare ? row16_lane(ex_old[0], k) : ex_old[k % NI]));
+    if constexpr (FP8) r = widen_bf16(row, __uint_as_float(kShare ? row16_lane(ex_old[0], k) : ex_old[k % NI]));
     else r = row;
     *(u32x4 __attribute__((address_space(3)))*)(uintptr_t)(dst_mine + lane * 16u + (uint32_t)stage_of(t) + 4u * k * group_mine) = r;
   };
@@ -432,7 +437,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
       for (int k = 0; k < NLD; ++k) request(t_begin + 1, k);
     } else if constexpr (FP8) {   // (no second tile whose exponents would have taken the first one's place)
 #pragma unroll
-      for (int i = 0; i < NI; ++i) ex_old[i] = ex[i];
+      for (int i = 0; i < NI; ++i) ex_old[i] = ex[i] << 23;
     }
     if constexpr (!DMA) {
 #pragma unroll
@@ -526,7 +531,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
     const bf16x2 pp = {(__bf16)sc[2 * e], (__bf16)sc[2 * e + 1]};
     p[e / 4][2 * (e % 4)] = pp[0];
     p[e / 4][2 * (e % 4) + 1] = pp[1];
-    if constexpr (PAGED) return psum + (sc[2 * e] + sc[2 * e + 1]);
+    if constexpr (PAGED) return psum;   // (half_pv adds them up)
     return __builtin_amdgcn_fdot2_f32_bf16(pp, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, psum, false);
   };
 
@@ -562,9 +567,11 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   };
   // Second half of a unit: O^T += V^T P^T; meanwhile the maximum of the next unit's scores, which it returns, and the K operands
   // of the unit after that.
-  auto half_pv = [&](auto next, const f32x16& sn, int u, auto between) __attribute__((always_inline)) {
+  // PAGED: and the sum of its own probabilities `sc`, where the vector unit has time for it.
+  auto half_pv = [&](auto next, const f32x16& sn, const f32x16& sc, int u, auto between) __attribute__((always_inline)) {
     constexpr int E = 16 / KS;
     float mx = -INFINITY;
+    float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < KS; ++i) {
       const s16x8 both = __builtin_shufflevector(vop[i][0], vop[i][1], 0, 1, 2, 3, 4, 5, 6, 7);
@@ -576,9 +583,15 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
         for (int e = E * i; e < E * i + E; ++e) mx = fmaxf(mx, sn[e]);
         asm volatile("" : "+v"(mx));   // (or all of it ends up behind the last product)
       }
+      if constexpr (PAGED) {
+#pragma unroll
+        for (int e = E * i; e < E * i + E; e += 2) sum += sc[e] + sc[e + 1];
+        asm volatile("" : "+v"(sum));
+      }
       between(KS + i);
       __builtin_amdgcn_sched_barrier(0);
     }
+    if constexpr (PAGED) l_run += sum;
     return mx;
   };
   // Keys of unit u of tile t that a row does not see (wave-uniform branch).
@@ -647,6 +660,11 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
       for (int i = 0; i < NI; ++i) asm volatile("" : "+v"(src[i]));
     }
     address(DMA ? j + 2 - set : j + 3 - set);
+    if constexpr (!PAGED) look_up(DMA ? j + 3 - set : j + 4 - set);
+  };
+  // (PAGED: the look-up is some twenty instructions, so in the loop it goes between products)
+  auto look_up_next = [&](int j, auto can_be_first) __attribute__((always_inline)) {
+    if (!PAGED || (DMA && decltype(can_be_first)::value && j < t_begin)) return;
     look_up(DMA ? j + 3 - set : j + 4 - set);
   };
   auto stage_all = [&](int j, auto can_be_first) __attribute__((always_inline)) {
@@ -658,16 +676,19 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   int j = t_begin < t_end ? t_begin - 1 : t_end;
   for (; j < min(w0 - 1, t_end); ++j) {
     begin_step(j, yes{});
+    look_up_next(j, yes{});
     stage_all(j, yes{});
   }
   if (w0 < w1) {
     // The staging of a step, a load at a time: between the products of the first unit's second half, or, where there are as many
     // chunks as products in it (blocks of four row blocks, d 128), of both its halves.
     auto staging = [&](int i) __attribute__((always_inline)) {
+      if (i == 1) look_up_next(j, no{});
       constexpr int first = NLD == KS ? 0 : KS, every = (2 * KS - first) / NLD;
       if (i >= first && (i - first) % every == 0) stage(j, (i - first) / every);
     };
     begin_step(j, yes{});
+    look_up_next(j, yes{});
     {   // S of the first unit, the operands of the second, the reference point
 #pragma unroll
       for (int i = 0; i < KS; ++i) read_k(0, i);
@@ -696,15 +717,16 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
       move_k(j);
       half_qk(yes{}, s[1], s[0], 0, staging);
       mask(s[1], j, 1);
-      float mx = half_pv(yes{}, s[1], 0, staging);
+      float mx = half_pv(yes{}, s[1], s[0], 0, staging);
       move_reference(s[1], mx);
       half_qk(yes{}, s[0], s[1], 1, nothing);
       move_v(j);
       mask(s[0], j + 1, 0);
-      mx = half_pv(yes{}, s[0], 1, nothing);
+      mx = half_pv(yes{}, s[0], s[1], 1, nothing);
       move_reference(s[0], mx);
     }
     begin_step(j, no{});
+    look_up_next(j, no{});
     stage_all(j, no{});
     if (both_units(j)) {
       half_qk(yes{}, s[1], s[0], 0, nothing);
@@ -712,7 +734,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
       float mx = -INFINITY;
 #pragma unroll
       for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[1][v]);
-      half_pv(no{}, s[1], 0, nothing);
+      half_pv(no{}, s[1], s[0], 0, nothing);
       move_reference(s[1], mx);
       if constexpr (!KSPLIT) {   // the second unit takes the first one's place
         s[0] = s[1];
@@ -721,11 +743,12 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
       }
     }
     half_qk(no{}, s[0], s[KSPLIT ? 1 : 0], KSPLIT ? 1 : 0, nothing);
-    half_pv(no{}, s[0], 0, nothing);
+    half_pv(no{}, s[0], s[KSPLIT ? 1 : 0], 0, nothing);
     ++j;
   }
   for (; j < t_end; ++j) {
     begin_step(j, no{});
+    look_up_next(j, no{});
     stage_all(j, no{});
   }
   if constexpr (DMA) wait_vmcnt<0>();   // nothing may land in LDS from here on

@@ -133,7 +133,7 @@ __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs
   const uint64_t v_pool = reinterpret_cast<uint64_t>(pg.v) + (uint64_t)kv * pg.st[1] * es + c * 16;
   const uint8_t* k_scales = pg.k_scale + ((size_t)kv << pg.shift);
   const uint8_t* v_scales = pg.v_scale + ((size_t)kv << pg.shift);
-  const uint32_t page_units = (uint32_t)(pg.st[0] / 16), slot_units = (uint32_t)(pg.st[2] / 16), page_scales = (uint32_t)pg.n_kv << pg.shift;
+  const uint32_t page_units = (uint32_t)(pg.st[0] / (16 / es)), slot_units = (uint32_t)(pg.st[2] / (16 / es)), page_scales = (uint32_t)pg.n_kv << pg.shift;
   const int my_slot = group * NLD + lane % NLD;   // the slot of a tile that this lane looks up
   auto slot_of_tile = [&](int tt) __attribute__((always_inline)) { return min(tt * kPdTile + my_slot, n_keys - 1); };   // (tail slots repeat a real one)
 
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs
     typedef const u32x4 __attribute__((address_space(1))) * global_row;
 #pragma unroll
     for (int i = 0; i < NLD; ++i) {
-      const uint64_t o = (uint64_t)group_lane<LPR>(off, i) << (FP8 ? 4 : 5);
+      const uint64_t o = (uint64_t)group_lane<LPR>(off, i) << 4;
       r.k[i] = *(global_row)(k_pool + o);
       r.v[i] = *(global_row)(v_pool + o);
     }
