@@ -87,7 +87,20 @@ __global__ __launch_bounds__(kFaThreads, 2) void attn_f32(Dims dm, attn_args<SRC
   const int split = blockIdx.y;
   const int kv = blockIdx.z % dm.n_kv, b = blockIdx.z / dm.n_kv;
   const int g = dm.g, n_rows = (PAGED ? chunk_of(dm, a, b) : dm.C) * g, row0 = rb * 32;
-  if (PAGED && row0 >= n_rows) return;   // block-uniform: a short chunk has no rows here
+  if constexpr (PAGED) {
+    if (split == 0 && n_rows < dm.C * g) {   // rows past the sequence's chunk: zeros, and no weight
+      for (int i = tid; i < 32 * (D / 4); i += kFaThreads) {
+        const int r = row0 + i / (D / 4);
+        if (r < n_rows || r >= dm.C * g) continue;
+        const FaRow fr = fa_row(r, g);
+        const int h = kv * g + fr.head;
+        *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + b * dm.os[0] + h * dm.os[1] + (size_t)fr.tok * dm.os[2] + 4 * (i % (D / 4))) =
+            f32x4{0.f, 0.f, 0.f, 0.f};
+        if (a.lse != nullptr && i % (D / 4) == 0) a.lse[(size_t)(b * dm.n_q + h) * dm.C + fr.tok] = -INFINITY;
+      }
+    }
+    if (row0 >= n_rows) return;   // block-uniform: a short chunk has no rows here
+  }
 
   const bool sparse = a.k_idx != nullptr;
   int n_cache = sparse ? min(a.n_cache[b * dm.n_kv + kv], dm.B_max) : min(a.n_cache[b * dm.ls], dm.T_max);

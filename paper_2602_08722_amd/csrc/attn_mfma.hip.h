@@ -79,6 +79,63 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, p);
 }
 
+// Shares of key lists in a launch over pages, whose sequences differ in length and in tokens: the fewest tiles a block with which the
+// sequences' groups of `per_block` row blocks fit the `slots` blocks of a KV head, so that blocks take about equally long whatever the
+// lengths (an equal number of shares for each, 4 KV heads of 3, d 64, 101 - 333 tokens over 1237 - 9999 keys: 60 us).  More than 64
+// sequences: an equal number each.  Every wave works it out for itself, lane i for sequence i; the merge does the same.
+struct ListShare {
+  int b, n_splits;          // b < 0: nothing to do
+  uint32_t block, record;   // the block's number among the sequence's; the sequence's first record of the KV head's
+};
+struct ListShares {   // of lane i's sequence
+  uint32_t n_splits, first_block, blocks, first_record;
+};
+__device__ __forceinline__ ListShares list_shares(const Dims& dm, const PagedAttnArgs& a, int kv) {
+  const int lane = threadIdx.x & 63;
+  uint32_t row_blocks = 0, groups = 0, tiles = 0;
+  if (lane < dm.b) {
+    const int C = chunk_of(dm, a, lane);
+    const int n = a.k_idx != nullptr ? min(max(a.n_cache[lane * dm.n_kv + kv], 0), dm.B_max) : paged_len(dm, a, lane);
+    row_blocks = (uint32_t)(dm.g * ((C + 31) / 32));
+    groups = (row_blocks + a.per_block - 1) / a.per_block;
+    tiles = C == 0 ? 0u : (uint32_t)((n + a.tile_keys - 1) / a.tile_keys + (C + a.tile_keys - 1) / a.tile_keys);
+  }
+  const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan_u32(groups), 63);
+  const float work = wave64_sum((float)groups * (float)tiles);
+  auto shares_of = [&](int steps) __attribute__((always_inline)) {   // (n_splits: the most that a list is shared by)
+    const uint32_t n = (uint32_t)((float)(tiles + steps - 1) / (float)steps);
+    return min(max(n, 1u), min((uint32_t)a.n_splits, max(tiles, 1u)));
+  };
+  // With `lo` tiles a block there may be too many blocks; with `hi` there are not (one more than the quotient for each group at most).
+  int lo = max((int)(work / (float)a.slots), 1), hi = (uint32_t)a.slots > all ? (int)(work / (float)(a.slots - (int)all)) + 2 : kMaxKv;
+  while (lo < hi) {   // (wave-uniform; three to five times)
+    const int mid = __builtin_amdgcn_readfirstlane(lo + (hi - lo) / 2);
+    if ((uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan_u32(groups * shares_of(mid)), 63) <= (uint32_t)a.slots) hi = mid;
+    else lo = mid + 1;
+  }
+  const uint32_t n = shares_of(hi);
+  const uint32_t blocks = groups * n, records = row_blocks * n;
+  return {n, wave_incl_scan_u32(blocks) - blocks, blocks, wave_incl_scan_u32(records) - records};
+}
+// The share of block `slot` (b < 0: of the block itself, else of sequence b's block 0).
+__device__ __forceinline__ ListShare list_share(const Dims& dm, const PagedAttnArgs& a, int kv, int slot, int b) {
+  if (dm.b > kWave) {
+    const int each = a.slots / dm.b, groups = (dm.g * ((dm.C + 31) / 32) + a.per_block - 1) / a.per_block, n = each / groups;
+    if (b < 0) b = slot / each;
+    return {b < dm.b && slot % each < groups * n ? b : -1, n, (uint32_t)(slot % each), (uint32_t)(b * dm.g * ((dm.C + 31) / 32) * n)};
+  }
+  const ListShares s = list_shares(dm, a, kv);
+  if (b < 0) {
+    const unsigned long long mine = __builtin_amdgcn_ballot_w64((uint32_t)slot >= s.first_block && (uint32_t)slot < s.first_block + s.blocks);
+    if (mine == 0) return {-1, 1, 0u, 0u};
+    b = (int)__builtin_ctzll(mine);
+  } else {
+    slot = __builtin_amdgcn_readlane((int)s.first_block, b);
+  }
+  return {b, __builtin_amdgcn_readlane((int)s.n_splits, b), (uint32_t)(slot - __builtin_amdgcn_readlane((int)s.first_block, b)),
+          (uint32_t)__builtin_amdgcn_readlane((int)s.first_record, b)};
+}
+
 template <int D>
 __device__ __forceinline__ int k_swizzle(int row) { return D == 128 ? row & 3 : (row >> 1) & 3; }
 template <int D>
@@ -148,7 +205,12 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   // otherwise a long sequence that happens to come last starts when most of the chip has already drained.
   // (The chunks of a prompt lie shortest first: no length to wait for.)
   int b = dm.prompt_chunks ? dm.b - 1 - (int)blockIdx.z : (int)blockIdx.z;
-  if (dm.b > 1 && dm.b <= kWave && !dm.prompt_chunks)
+  [[maybe_unused]] ListShare share = {};
+  if constexpr (PAGED && KSPLIT) {
+    share = list_share(dm, a, kv, blockIdx.y, -1);
+    if (share.b < 0) return;   // block-uniform
+    b = share.b;
+  } else if (dm.b > 1 && dm.b <= kWave && !dm.prompt_chunks)
     b = seq_of_rank(sparse ? a.n_cache + kv : a.n_cache, sparse ? dm.n_kv : dm.ls, dm.b, blockIdx.z);
   // The list's length and the arguments that the start needs, fetched together: one by one, where each is first used, they are four fetches
   // in a row.
@@ -172,8 +234,13 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   // row block.  Otherwise set 0 is front, set 1 back.
   const int slot = SPLIT ? (w + 2 * set) % 4 : w + 4 * set;
   const bool back = SPLIT ? slot >= 2 : set == 1;
-  const int yb = KSPLIT ? (int)((blockIdx.y * a.inv_splits) >> 16) : (int)blockIdx.y;   // group of row blocks
-  const int split = KSPLIT ? (int)blockIdx.y - yb * a.n_splits : 0;                               // share of its key list
+  const int n_splits = PAGED && KSPLIT ? share.n_splits : a.n_splits;
+  int yb = KSPLIT ? (int)((blockIdx.y * a.inv_splits) >> 16) : (int)blockIdx.y;   // group of row blocks
+  int split = KSPLIT ? (int)blockIdx.y - yb * a.n_splits : 0;                               // share of its key list
+  if constexpr (PAGED && KSPLIT) {
+    yb = (int)share.block / n_splits;
+    split = (int)share.block - yb * n_splits;
+  }
   const int kf = yb * HW + slot % HW;
   // Row blocks of a block.  Paired (a launch of one round): half from the front of the list, half from the back, so all
   // blocks take equally long.  Adjacent (a launch of several rounds): 2*HW neighbours with nearly the same causal range,
@@ -187,6 +254,14 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   const int tok0 = xt * 32;
   const int h = kv * g + xj;
   const int xb_hi = nrb - 1 - yb * HW;                                     // the block's last row block
+  if constexpr (PAGED && !KSPLIT) {   // rows past the sequence's chunk: zeros and no weight, shared by its blocks (KSPLIT: by the merge)
+    for (int u = (int)blockIdx.y * 2 * kSetThreads + (int)threadIdx.x; u < (dm.C - C) * g * CG; u += (int)gridDim.y * 2 * kSetThreads) {
+      const int r = u / CG, t = C + r / g, hh = kv * g + r % g;
+      *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.out) + b * dm.os[0] + hh * dm.os[1] + (size_t)t * dm.os[2] + u % CG * 8) =
+          u32x4{0u, 0u, 0u, 0u};
+      if (a.lse != nullptr && u % CG == 0) a.lse[(size_t)(b * dm.n_q + hh) * dm.C + t] = -INFINITY;
+    }
+  }
   const int x_hi = adjacent ? nrb - 1 - yb * 2 * HW
                             : (xb_hi >= half ? xb_hi : min(yb * HW + HW - 1, half - 1));
   if (adjacent ? x_hi < 0 : yb * HW >= half) return;   // a short chunk has no row blocks here (block-uniform)
@@ -300,8 +375,8 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   const int n_ct = (n_cache + KT - 1) / KT;
   const int n_tiles = n_cht + n_ct;
   // Tiles are numbered from -1, so that the cache tiles are 0 .. n_ct - 1.
-  const int t_begin = (KSPLIT ? (int)((uint32_t)n_tiles * (uint32_t)split / (uint32_t)a.n_splits) : 0) - 1;
-  const int t_end = (KSPLIT ? (int)((uint32_t)n_tiles * (uint32_t)(split + 1) / (uint32_t)a.n_splits) : n_tiles) - 1;
+  const int t_begin = (KSPLIT ? (int)((uint32_t)n_tiles * (uint32_t)split / (uint32_t)n_splits) : 0) - 1;
+  const int t_end = (KSPLIT ? (int)((uint32_t)n_tiles * (uint32_t)(split + 1) / (uint32_t)n_splits) : n_tiles) - 1;
   auto is_cache = [&](int t) __attribute__((always_inline)) { return (uint32_t)t < (uint32_t)n_ct; };
   // first key (cache slot or chunk position) of tile t
   auto tile_base = [&](int t) __attribute__((always_inline)) { return (is_cache(t) ? t : max(t - (n_ct - 1), 0)) * KT; };
@@ -793,7 +868,9 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   const float l_tot = l_run + other_half(l_run);
   if constexpr (KSPLIT) {   // the partial goes out as the registers lie, 1 KiB per store
     if (!wave_on) return;
-    float* rec = a.part + (((size_t)(b * dm.n_kv + kv) * (g * ((dm.C + 31) / 32)) + x) * a.n_splits + split) * Cfg::kRecFloats;
+    float* rec;
+    if constexpr (PAGED) rec = a.part + ((size_t)kv * a.records + share.record + (size_t)x * n_splits + split) * Cfg::kRecFloats;
+    else rec = a.part + (((size_t)(b * dm.n_kv + kv) * (g * ((dm.C + 31) / 32)) + x) * a.n_splits + split) * Cfg::kRecFloats;
 #pragma unroll
     for (int c = 0; c < DB; ++c)
 #pragma unroll
@@ -877,9 +954,26 @@ __global__ __launch_bounds__(64 * kMergeWaves) void attn_bf16_merge(Dims dm, att
   int C;
   if constexpr (SRC == kContiguous) C = dm.chunk(b);
   else C = chunk_of(dm, a, b);
-  if (x >= dm.g * ((C + 31) / 32)) return;   // block-uniform
-  const float* rec = a.part + ((size_t)blockIdx.y * gridDim.x + x) * a.n_splits * REC;
-  const int s0 = a.n_splits * w / nw, s1 = a.n_splits * (w + 1) / nw;
+  int n_splits = a.n_splits;
+  const float* rec;
+  if constexpr (SRC == kContiguous) {
+    if (x >= dm.g * ((C + 31) / 32)) return;   // block-uniform
+    rec = a.part + ((size_t)blockIdx.y * gridDim.x + x) * a.n_splits * REC;
+  } else {
+    const int tok = x / dm.g * 32 + li;
+    if (w == 0 && tok >= C && tok < dm.C) {   // rows past the sequence's chunk
+      const int h = kv * dm.g + x % dm.g;
+      uint16_t* orow = static_cast<uint16_t*>(a.out) + b * dm.os[0] + h * dm.os[1] + (size_t)tok * dm.os[2];
+#pragma unroll
+      for (int v4 = 0; v4 < 4; ++v4) *reinterpret_cast<uint2*>(orow + 32 * c + 8 * v4 + 4 * hf) = make_uint2(0u, 0u);
+      if (a.lse != nullptr && hf == 0 && c == 0) a.lse[(size_t)(b * dm.n_q + h) * dm.C + tok] = -INFINITY;
+    }
+    if (x >= dm.g * ((C + 31) / 32)) return;   // block-uniform
+    const ListShare share = list_share(dm, a, kv, 0, b);
+    n_splits = share.n_splits;
+    rec = a.part + ((size_t)kv * a.records + share.record + (size_t)x * n_splits) * REC;
+  }
+  const int s0 = n_splits * w / nw, s1 = n_splits * (w + 1) / nw;
   float m = -INFINITY, l = 0.f;
   float o[16];
 #pragma unroll
@@ -968,6 +1062,12 @@ __global__ __launch_bounds__(64 * kMergeWaves) void attn_bf16_merge(Dims dm, att
     a.lse[(size_t)(b * dm.n_q + h) * dm.C + tok] = (m + log2f(l)) * 0.6931471805599453f;
 }
 
+inline int key_splits_limit(const Dims& dm, bool sparse, int keys_per_tile) {
+  const long long tiles = ((long long)attended_cap(dm, sparse) + keys_per_tile - 1) / keys_per_tile +
+                          (dm.C + keys_per_tile - 1) / keys_per_tile;
+  return (int)(tiles < kMaxKeySplits ? tiles : kMaxKeySplits);
+}
+
 template <int D, bool SPLIT, bool XS, bool KSPLIT, bool WHOLE, int SRC = kContiguous>
 static hipError_t launch_variant(const Dims& dm, const attn_args<SRC>& a, hipStream_t st) {
   using Cfg = AttnCfg<D, SPLIT, SRC>;
@@ -980,15 +1080,35 @@ static hipError_t launch_variant(const Dims& dm, const attn_args<SRC>& a, hipStr
   const int half = (nrb + 1) / 2;
   dim3 grid(dm.n_kv, (half + Cfg::HW - 1) / Cfg::HW * a.n_splits, dm.b);
   attn_args<SRC> aa = a;
+  int most_splits = a.n_splits;   // of any list
+  if constexpr (SRC != kContiguous && KSPLIT) {
+    // The plan's blocks, shared out by the kernels.  Their records: at most min(per_block, nrb) of a block, and nrb of a sequence and share.
+    // The first bound is kept within kMaxRecords: a plan has heads * nrb * splits of them within it, two splits at least, and groups of
+    // row blocks, filled up, are less than twice nrb, so that every group keeps a block.
+    aa.per_block = 2 * Cfg::HW;
+    aa.tile_keys = Cfg::KT;
+    const int of_block = aa.per_block < nrb ? aa.per_block : nrb;
+    // (a plan of one round leaves out what would be less than one more share for every group: unequal lists can use it)
+    const long long planned = (long long)grid.y * dm.b, one_more = planned + planned / a.n_splits - 1, round = kComputeUnits / dm.n_kv,
+                    room = kMaxRecords / (dm.n_kv * of_block);
+    const long long slots = dm.b == 1 || dm.b > kWave || planned >= round ? planned : one_more < round ? one_more : round;
+    aa.slots = (int)(slots < room ? slots : room);
+    if (dm.b <= kWave) most_splits = key_splits_limit(dm, a.k_idx != nullptr, Cfg::KT);
+    aa.n_splits = most_splits;
+    const long long of_lists = (long long)dm.b * nrb * most_splits;
+    aa.records = (int)((long long)aa.slots * of_block < of_lists ? (long long)aa.slots * of_block : of_lists);
+    grid = dim3(dm.n_kv, aa.slots, 1);
+  }
   aa.inv_g = quotient_factor(dm.g);
-  aa.inv_splits = quotient_factor(a.n_splits);
+  aa.inv_splits = quotient_factor(aa.n_splits);
   // one block is resident per compute unit: from two rounds on, neighbouring row blocks and longest ranges first
   // (measured at 512 blocks, 4096-token chunk over 131072 cached tokens: 3.5 % faster than pairing; a launch of one
   // round needs the pairing, or its last block sets the time alone)
   aa.adjacent = (long long)grid.x * grid.y * grid.z >= 2 * kComputeUnits ? 1 : 0;
   hipLaunchKernelGGL((attn_bf16<D, SPLIT, XS, KSPLIT, WHOLE, SRC>), grid, dim3(2 * kSetThreads), lds, st, dm, aa);
   if (KSPLIT) {
-    const int runs = (a.n_splits + kMergeRun - 1) / kMergeRun, waves = runs < kMergeWaves ? runs : kMergeWaves;
+    const int usual = 2 * a.n_splits < most_splits ? 2 * a.n_splits : most_splits;   // (longer lists take a wave's loop another time)
+    const int runs = (usual + kMergeRun - 1) / kMergeRun, waves = runs < kMergeWaves ? runs : kMergeWaves;
     const int dims = waves * (D / 32) <= kMergeWaves ? D / 32 : 1;
     hipLaunchKernelGGL((attn_bf16_merge<D, SRC>), dim3(nrb, dm.b * dm.n_kv, D / 32 / dims), dim3(64 * waves * dims), 0, st, dm, aa, dims);
   }
@@ -996,12 +1116,6 @@ static hipError_t launch_variant(const Dims& dm, const attn_args<SRC>& a, hipStr
 }
 
 // ---- which variant: 8 row blocks per block or 4 (SPLIT), and over how many blocks the key list is split -----------
-
-inline int key_splits_limit(const Dims& dm, bool sparse, int keys_per_tile) {
-  const long long tiles = ((long long)attended_cap(dm, sparse) + keys_per_tile - 1) / keys_per_tile +
-                          (dm.C + keys_per_tile - 1) / keys_per_tile;
-  return (int)(tiles < kMaxKeySplits ? tiles : kMaxKeySplits);
-}
 
 // Whole key lists of more than 1024 row blocks: eight row blocks per block, or four.
 // A batch: eight where that gives every compute unit a block.  (The lengths may differ, which the host cannot know, and then

@@ -1,5 +1,5 @@
-// Attention of a chunk over a cache in pages: which kernel takes the call, and the rows that a ragged batch does not have.  Float32 attention
-// over pages: the kernel of attn_f32.hip.h, and one for short lists.
+// Attention of a chunk over a cache in pages: which kernel takes the call.  Float32 attention over pages: the kernel of attn_f32.hip.h, and
+// one for short lists.
 #include "attn_f32.hip.h"
 
 namespace quoka {
@@ -23,7 +23,15 @@ __global__ __launch_bounds__(kPsThreads) void paged_f32_short(Dims dm, PagedArgs
     for (int e = 0; e < EPL; ++e) qs[w][lane + 64 * e] = q[lane + 64 * e];
   }
   __syncthreads();
-  if (!row_on) return;   // wave-uniform; no barrier follows
+  if (!row_on) {   // wave-uniform; no barrier follows
+    if (i < dm.C) {   // a row past the sequence's chunk
+      float* out = static_cast<float*>(a.out) + b * dm.os[0] + h * dm.os[1] + i * dm.os[2];
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) out[lane + 64 * e] = 0.f;
+      if (a.lse != nullptr && lane == 0) a.lse[(long long)(b * dm.n_q + h) * dm.C + i] = -INFINITY;
+    }
+    return;
+  }
   const int kv = h / dm.g;
   const int n_before = min(max(a.kv_lens[b], 0), dm.T_max);
   const int n_list = a.k_idx == nullptr ? n_before : min(max(a.k_cnt[b * dm.n_kv + kv], 0), dm.B_max);
@@ -82,20 +90,6 @@ __global__ __launch_bounds__(kPsThreads) void paged_f32_short(Dims dm, PagedArgs
   if (a.lse != nullptr && lane == 0) a.lse[(long long)(b * dm.n_q + h) * dm.C + i] = m_run + logf(l_run);
 }
 
-// Rows past a sequence's chunk: zeros, and no weight at all.  (A launch of its own, and only where lengths are given, since the attention
-// kernels' grids follow the chunk's row blocks and such rows may be most of a ragged batch.)
-constexpr int kFillRows = 32;
-__global__ __launch_bounds__(256) void paged_fill(Dims dm, PagedArgs a, int row_units) {   // row_units: 16-byte units of a row
-  const int h = blockIdx.y, b = blockIdx.z, C = max(min(a.chunk_lens[b], dm.C), 0);
-  const int i0 = max((int)blockIdx.x * kFillRows, C), i1 = min((int)(blockIdx.x + 1) * kFillRows, dm.C);
-  const long long es = dm.d * 2 == row_units * 16 ? 2 : 4;
-  char* out = static_cast<char*>(a.out) + (b * dm.os[0] + h * dm.os[1]) * es;
-  for (int u = threadIdx.x; u < (i1 - i0) * row_units; u += 256)
-    *reinterpret_cast<u32x4*>(out + (i0 + u / row_units) * dm.os[2] * es + (u % row_units) * 16) = u32x4{0u, 0u, 0u, 0u};
-  if (a.lse != nullptr)
-    for (int i = i0 + threadIdx.x; i < i1; i += 256) a.lse[(long long)(b * dm.n_q + h) * dm.C + i] = -INFINITY;
-}
-
 template <bool FP8, int D>
 static hipError_t launch_paged_f32(const Dims& dm, const PagedArgs& a, float* part, hipStream_t st) {
   if (attn_f32_is_short(dm, a.k_idx != nullptr)) {
@@ -112,12 +106,6 @@ size_t paged_attn_ws_floats(const Dims& dm, int dtype) {
 }
 
 hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float* part, hipStream_t st) {
-  if (a.chunk_lens != nullptr) {
-    hipLaunchKernelGGL(paged_fill, dim3((dm.C + kFillRows - 1) / kFillRows, dm.n_q, dm.b), dim3(256), 0, st, dm, a,
-                       dm.d * (dtype == QUOKA_BF16 ? 2 : 4) / 16);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
   if (dtype == QUOKA_BF16)
     return attn_decode_applies(dm) ? launch_paged_decode(dm, fp8, a, part, st) : launch_paged_attn_bf16(dm, fp8, a, part, st);
   if (dm.d == 64) return fp8 ? launch_paged_f32<true, 64>(dm, a, part, st) : launch_paged_f32<false, 64>(dm, a, part, st);

@@ -345,8 +345,14 @@ __global__ __launch_bounds__(kPdThreads) void paged_decode_merge(Dims dm, PagedA
   __shared__ float4 red[NG][TPR];
   __shared__ float wm[kPdWaves], wl[kPdWaves];
   const int r = blockIdx.x, kv = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
-  const int C = a.chunk_lens == nullptr ? dm.C : min(a.chunk_lens[b], dm.C);
-  if (r >= C * dm.g) return;   // block-uniform
+  const int C = a.chunk_lens == nullptr ? dm.C : max(min(a.chunk_lens[b], dm.C), 0);
+  if (r >= C * dm.g) {   // block-uniform: a row past the sequence's chunk
+    const int tok = r / dm.g, h = kv * dm.g + r % dm.g;
+    uint16_t* orow = static_cast<uint16_t*>(a.out) + b * dm.os[0] + h * dm.os[1] + (size_t)tok * dm.os[2];
+    if (tid < TPR) *reinterpret_cast<u32x2*>(orow + 4 * tid) = u32x2{0u, 0u};
+    if (tid == 0 && a.lse != nullptr) a.lse[(size_t)(b * dm.n_q + h) * dm.C + tok] = -INFINITY;
+    return;
+  }
   const PdWork share = pd_share(dm, a, b, kv, n_slots);
   const int n = share.n_splits;
   const float* base = part + ((size_t)kv * n_slots + share.first) * REC;
