@@ -223,7 +223,8 @@ quoka_status quoka_prefill_attn(const quoka_shape* shape, int sparse, const void
  * pool past a length are never used, whatever they hold (NaN included).  Entries that are used must be in [0, n_pages); others
  * are harmless: a write drops the row, everything else takes some row of the pool in its place.  The same goes for positions
  * from max_pages * page_len on.  Sequences may share pages that are only read.
- * Limits: the rows of one head span at most 64 GiB of a pool (K and V have one each), n_pages * n_KV * page_len <= 2^32.              */
+ * Limits: the rows of one head span at most 64 GiB of a pool (K and V have one each), n_pages * n_KV * page_len <= 2^32;
+ * attention takes batch * (max_kv_len + chunk_len + 32) < 2^36.                                                                       */
 typedef enum { QUOKA_PAGES_RAW = 0, QUOKA_PAGES_FP8 = 1 } quoka_page_format;
 
 typedef struct quoka_pages {

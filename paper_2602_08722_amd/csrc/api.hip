@@ -668,6 +668,8 @@ quoka_status quoka_paged_attn(const quoka_shape* shape, const quoka_pages* pages
   if (st != QUOKA_OK) return st;
   if (q == nullptr || out == nullptr || kv_lens == nullptr || !aligned16(q) || !aligned16(out)) return QUOKA_EINVAL;
   if (k_idx != nullptr && k_cnt == nullptr) return QUOKA_EINVAL;
+  // (kernels number the keys of all sequences together, in tiles of 32, with 32 bits)
+  if ((long long)dm.b * ((long long)dm.T_max + dm.C + 32) >= 1ll << 36) return QUOKA_EUNSUPPORTED;
   if (workspace == nullptr) return QUOKA_EINVAL;
   size_t need = 0;
   st = quoka_paged_workspace_bytes(shape, &need);

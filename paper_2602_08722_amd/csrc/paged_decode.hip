@@ -7,8 +7,11 @@
 //
 // Bound by memory: every row of K and V is used once, by one wave, which works by itself on 32 slots at a time.  A load takes 16
 // bytes a lane and whole rows by LPR neighbouring lanes (16, 8 or 4 of them); such a group fetches NLD neighbouring slots, one a load, so
-// each of its lanes looks up one slot's row and hands it to the others by a cross-lane move.  Entries are fetched three tiles ahead,
-// pages two, rows one; 8-bit rows are widened on their way to LDS.
+// each of its lanes looks up one slot's row and hands it to the others by a cross-lane move.  Rows are fetched one tile ahead, pages two,
+// entries three; 8-bit rows are widened on their way to LDS.
+//
+// The tiles of all sequences lie one behind the other, and every block of a KV head takes as many of them: the end of one
+// sequence, whole ones, the beginning of another.  A part of a sequence leaves a partial.
 #include <type_traits>
 
 #include "pages.hip.h"
@@ -22,8 +25,7 @@ typedef s16x4 __attribute__((address_space(3))) * tr_ptr;
 constexpr int kPdWaves = 4;
 constexpr int kPdThreads = 64 * kPdWaves;
 constexpr int kPdTile = 32;        // list slots a wave handles at a time
-constexpr int kPdMaxSplits = 256;  // blocks per (sequence, KV head)
-static_assert(((long long)kMaxKv / kPdTile + 2) * kPdMaxSplits <= 1ll << 32, "tiles times shares in 32 bits");
+constexpr int kPdMaxSlots = 512;   // blocks per KV head: two for every compute unit, which are resident together
 
 template <int D, bool FP8>
 struct PdCfg {
@@ -32,6 +34,15 @@ struct PdCfg {
   static constexpr int NLD = kPdTile * LPR / 64;       // rows of a group of lanes
   static constexpr int LD = D + 8;         // K rows in LDS: 16 bytes of padding (conflict-free 16-byte reads)
   static constexpr int LDV = D + 32;       // V rows: 64 bytes apart modulo 256 (transposing reads)
+  // The first row of a group of lanes.  8-bit rows: 16 lanes store 16 bytes of LDS at a time, of two rows (D = 64: four), so neighbouring
+  // groups have rows that are 128 (64) bytes apart modulo 256; a lane's two pieces of K lie half a row apart (the contraction index may
+  // be permuted: Q follows), and of V side by side, the other way round in every other group of eight (D = 64: four) rows.
+  __device__ static __forceinline__ int first_row(int group) {
+    if constexpr (!FP8) return group * NLD;
+    if constexpr (D == 128) return 8 * (group & 3) + 4 * (group >> 2);
+    return 4 * (group & 7) + 2 * (group >> 3);
+  }
+  static constexpr int kTurn = D == 128 ? 8 : 4;
   static constexpr size_t kKBytes = (size_t)kPdTile * LD * 2;
   static constexpr size_t kWaveBytes = kKBytes + (size_t)kPdTile * LDV * 2;
   static constexpr int kRec = 32 * (D + 2);   // floats of a block's partial: O[32][D], m[32], l[32]
@@ -66,45 +77,47 @@ __device__ __forceinline__ PdSeq pd_seq(const Dims& dm, const PagedArgs& a, int 
   return s;
 }
 
-// The blocks of one KV head, `n_slots` of them, over the sequences: 1 + floor(share * (n_slots - batch)) for each, share its part of all
-// tiles, and never more than there are tiles for the four waves of each (more than 64 sequences: an equal number each).  Every wave works it out for itself.
-struct PdWork {
-  int b, split, n_splits, first;   // b < 0: nothing to do; first: the sequence's first slot
+// Tiles of sequence `b` (none where it has no token in this chunk).
+__device__ __forceinline__ uint32_t pd_tiles(const Dims& dm, const PagedArgs& a, int b, int kv) {
+  const PdSeq s = pd_seq(dm, a, b, kv);
+  return s.C > 0 ? (uint32_t)(s.n_list + s.C + kPdTile - 1) / kPdTile : 0u;
+}
+// A sequence's place in the KV head's line of tiles.  Every wave works these out for itself, 64 sequences at a time.
+struct PdPlace {
+  int b;
+  uint32_t first, tiles;
 };
-__device__ __forceinline__ uint32_t pd_lane_splits(const Dims& dm, const PagedArgs& a, int kv, int n_slots, uint32_t* before) {
-  const int lane = threadIdx.x & 63;
-  uint32_t tiles = 0;
-  if (lane < dm.b) {
-    const PdSeq s = pd_seq(dm, a, lane, kv);
-    tiles = s.C > 0 ? (uint32_t)(s.n_list + s.C + kPdTile - 1) / kPdTile : 0u;
+__device__ __forceinline__ uint32_t pd_total(const Dims& dm, const PagedArgs& a, int kv) {
+  uint32_t total = 0;
+  for (int b0 = 0; b0 < dm.b; b0 += kWave) {
+    const int b = b0 + (threadIdx.x & 63);
+    total += (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan_u32(b < dm.b ? pd_tiles(dm, a, b, kv) : 0u), 63);
   }
-  const uint32_t total = max((uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan_u32(tiles), 63), 1u);
-  uint32_t n = 1u + (uint32_t)((unsigned long long)tiles * (uint32_t)(n_slots - dm.b) / total);
-  n = min(min(n, max((tiles + kPdWaves - 1) / kPdWaves, 1u)), (uint32_t)kPdMaxSplits);
-  if (lane >= dm.b) n = 0;
-  *before = wave_incl_scan_u32(n) - n;
-  return n;
+  return total;
 }
-__device__ __forceinline__ PdWork pd_work(const Dims& dm, const PagedArgs& a, int slot, int kv, int n_slots) {
-  if (dm.b > 64) {
-    const int n = n_slots / dm.b;
-    return {slot < n * dm.b ? slot / n : -1, slot % n, n, slot / n * n};
+// The sequence that tile `at` of the line belongs to (seq < 0), or sequence `seq`.
+__device__ __forceinline__ PdPlace pd_place(const Dims& dm, const PagedArgs& a, int kv, uint32_t at, int seq) {
+  uint32_t before = 0;
+  for (int b0 = 0; b0 < dm.b; b0 += kWave) {
+    const int b = b0 + (threadIdx.x & 63);
+    const uint32_t tiles = b < dm.b ? pd_tiles(dm, a, b, kv) : 0u, end = before + wave_incl_scan_u32(tiles);
+    const unsigned long long hit = __builtin_amdgcn_ballot_w64(seq < 0 ? at >= end - tiles && at < end : b == seq);
+    if (hit != 0) {
+      const int lane = (int)__builtin_ctzll(hit);
+      const uint32_t n = (uint32_t)__builtin_amdgcn_readlane((int)tiles, lane);
+      return {b0 + lane, (uint32_t)__builtin_amdgcn_readlane((int)end, lane) - n, n};
+    }
+    before = (uint32_t)__builtin_amdgcn_readlane((int)end, 63);
   }
-  uint32_t before;
-  const uint32_t n = pd_lane_splits(dm, a, kv, n_slots, &before);
-  const unsigned long long mine = __builtin_amdgcn_ballot_w64((uint32_t)slot >= before && (uint32_t)slot < before + n);
-  if (mine == 0) return {-1, 0, 0, 0};
-  const int b = (int)__builtin_ctzll(mine), first = __builtin_amdgcn_readlane((int)before, b);
-  return {b, slot - first, __builtin_amdgcn_readlane((int)n, b), first};
+  return {-1, 0u, 0u};
 }
-__device__ __forceinline__ PdWork pd_share(const Dims& dm, const PagedArgs& a, int b, int kv, int n_slots) {
-  if (dm.b > 64) return {b, 0, n_slots / dm.b, b * (n_slots / dm.b)};
-  uint32_t before;
-  const uint32_t n = pd_lane_splits(dm, a, kv, n_slots, &before);
-  return {b, 0, __builtin_amdgcn_readlane((int)n, b), __builtin_amdgcn_readlane((int)before, b)};
+// Tiles of a block: all of them over the blocks, at least one for each wave.
+__device__ __forceinline__ uint32_t pd_quota(uint32_t total, int n_slots) {
+  return max((total + (uint32_t)n_slots - 1) / (uint32_t)n_slots, (uint32_t)kPdWaves);
 }
 
-// part: [n_kv, n_slots, kRec] float32
+// part: [n_kv, n_slots + batch, kRec] float32.  The partial of sequence b from block s is s + b: along the line of tiles either grows with every
+// part of a sequence.
 template <int D, bool FP8, bool LIST>
 __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs a, float* __restrict__ part, int n_slots) {
   using Cfg = PdCfg<D, FP8>;
@@ -115,233 +128,243 @@ __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 31, hf = lane >> 5;
-  const PdWork work = pd_work(dm, a, blockIdx.x, kv, n_slots);
-  if (work.b < 0) return;   // block-uniform
-  const int b = work.b, g = dm.g;
-  const PdSeq seq = pd_seq(dm, a, b, kv);
-  if (seq.C == 0) return;   // block-uniform; no row of it is merged
-  const int n_list = seq.n_list, n_keys = n_list + seq.C, n_rows = seq.C * g;   // n_rows <= 32, checked by the launcher
-  const uint32_t tiles = (uint32_t)(n_keys + kPdTile - 1) / kPdTile;
-  const int t_end = (int)(tiles * (uint32_t)(work.split + 1) / (uint32_t)work.n_splits);
-  int t = (int)(tiles * (uint32_t)work.split / (uint32_t)work.n_splits) + w;   // this wave's tiles: every fourth
+  const int g = dm.g;
+  const uint32_t total = pd_total(dm, a, kv), quota = pd_quota(total, n_slots);
+  uint32_t line = blockIdx.x * quota;   // (blocks x quota < total + a block's share: 32 bits)
+  const uint32_t line_end = min(line + quota, total);
+  while (line < line_end) {   // block-uniform: the sequences that the block has a part of
+    const PdPlace place = pd_place(dm, a, kv, line, -1);
+    const int b = place.b;
+    const PdSeq seq = pd_seq(dm, a, b, kv);
+    const int n_list = seq.n_list, n_keys = n_list + seq.C, n_rows = seq.C * g;   // n_rows <= 32, checked by the launcher
+    const int t_end = (int)(min(line_end, place.first + place.tiles) - place.first);
+    int t = (int)(line - place.first) + w;   // this wave's tiles: every fourth
+    line = place.first + t_end;
 
-  const int32_t* table = pg.table + (size_t)b * pg.max_pages;
-  const int32_t* list = LIST ? a.k_idx + (size_t)(b * dm.n_kv + kv) * dm.B_max : nullptr;
-  constexpr int es = FP8 ? 1 : 2;
-  const int c = lane % LPR, group = lane / LPR;   // 16 bytes of a row; the group's slots are group * NLD + 0 .. NLD - 1
-  const uint64_t k_pool = reinterpret_cast<uint64_t>(pg.k) + (uint64_t)kv * pg.st[1] * es + c * 16;
-  const uint64_t v_pool = reinterpret_cast<uint64_t>(pg.v) + (uint64_t)kv * pg.st[1] * es + c * 16;
-  const uint8_t* k_scales = pg.k_scale + ((size_t)kv << pg.shift);
-  const uint8_t* v_scales = pg.v_scale + ((size_t)kv << pg.shift);
-  const uint32_t page_units = (uint32_t)(pg.st[0] / (16 / es)), slot_units = (uint32_t)(pg.st[2] / (16 / es)), page_scales = (uint32_t)pg.n_kv << pg.shift;
-  const int my_slot = group * NLD + lane % NLD;   // the slot of a tile that this lane looks up
-  auto slot_of_tile = [&](int tt) __attribute__((always_inline)) { return min(tt * kPdTile + my_slot, n_keys - 1); };   // (tail slots repeat a real one)
+    const int32_t* table = pg.table + (size_t)b * pg.max_pages;
+    const int32_t* list = LIST ? a.k_idx + (size_t)(b * dm.n_kv + kv) * dm.B_max : nullptr;
+    constexpr int es = FP8 ? 1 : 2;
+    const int c = lane % LPR, group = lane / LPR;   // 16 bytes of a row
+    const uint64_t k_pool = reinterpret_cast<uint64_t>(pg.k) + (uint64_t)kv * pg.st[1] * es;
+    const uint64_t v_pool = reinterpret_cast<uint64_t>(pg.v) + (uint64_t)kv * pg.st[1] * es;
+    const uint8_t* k_scales = pg.k_scale + ((size_t)kv << pg.shift);
+    const uint8_t* v_scales = pg.v_scale + ((size_t)kv << pg.shift);
+    const uint32_t page_units = (uint32_t)(pg.st[0] / (16 / es)), slot_units = (uint32_t)(pg.st[2] / (16 / es)), page_scales = (uint32_t)pg.n_kv << pg.shift;
+    const int row0 = Cfg::first_row(group), my_slot = row0 + lane % NLD;   // the group's rows; the one that this lane looks up
+    auto slot_of_tile = [&](int tt) __attribute__((always_inline)) { return min(tt * kPdTile + my_slot, n_keys - 1); };   // (tail slots repeat a real one)
 
-  uint32_t entry = 0;          // of the tile after the one whose page is looked up
-  uint32_t pos = 0, page = 0;  // of the tile whose rows are fetched next
-  auto look_up_entry = [&](int tt) __attribute__((always_inline)) {
-    if constexpr (LIST) entry = (uint32_t)list[max(min(slot_of_tile(tt), n_list - 1), 0)];
-  };
-  auto look_up_page = [&](int tt) __attribute__((always_inline)) {
-    const int n = slot_of_tile(tt);
-    if constexpr (LIST) pos = n < n_list ? min(entry, (uint32_t)max(dm.T_max - 1, 0)) : (uint32_t)(seq.n_before + n - n_list);
-    else pos = (uint32_t)n;
-    page = (uint32_t)table[min((int)(pos >> pg.shift), pg.max_pages - 1)];
-  };
-  struct Rows {
-    u32x4 k[NLD], v[NLD];
-    uint32_t ex;   // exponents of K's (low byte) and V's row of the slot that this lane looked up
-  };
-  auto issue = [&](Rows& r) __attribute__((always_inline)) {
-    const uint32_t at_page = min(page, (uint32_t)(pg.n_pages - 1)), slot = pos & ((1u << pg.shift) - 1u);
-    const uint32_t off = at_page * page_units + slot * slot_units;
-    typedef const u32x4 __attribute__((address_space(1))) * global_row;
-#pragma unroll
-    for (int i = 0; i < NLD; ++i) {
-      const uint64_t o = (uint64_t)group_lane<LPR>(off, i) << 4;
-      r.k[i] = *(global_row)(k_pool + o);
-      r.v[i] = *(global_row)(v_pool + o);
-    }
-    if constexpr (FP8) {
-      const uint32_t s = at_page * page_scales + slot;
-      r.ex = (uint32_t)k_scales[s] | (uint32_t)v_scales[s] << 8;
-    }
-  };
-  uint16_t* kt = reinterpret_cast<uint16_t*>(smem + (size_t)w * Cfg::kWaveBytes);
-  uint16_t* vt = reinterpret_cast<uint16_t*>(smem + (size_t)w * Cfg::kWaveBytes + Cfg::kKBytes);
-  auto to_lds = [&](const Rows& r) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < NLD; ++i) {
-      uint16_t* kd = kt + (group * NLD + i) * LD + c * (16 / es);
-      uint16_t* vd = vt + (group * NLD + i) * LDV + c * (16 / es);
+    uint32_t entry = 0;          // of the tile after the one whose page is looked up
+    uint32_t pos = 0, page = 0;  // of the tile whose rows are fetched next
+    auto look_up_entry = [&](int tt) __attribute__((always_inline)) {
+      if constexpr (LIST) entry = (uint32_t)list[max(min(slot_of_tile(tt), n_list - 1), 0)];
+    };
+    auto look_up_page = [&](int tt) __attribute__((always_inline)) {
+      const int n = slot_of_tile(tt);
+      if constexpr (LIST) pos = n < n_list ? min(entry, (uint32_t)max(dm.T_max - 1, 0)) : (uint32_t)(seq.n_before + n - n_list);
+      else pos = (uint32_t)n;
+      page = (uint32_t)table[min((int)(pos >> pg.shift), pg.max_pages - 1)];
+    };
+    struct Rows {
+      u32x4 k[NLD], v[NLD];
+      uint32_t k_ex, v_ex;   // exponents of the slot that this lane looked up
+    };
+    // Requests the rows whose pages have been looked up last, and looks up the pages of tile tt and the entries of the one after it: ahead
+    // of the rows, since fetches arrive in order and the next call waits for the pages.
+    auto issue = [&](Rows& r, int tt) __attribute__((always_inline)) {
+      const uint32_t at_page = min(page, (uint32_t)(pg.n_pages - 1)), slot = pos & ((1u << pg.shift) - 1u);
+      const uint32_t off = at_page * page_units + slot * slot_units;
+      look_up_page(tt);
+      look_up_entry(tt + kPdWaves);
       if constexpr (FP8) {
-        const uint32_t ex = group_lane<LPR>(r.ex, i);
-        const float ks = row_scale(ex & 255u), vs = row_scale(ex >> 8);
-        *reinterpret_cast<u32x4*>(kd) = widen_bf16(u32x2{r.k[i][0], r.k[i][1]}, ks);
-        *reinterpret_cast<u32x4*>(kd + 8) = widen_bf16(u32x2{r.k[i][2], r.k[i][3]}, ks);
-        *reinterpret_cast<u32x4*>(vd) = widen_bf16(u32x2{r.v[i][0], r.v[i][1]}, vs);
-        *reinterpret_cast<u32x4*>(vd + 8) = widen_bf16(u32x2{r.v[i][2], r.v[i][3]}, vs);
-      } else {
-        *reinterpret_cast<u32x4*>(kd) = r.k[i];
-        *reinterpret_cast<u32x4*>(vd) = r.v[i];
+        const uint32_t s = at_page * page_scales + slot;
+        r.k_ex = k_scales[s];
+        r.v_ex = v_scales[s];
       }
-    }
-  };
-
-  Rows rows;
-  if (t < t_end) {
-    look_up_entry(t);
-    look_up_page(t);
-    look_up_entry(t + kPdWaves);
-    issue(rows);
-    look_up_page(t + kPdWaves);
-    look_up_entry(t + 2 * kPdWaves);
-  }
-
-  // Q operand: row li -> (token li / g, head li % g); padding rows repeat row 0 and are never stored
-  const int row = li < n_rows ? li : 0;
-  const int tok = row / g, hj = row % g;
-  bf16x8 qreg[KS];
-  {
-    const uint16_t* qrow = static_cast<const uint16_t*>(a.q) + b * dm.qs[0] + (size_t)(kv * g + hj) * dm.qs[1] +
-                           (size_t)tok * dm.qs[2] + 8 * hf;
+      __builtin_amdgcn_sched_barrier(0);
+      typedef const u32x4 __attribute__((address_space(1))) * global_row;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qreg[ks] = *reinterpret_cast<const bf16x8*>(qrow + ks * 16);
-  }
-
-  f32x16 o[DB];
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
-  const float sl2 = 1.4426950408889634f / sqrtf((float)D);   // the softmax scale and the change to base 2
-  for (; t < t_end; t += kPdWaves) {
-    to_lds(rows);   // (this wave's own piece of LDS: its accesses stay in order, no barrier)
-    __builtin_amdgcn_wave_barrier();
-    if (t + kPdWaves < t_end) {
-      issue(rows);
-      look_up_page(t + 2 * kPdWaves);
-      look_up_entry(t + 3 * kPdWaves);
-    }
-    const int slot0 = t * kPdTile;
-    // ---- S^T = K Q^T ----
-    f32x16 s;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) s[v] = 0.f;
-    const uint16_t* kp = kt + li * LD + 8 * hf;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kp + ks * 16), qreg[ks], s, 0, 0, 0);
-    if (slot0 + kPdTile > n_list) {   // wave-uniform: the tile touches the chunk's rows or the end
-      const int limit = n_list + tok + 1 - slot0;   // keys kk < limit of the tile are visible
-#pragma unroll
-      for (int v = 0; v < 16; ++v)
-        if (8 * (v / 4) + 4 * hf + v % 4 >= limit) s[v] = -INFINITY;
-    }
-    // ---- online softmax ----
-    float mx = -INFINITY;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[v]);
-    mx = fmaxf(mx, other_half(mx)) * sl2;
-    // the reference point only moves when the tile's maximum exceeds it by more than 2^8
-    constexpr float kLazy = 8.0f;
-    if (__builtin_amdgcn_ballot_w64(mx > m_run + kLazy) != 0) {   // wave-uniform branch
-      const float m_new = mx > m_run + kLazy ? mx : m_run;
-      const float alpha = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
-      m_run = m_new;
-      l_run *= alpha;
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) o[db][v] *= alpha;
-    }
-    const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
-    float psum = 0.f;   // (of the probabilities before they are rounded: what lse shows)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], sl2, neg_m));
-      psum += s[v];
-    }
-    l_run += psum;
-    // ---- O^T += V^T P^T ----
-    const tr_ptr vtr = (tr_ptr)(vt + (4 * hf + ((lane & 15) >> 2)) * LDV + 16 * ((lane >> 4) & 1) + 4 * (lane & 3));
-#pragma unroll
-    for (int t2 = 0; t2 < 2; ++t2) {
-      bf16x8 p;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[8 * t2 + e];   // (the operands of a product are bfloat16: one rounding)
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const int e0 = 16 * t2 * LDV + db * 32;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(vtr + e0 / 4);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(vtr + (e0 + 8 * LDV) / 4);
-        const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), p, o[db], 0, 0, 0);
+      for (int i = 0; i < NLD; ++i) {
+        const uint64_t o = (uint64_t)(group_lane<LPR>(off, i) + (uint32_t)c) << 4;
+        r.k[i] = *(global_row)(k_pool + o);
+        r.v[i] = *(global_row)(v_pool + o);
       }
-    }
-    __builtin_amdgcn_wave_barrier();
-  }
+    };
+    uint16_t* kt = reinterpret_cast<uint16_t*>(smem + (size_t)w * Cfg::kWaveBytes);
+    uint16_t* vt = reinterpret_cast<uint16_t*>(smem + (size_t)w * Cfg::kWaveBytes + Cfg::kKBytes);
+    const int turn = (row0 / Cfg::kTurn) % 2 * 8;   // FP8: where a lane's first piece of V goes
+    auto to_lds = [&](const Rows& r) __attribute__((always_inline)) {
+      const uint32_t both = FP8 ? r.k_ex | r.v_ex << 8 : 0u;
+#pragma unroll
+      for (int i = 0; i < NLD; ++i) {
+        uint16_t* kd = kt + (row0 + i) * LD + c * 8;
+        uint16_t* vd = vt + (row0 + i) * LDV + c * (16 / es);
+        if constexpr (FP8) {
+          const uint32_t ex = group_lane<LPR>(both, i);
+          const float ks = row_scale(ex & 255u), vs = row_scale(ex >> 8);
+          *reinterpret_cast<u32x4*>(kd) = widen_bf16(u32x2{r.k[i][0], r.k[i][1]}, ks);
+          *reinterpret_cast<u32x4*>(kd + D / 2) = widen_bf16(u32x2{r.k[i][2], r.k[i][3]}, ks);
+          *reinterpret_cast<u32x4*>(vd + turn) = widen_bf16(u32x2{r.v[i][0], r.v[i][1]}, vs);
+          *reinterpret_cast<u32x4*>(vd + (8 - turn)) = widen_bf16(u32x2{r.v[i][2], r.v[i][3]}, vs);
+        } else {
+          *reinterpret_cast<u32x4*>(kd) = r.k[i];
+          *reinterpret_cast<u32x4*>(vd) = r.v[i];
+        }
+      }
+    };
 
-  // ---- the four waves' partials of the real rows are merged through LDS, then the block's partial goes out ----
-  const float l_wave = l_run + other_half(l_run);
-  __syncthreads();   // the waves' pieces may be reused
-  float* mo = reinterpret_cast<float*>(smem);      // [4 waves][32 rows][LDO]
-  float* mm = mo + kPdWaves * 32 * LDO;             // [4][32]
-  float* ml = mm + kPdWaves * 32;
-  float* mw = ml + kPdWaves * 32;
-  if (li < n_rows) {
-    if (hf == 0) {
-      mm[w * 32 + li] = m_run;
-      ml[w * 32 + li] = l_wave;
+    Rows rows;
+    if (t < t_end) {
+      look_up_entry(t);
+      look_up_page(t);
+      look_up_entry(t + kPdWaves);
+      issue(rows, t + kPdWaves);
     }
-    float* rec = mo + ((size_t)w * 32 + li) * LDO + 4 * hf;
+
+    // Q operand: row li -> (token li / g, head li % g); padding rows repeat row 0 and are never stored
+    const int row = li < n_rows ? li : 0;
+    const int tok = row / g, hj = row % g;
+    bf16x8 qreg[KS];
+    {
+      const uint16_t* qrow = static_cast<const uint16_t*>(a.q) + b * dm.qs[0] + (size_t)(kv * g + hj) * dm.qs[1] +
+                             (size_t)tok * dm.qs[2] + (FP8 ? 16 : 8) * hf;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)   // (FP8: piece j of a row in LDS holds elements 16 j .. + 7, or 16 (j - D / 16) + 8 .. + 15)
+        qreg[ks] = *reinterpret_cast<const bf16x8*>(qrow + (!FP8 ? ks * 16 : ks < KS / 2 ? ks * 32 : (ks - KS / 2) * 32 + 8));
+    }
+
+    f32x16 o[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int v4 = 0; v4 < 4; ++v4)   // registers 4*v4 .. 4*v4+3 are four consecutive dims
-        *reinterpret_cast<float4*>(rec + 32 * db + 8 * v4) = make_float4(o[db][4 * v4], o[db][4 * v4 + 1], o[db][4 * v4 + 2], o[db][4 * v4 + 3]);
-  }
-  __syncthreads();
-  float* my_part = part + ((size_t)kv * n_slots + blockIdx.x) * Cfg::kRec;
-  if (tid < kPdWaves * 32 && li < n_rows) {   // thread (wave tid / 32, row tid % 32 == li)
-    float m = mm[li];
+      for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+    const float sl2 = 1.4426950408889634f / sqrtf((float)D);   // the softmax scale and the change to base 2
+    for (; t < t_end; t += kPdWaves) {
+      to_lds(rows);   // (this wave's own piece of LDS: its accesses stay in order, no barrier)
+      __builtin_amdgcn_wave_barrier();
+      if (t + kPdWaves < t_end) issue(rows, t + 2 * kPdWaves);
+      const int slot0 = t * kPdTile;
+      // ---- S^T = K Q^T ----
+      f32x16 s;
 #pragma unroll
-    for (int u = 1; u < kPdWaves; ++u) m = fmaxf(m, mm[u * 32 + li]);
-    mw[tid] = mm[tid] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mm[tid] - m);
-    if (tid < 32) my_part[32 * D + li] = m;
-  }
-  __syncthreads();
-  if (tid < n_rows) {
-    float l = 0.f;
+      for (int v = 0; v < 16; ++v) s[v] = 0.f;
+      const uint16_t* kp = kt + li * LD + 8 * hf;
 #pragma unroll
-    for (int u = 0; u < kPdWaves; ++u) l += mw[u * 32 + tid] * ml[u * 32 + tid];
-    my_part[32 * D + 32 + tid] = l;
-  }
-  for (int i = tid; i < n_rows * (D / 4); i += kPdThreads) {
-    const int r = i / (D / 4), c4 = i % (D / 4);
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int ks = 0; ks < KS; ++ks)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kp + ks * 16), qreg[ks], s, 0, 0, 0);
+      if (slot0 + kPdTile > n_list) {   // wave-uniform: the tile touches the chunk's rows or the end
+        const int limit = n_list + tok + 1 - slot0;   // keys kk < limit of the tile are visible
 #pragma unroll
-    for (int u = 0; u < kPdWaves; ++u) {
-      const float wgt = mw[u * 32 + r];
-      const float4 x = *reinterpret_cast<const float4*>(mo + ((size_t)u * 32 + r) * LDO + 4 * c4);
-      acc.x += wgt * x.x;
-      acc.y += wgt * x.y;
-      acc.z += wgt * x.z;
-      acc.w += wgt * x.w;
+        for (int v = 0; v < 16; ++v)
+          if (8 * (v / 4) + 4 * hf + v % 4 >= limit) s[v] = -INFINITY;
+      }
+      // ---- online softmax ----
+      float mx = -INFINITY;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[v]);
+      mx = fmaxf(mx, other_half(mx)) * sl2;
+      // the reference point only moves when the tile's maximum exceeds it by more than 2^8
+      constexpr float kLazy = 8.0f;
+      if (__builtin_amdgcn_ballot_w64(mx > m_run + kLazy) != 0) {   // wave-uniform branch
+        const float m_new = mx > m_run + kLazy ? mx : m_run;
+        const float alpha = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+        m_run = m_new;
+        l_run *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) o[db][v] *= alpha;
+      }
+      const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
+      float psum = 0.f;   // (of the probabilities before they are rounded: what lse shows)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], sl2, neg_m));
+        psum += s[v];
+      }
+      l_run += psum;
+      // ---- O^T += V^T P^T ----
+      // (FP8, rows in which pieces are the other way round: D = 128 rows 8 .. 15 of 16, D = 64 rows 4 .. 7 of 8)
+      const int v_at = (4 * hf + ((lane & 15) >> 2)) * LDV + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+      const tr_ptr vtr = (tr_ptr)(vt + (FP8 && D == 64 ? v_at ^ (8 * hf) : v_at)), vtr_hi = (tr_ptr)(vt + (!FP8 ? v_at : D == 64 ? v_at ^ (8 * hf) : v_at ^ 8));
+#pragma unroll
+      for (int t2 = 0; t2 < 2; ++t2) {
+        bf16x8 p;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = (__bf16)s[8 * t2 + e];   // (the operands of a product are bfloat16: one rounding)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const int e0 = 16 * t2 * LDV + db * 32;
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(vtr + e0 / 4);
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(vtr_hi + (e0 + 8 * LDV) / 4);
+          const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), p, o[db], 0, 0, 0);
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
     }
-    *reinterpret_cast<float4*>(my_part + r * D + 4 * c4) = acc;
+
+    // ---- the four waves' partials of the real rows are merged through LDS, then the block's partial goes out ----
+    const float l_wave = l_run + other_half(l_run);
+    __syncthreads();   // the waves' pieces may be reused
+    float* mo = reinterpret_cast<float*>(smem);      // [4 waves][32 rows][LDO]
+    float* mm = mo + kPdWaves * 32 * LDO;             // [4][32]
+    float* ml = mm + kPdWaves * 32;
+    float* mw = ml + kPdWaves * 32;
+    if (li < n_rows) {
+      if (hf == 0) {
+        mm[w * 32 + li] = m_run;
+        ml[w * 32 + li] = l_wave;
+      }
+      float* rec = mo + ((size_t)w * 32 + li) * LDO + 4 * hf;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int v4 = 0; v4 < 4; ++v4)   // registers 4*v4 .. 4*v4+3 are four consecutive dims
+          *reinterpret_cast<float4*>(rec + 32 * db + 8 * v4) = make_float4(o[db][4 * v4], o[db][4 * v4 + 1], o[db][4 * v4 + 2], o[db][4 * v4 + 3]);
+    }
+    __syncthreads();
+    float* my_part = part + ((size_t)kv * (n_slots + dm.b) + blockIdx.x + b) * Cfg::kRec;
+    if (tid < kPdWaves * 32 && li < n_rows) {   // thread (wave tid / 32, row tid % 32 == li)
+      float m = mm[li];
+#pragma unroll
+      for (int u = 1; u < kPdWaves; ++u) m = fmaxf(m, mm[u * 32 + li]);
+      mw[tid] = mm[tid] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mm[tid] - m);
+      if (tid < 32) my_part[32 * D + li] = m;
+    }
+    __syncthreads();
+    if (tid < n_rows) {
+      float l = 0.f;
+#pragma unroll
+      for (int u = 0; u < kPdWaves; ++u) l += mw[u * 32 + tid] * ml[u * 32 + tid];
+      my_part[32 * D + 32 + tid] = l;
+    }
+    for (int i = tid; i < n_rows * (D / 4); i += kPdThreads) {
+      const int r = i / (D / 4), c4 = i % (D / 4);
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int u = 0; u < kPdWaves; ++u) {
+        const float wgt = mw[u * 32 + r];
+        const float4 x = *reinterpret_cast<const float4*>(mo + ((size_t)u * 32 + r) * LDO + 4 * c4);
+        acc.x += wgt * x.x;
+        acc.y += wgt * x.y;
+        acc.z += wgt * x.z;
+        acc.w += wgt * x.w;
+      }
+      *reinterpret_cast<float4*>(my_part + r * D + 4 * c4) = acc;
+    }
+    __syncthreads();   // LDS is free for the next sequence
   }
 }
 
-// One block per (row, KV head, sequence).  Thread s < n_splits weighs split s; thread (four dims c4, group sg) adds up the outputs of
+// One block per (row, KV head, sequence).  Threads weigh a partial each, or two; thread (four dims c4, group sg) adds up the outputs of
 // every NG-th split, four of them on the way at a time, and the groups' sums meet in LDS, in a fixed order.
 template <int D>
 __global__ __launch_bounds__(kPdThreads) void paged_decode_merge(Dims dm, PagedArgs a, const float* __restrict__ part, int n_slots) {
   constexpr int TPR = D / 4, NG = kPdThreads / TPR, RUN = 4;
-  static_assert(kPdMaxSplits <= kPdThreads, "a thread a split");
+  static_assert(kPdMaxSlots <= 2 * kPdThreads, "two partials a thread");
   constexpr size_t REC = PdCfg<D, false>::kRec;
-  __shared__ float wgt[kPdThreads];
+  __shared__ float wgt[2 * kPdThreads];
   __shared__ float4 red[NG][TPR];
   __shared__ float wm[kPdWaves], wl[kPdWaves];
   const int r = blockIdx.x, kv = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
@@ -353,30 +376,41 @@ __global__ __launch_bounds__(kPdThreads) void paged_decode_merge(Dims dm, PagedA
     if (tid == 0 && a.lse != nullptr) a.lse[(size_t)(b * dm.n_q + h) * dm.C + tok] = -INFINITY;
     return;
   }
-  const PdWork share = pd_share(dm, a, b, kv, n_slots);
-  const int n = share.n_splits;
-  const float* base = part + ((size_t)kv * n_slots + share.first) * REC;
+  const uint32_t quota = pd_quota(pd_total(dm, a, kv), n_slots);
+  const PdPlace place = pd_place(dm, a, kv, 0u, b);
+  const uint32_t s_first = place.first / quota;
+  const int n = (int)((place.first + place.tiles - 1) / quota - s_first) + 1;
+  const float* base = part + ((size_t)kv * (n_slots + dm.b) + s_first + b) * REC;
   const int c4 = tid % TPR, sg = tid / TPR;
   float4 x[RUN];
   auto load = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < RUN; ++u) x[u] = *reinterpret_cast<const float4*>(base + (size_t)min(s0 + u * NG, n - 1) * REC + r * D + 4 * c4);
   };
-  float m_s = -INFINITY, l_s = 0.f;
-  if (tid < n) {
-    m_s = base[tid * REC + 32 * D + r];
-    l_s = base[tid * REC + 32 * D + 32 + r];
+  float m_s[2] = {-INFINITY, -INFINITY}, l_s[2] = {0.f, 0.f};
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int i = tid + u * kPdThreads;
+    if (i < n) {
+      m_s[u] = base[i * REC + 32 * D + r];
+      l_s[u] = base[i * REC + 32 * D + 32 + r];
+    }
   }
   load(sg);
-  const float m_wave = wave64_max(m_s);
+  const float m_wave = wave64_max(fmaxf(m_s[0], m_s[1]));
   if ((tid & 63) == 0) wm[tid >> 6] = m_wave;
   __syncthreads();
   float m = wm[0];
 #pragma unroll
   for (int u = 1; u < kPdWaves; ++u) m = fmaxf(m, wm[u]);   // (every row sees its own key: finite)
-  const float w = m_s == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_s - m);
-  wgt[tid] = w;
-  const float l_wave = wave64_sum(w * l_s);
+  float l_mine = 0.f;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const float w = m_s[u] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_s[u] - m);
+    wgt[tid + u * kPdThreads] = w;
+    l_mine += w * l_s[u];
+  }
+  const float l_wave = wave64_sum(l_mine);
   if ((tid & 63) == 0) wl[tid >> 6] = l_wave;
   __syncthreads();
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -419,20 +453,15 @@ __global__ __launch_bounds__(kPdThreads) void paged_decode_merge(Dims dm, PagedA
 }
 
 // ---------------------------------------------------------------------------------------------
-// Blocks per KV head: two for every compute unit, which are resident together, and where a sequence has fewer than four of them one
-// more for every sequence (each has one, and the others go by length).
-static int pd_slots(const Dims& dm) {
-  const long long n = (512 + dm.n_kv - 1) / dm.n_kv, most = (long long)kPdMaxSplits * dm.b;
-  const long long want = dm.b > 64 ? (n + dm.b - 1) / dm.b * dm.b : (4 * dm.b <= n ? n : n + dm.b);
-  return (int)(want < most ? want : most);
-}
+static int pd_slots(const Dims& dm) { return (kPdMaxSlots + dm.n_kv - 1) / dm.n_kv; }
 
-size_t paged_decode_ws_floats(const Dims& dm) { return (size_t)dm.n_kv * pd_slots(dm) * 32 * (dm.d + 2); }
+size_t paged_decode_ws_floats(const Dims& dm) { return (size_t)dm.n_kv * (pd_slots(dm) + dm.b) * 32 * (dm.d + 2); }
 
 hipError_t launch_paged_decode(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st) {
   const int n_slots = pd_slots(dm);
   const long long tiles = ((long long)attended_cap(dm, a.k_idx != nullptr) + dm.C + kPdTile - 1) / kPdTile;
-  const long long most = dm.b > 64 ? n_slots : dm.b * ((tiles + kPdWaves - 1) / kPdWaves);   // (blocks that short lists leave without work)
+  if (dm.b * tiles >= 1ll << 31) return hipErrorInvalidValue;   // (refused by the entry point)
+  const long long most = (dm.b * tiles + kPdWaves - 1) / kPdWaves;   // (blocks that short lists leave without work)
   auto launch = [&](auto d, auto eight_bit, auto is_list) -> hipError_t {
     constexpr int D = decltype(d)::value;
     constexpr bool FP8 = decltype(eight_bit)::value, LIST = decltype(is_list)::value;
