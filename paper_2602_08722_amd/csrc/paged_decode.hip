@@ -77,39 +77,27 @@ __device__ __forceinline__ PdSeq pd_seq(const Dims& dm, const PagedArgs& a, int 
   return s;
 }
 
-// Tiles of sequence `b` (none where it has no token in this chunk).
-__device__ __forceinline__ uint32_t pd_tiles(const Dims& dm, const PagedArgs& a, int b, int kv) {
-  const PdSeq s = pd_seq(dm, a, b, kv);
-  return s.C > 0 ? (uint32_t)(s.n_list + s.C + kPdTile - 1) / kPdTile : 0u;
-}
-// A sequence's place in the KV head's line of tiles.  Every wave works these out for itself, 64 sequences at a time.
-struct PdPlace {
-  int b;
-  uint32_t first, tiles;
+// 64 sequences (from b0 on) in a line of tiles: lane i has those of sequence b0 + i and where they end (a sequence without a token in
+// this chunk has none).  Every wave works it out for itself.
+struct PdLine {
+  PdSeq seq;
+  uint32_t tiles, end;
+  int b0;
 };
-__device__ __forceinline__ uint32_t pd_total(const Dims& dm, const PagedArgs& a, int kv) {
-  uint32_t total = 0;
-  for (int b0 = 0; b0 < dm.b; b0 += kWave) {
-    const int b = b0 + (threadIdx.x & 63);
-    total += (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan_u32(b < dm.b ? pd_tiles(dm, a, b, kv) : 0u), 63);
-  }
-  return total;
+__device__ __forceinline__ PdLine pd_line(const Dims& dm, const PagedArgs& a, int kv, int b0, uint32_t before) {
+  PdLine line;
+  line.b0 = b0;
+  const int b = b0 + (threadIdx.x & 63);
+  line.seq = dm.b == 1 ? pd_seq(dm, a, 0, kv) : pd_seq(dm, a, min(b, dm.b - 1), kv);   // (one sequence: scalar fetches)
+  line.tiles = b < dm.b && line.seq.C > 0 ? (uint32_t)(line.seq.n_list + line.seq.C + kPdTile - 1) / kPdTile : 0u;
+  line.end = before + (dm.b == 1 ? (uint32_t)__builtin_amdgcn_readfirstlane((int)line.tiles) : wave_incl_scan_u32(line.tiles));
+  return line;
 }
-// The sequence that tile `at` of the line belongs to (seq < 0), or sequence `seq`.
-__device__ __forceinline__ PdPlace pd_place(const Dims& dm, const PagedArgs& a, int kv, uint32_t at, int seq) {
-  uint32_t before = 0;
-  for (int b0 = 0; b0 < dm.b; b0 += kWave) {
-    const int b = b0 + (threadIdx.x & 63);
-    const uint32_t tiles = b < dm.b ? pd_tiles(dm, a, b, kv) : 0u, end = before + wave_incl_scan_u32(tiles);
-    const unsigned long long hit = __builtin_amdgcn_ballot_w64(seq < 0 ? at >= end - tiles && at < end : b == seq);
-    if (hit != 0) {
-      const int lane = (int)__builtin_ctzll(hit);
-      const uint32_t n = (uint32_t)__builtin_amdgcn_readlane((int)tiles, lane);
-      return {b0 + lane, (uint32_t)__builtin_amdgcn_readlane((int)end, lane) - n, n};
-    }
-    before = (uint32_t)__builtin_amdgcn_readlane((int)end, 63);
-  }
-  return {-1, 0u, 0u};
+__device__ __forceinline__ uint32_t last_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); }
+__device__ __forceinline__ uint32_t pd_total(const Dims& dm, const PagedArgs& a, int kv, const PdLine& start) {   // start: b0 = 0
+  uint32_t total = last_lane(start.end);
+  for (int b0 = kWave; b0 < dm.b; b0 += kWave) total = last_lane(pd_line(dm, a, kv, b0, total).end);
+  return total;
 }
 // Tiles of a block: all of them over the blocks, at least one for each wave.
 __device__ __forceinline__ uint32_t pd_quota(uint32_t total, int n_slots) {
@@ -129,17 +117,25 @@ __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 31, hf = lane >> 5;
   const int g = dm.g;
-  const uint32_t total = pd_total(dm, a, kv), quota = pd_quota(total, n_slots);
-  uint32_t line = blockIdx.x * quota;   // (blocks x quota < total + a block's share: 32 bits)
-  const uint32_t line_end = min(line + quota, total);
-  while (line < line_end) {   // block-uniform: the sequences that the block has a part of
-    const PdPlace place = pd_place(dm, a, kv, line, -1);
-    const int b = place.b;
-    const PdSeq seq = pd_seq(dm, a, b, kv);
+  PdLine line = pd_line(dm, a, kv, 0, 0u);
+  const uint32_t total = pd_total(dm, a, kv, line), quota = pd_quota(total, n_slots);
+  uint32_t at = blockIdx.x * quota;   // (blocks x quota < total + a block's share: 32 bits)
+  const uint32_t at_end = min(at + quota, total);
+  while (at < at_end) {   // block-uniform: the sequences that the block has a part of
+    unsigned long long hit;
+    while ((hit = __builtin_amdgcn_ballot_w64(at >= line.end - line.tiles && at < line.end)) == 0)   // (at < total: some sequence has it)
+      line = pd_line(dm, a, kv, line.b0 + kWave, last_lane(line.end));
+    const int of = (int)__builtin_ctzll(hit), b = line.b0 + of;
+    PdSeq seq;
+    seq.n_list = __builtin_amdgcn_readlane(line.seq.n_list, of);
+    seq.n_before = __builtin_amdgcn_readlane(line.seq.n_before, of);
+    seq.C = __builtin_amdgcn_readlane(line.seq.C, of);
+    const uint32_t end = (uint32_t)__builtin_amdgcn_readlane((int)line.end, of),
+                   first = end - (uint32_t)__builtin_amdgcn_readlane((int)line.tiles, of);
     const int n_list = seq.n_list, n_keys = n_list + seq.C, n_rows = seq.C * g;   // n_rows <= 32, checked by the launcher
-    const int t_end = (int)(min(line_end, place.first + place.tiles) - place.first);
-    int t = (int)(line - place.first) + w;   // this wave's tiles: every fourth
-    line = place.first + t_end;
+    const int t_end = (int)(min(at_end, end) - first);
+    int t = (int)(at - first) + w;   // this wave's tiles: every fourth
+    at = first + t_end;
 
     const int32_t* table = pg.table + (size_t)b * pg.max_pages;
     const int32_t* list = LIST ? a.k_idx + (size_t)(b * dm.n_kv + kv) * dm.B_max : nullptr;
@@ -376,27 +372,51 @@ __global__ __launch_bounds__(kPdThreads) void paged_decode_merge(Dims dm, PagedA
     if (tid == 0 && a.lse != nullptr) a.lse[(size_t)(b * dm.n_q + h) * dm.C + tok] = -INFINITY;
     return;
   }
-  const uint32_t quota = pd_quota(pd_total(dm, a, kv), n_slots);
-  const PdPlace place = pd_place(dm, a, kv, 0u, b);
-  const uint32_t s_first = place.first / quota;
-  const int n = (int)((place.first + place.tiles - 1) / quota - s_first) + 1;
-  const float* base = part + ((size_t)kv * (n_slots + dm.b) + s_first + b) * REC;
+  const int records = n_slots + dm.b;   // of a KV head
+  int s_first = 0, n = 0;
   const int c4 = tid % TPR, sg = tid / TPR;
   float4 x[RUN];
+  float m_s[2], l_s[2];
+  const float* base = part + (size_t)kv * records * REC;
+  // (a part past the sequence's last is some record of the KV head, and is not used)
   auto load = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int u = 0; u < RUN; ++u) x[u] = *reinterpret_cast<const float4*>(base + (size_t)min(s0 + u * NG, n - 1) * REC + r * D + 4 * c4);
+    for (int u = 0; u < RUN; ++u)
+      x[u] = *reinterpret_cast<const float4*>(base + (size_t)min(s_first + b + s0 + u * NG, records - 1) * REC + r * D + 4 * c4);
   };
-  float m_s[2] = {-INFINITY, -INFINITY}, l_s[2] = {0.f, 0.f};
+  auto load_weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int i = tid + u * kPdThreads;
-    if (i < n) {
-      m_s[u] = base[i * REC + 32 * D + r];
-      l_s[u] = base[i * REC + 32 * D + 32 + r];
+    for (int u = 0; u < 2; ++u) {
+      const float* rec = base + (size_t)min(s_first + b + tid + u * kPdThreads, records - 1) * REC + 32 * D;
+      m_s[u] = rec[r];
+      l_s[u] = rec[32 + r];
     }
+  };
+  auto find = [&]() __attribute__((always_inline)) {   // the sequence's partials: n of them from s_first + b on
+    PdLine line = pd_line(dm, a, kv, 0, 0u);
+    const uint32_t quota = pd_quota(pd_total(dm, a, kv, line), n_slots);
+    while (line.b0 + kWave <= b) line = pd_line(dm, a, kv, line.b0 + kWave, last_lane(line.end));
+    const uint32_t end = (uint32_t)__builtin_amdgcn_readlane((int)line.end, b - line.b0),
+                   first = end - (uint32_t)__builtin_amdgcn_readlane((int)line.tiles, b - line.b0);
+    s_first = (int)(first / quota);
+    n = (int)((end - 1) / quota) - s_first + 1;
+  };
+  if (dm.b == 1) {   // the partials begin at the first whatever the length is: they are requested beside it
+    load_weights();
+    load(sg);
+    __builtin_amdgcn_sched_barrier(0);
+    find();
+  } else {
+    find();
+    load_weights();
+    load(sg);
   }
-  load(sg);
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+    if (tid + u * kPdThreads >= n) {
+      m_s[u] = -INFINITY;
+      l_s[u] = 0.f;
+    }
   const float m_wave = wave64_max(fmaxf(m_s[0], m_s[1]));
   if ((tid & 63) == 0) wm[tid >> 6] = m_wave;
   __syncthreads();
