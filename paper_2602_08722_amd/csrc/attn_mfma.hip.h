@@ -141,14 +141,6 @@ __device__ __forceinline__ int k_swizzle(int row) { return D == 128 ? row & 3 : 
 template <int D>
 __device__ __forceinline__ int v_swizzle(int row) { return D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1); }
 
-__device__ __forceinline__ int k8_place(int row) { return (row & ~7) | 2 * (row & 3) | ((row >> 2) & 1); }
-__device__ __forceinline__ int k8_swizzle(int place) { return (place >> 1) & 7; }
-// Value of the first lane of the lower (0) or upper (1) eight lanes of the caller's 16-lane row.
-__device__ __forceinline__ uint32_t row8_first(uint32_t v, int upper) {
-  return upper ? (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x158, 0xF, 0xF, true)    // row_newbcast:8
-               : (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x150, 0xF, 0xF, true);
-}
-
 template <int D>
 __device__ __forceinline__ int q_swizzle(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
 
@@ -169,16 +161,11 @@ struct AttnCfg {
   // Elsewhere the stores to LDS were what staging cost (by leaving them out, blocks of eight 7 %, of four 17 - 22 %), and direct loads take
   // them off the waves: 32/8 heads, d 128, 1024 tokens over 8192 keys 140.7 -> 133.2 us, 1024 over 983 33.6 -> 31.7, 4096 over 8192
   // 576 -> 560.  (Three stages, so that every load has two steps: 1 - 3 % slower throughout.)
-  // (8-bit rows are widened on their way, so they go through registers; at d 128 those of K go straight to LDS as they are.)
+  // (8-bit rows are widened on their way, so they go through registers everywhere.)
   static constexpr bool DMA = SRC != kFp8Pages && (D == 128 || SPLIT);
   static constexpr int RPW = 64 / CG, ROW = D * 2;
   static constexpr int KG = 1024 + 64, VG = 1024;   // pitches of a group
-  // K8: K's rows are kept in 8 bits, one behind the other in groups of eight, one group a wave, and their powers of two behind all of
-  // them.  A group's places 0 .. 7 hold rows 0, 4, 1, 5, 2, 6, 3, 7: then the 16 lanes that carry a row of V, four neighbouring rows a load, are those
-  // that have fetched two rows of K, which are two of V's too, and one look-up serves both (k8_place).  16 lanes read a 16-byte piece of 16 rows at a
-  // time; the permutation of a row's pieces (k8_swizzle) puts them on distinct banks.
-  static constexpr bool K8 = SRC == kFp8Pages && D == 128;
-  static constexpr int kKTileBytes = K8 ? KT * D + 128 : KT / RPW * KG;
+  static constexpr int kKTileBytes = KT / RPW * KG;
   static constexpr int kStageBytes = kKTileBytes + KT / RPW * VG;   // one K tile and one V tile
   static constexpr size_t kOutBytes = (size_t)8 * 32 * (D + 8) * 2;   // what the rows go out through
   static constexpr size_t kQBytes = SPLIT ? 0 : (size_t)8 * 32 * ROW;   // (SPLIT: in the place of a V tile)
@@ -202,18 +189,10 @@ struct AttnCfg {
 // are blocks of eight at d 64 (1 - 1.5 % in launches of many rounds).  (As a run-time choice it cost all others 2 - 5 %.)
 // SRC = kRawPages, kFp8Pages: every row, the chunk's own among them, is found through the page table, and the row sums are those of the
 // probabilities before they are rounded (the sums are what `lse` shows; elsewhere they are of the rounded ones, in half the instructions).
-// SRC = kFp8Pages, d 128: K Q^T is formed from K's rows as they are, 8 bits and a power of two, which the matrix instruction for such operands
-// takes (v_mfma_scale_f32_32x32x64_f8f6f4: twice the products of a bfloat16 one in the same time), and from Q as the sum of two such rows: a
-// bfloat16 number has eight significant bits, its nearest e4m3 number four of them, and what is left four or fewer, so that two terms
-// with powers of two of their own are the row, but for elements below 2^-14 of its largest, which are off by 2^-22 of that.  Two products in the time of
-// one, so the matrix core has the same work as with widened rows; K's tiles are half as large, are read with half the LDS operands and cost no
-// conversion.  (V needs P as its other operand, and two terms a probability would cost more than widening V's rows, which eight waves share.  At
-// d 64 Q's terms cost short lists more than this gains: 12/4 heads, 101 - 333 tokens over 1237 - 9999 keys 47.5 -> 49.8 us.)
-// The contraction index may be permuted freely here too: piece 2 q + hf of 16 elements of a row is the lane's q-th.
 template <int D, bool SPLIT, bool XS, bool KSPLIT, bool WHOLE, int SRC = kContiguous>
 __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_args<SRC> a) {
   using Cfg = AttnCfg<D, SPLIT, SRC>;
-  constexpr bool PAGED = SRC != kContiguous, FP8 = SRC == kFp8Pages, K8 = Cfg::K8;
+  constexpr bool PAGED = SRC != kContiguous, FP8 = SRC == kFp8Pages;
   constexpr bool DMA = Cfg::DMA;
   constexpr int KT = Cfg::KT, KS = Cfg::KS, CG = Cfg::CG, RPI = Cfg::RPI, NLD = Cfg::NLD,
                 DB = Cfg::DB, HW = Cfg::HW;
@@ -303,24 +282,17 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   // never sits on the critical path.  At d 128 the 16 lanes that carry a row look up NLD rows between them, one each, and take
   // them from each other where they are used: one register instead of NLD.
   constexpr bool kShare = CG == 16;
-  constexpr int NI = K8 ? KT / 64 : kShare ? 1 : NLD;
+  constexpr int NI = kShare ? 1 : NLD;
   const int r0 = tid / CG;
-  // K8: a wave stages eight rows of every 64, K's and V's, and a lane looks up the one of which it fetches a piece of K.
-  const int wave = w + 4 * set;
-  const int row8 = 8 * wave + ((lane >> 4) | ((lane >> 1) & 4));
-  auto row_in_tile = [&](int i) __attribute__((always_inline)) {   // PAGED
-    return K8 ? row8 + 64 * i : r0 + RPI * (kShare ? lane % NLD : i);
-  };
   const uint32_t cg_src = (uint32_t)(tid % CG ^ (set == 0 ? k_swizzle<D>(lane / CG) : v_swizzle<D>(lane / CG))) * 16u;
   const uint32_t idx_max = (uint32_t)max(dm.T_max - 1, 0);
   uint32_t src[NI];     // rows of the tile to be requested next, as looked up (PAGED: the list's entries of the tile after it)
   uint32_t off[NI];     // the same as byte offsets, of the tile being requested (PAGED: in 16 bytes)
   using Row = std::conditional_t<FP8, u32x2, u32x4>;   // eight elements
-  constexpr int NR = DMA ? 1 : K8 ? KT / 32 : NLD;
-  Row R[NR];   // the tile in flight (not DMA; K8: of V)
+  Row R[DMA ? 1 : NLD];   // the tile in flight (not DMA)
   // PAGED: positions and pages of the tile to be requested next; FP8: exponents of the rows of the tile in flight, and powers of two of the
   // one before
-  uint32_t pos[PAGED ? NI : 1], page[PAGED ? NI : 1], ex[FP8 ? NI : 1], ex_old[FP8 ? NI : 1], k_ex[K8 ? NI : 1];   // (K8: ex of V's rows)
+  uint32_t pos[PAGED ? NI : 1], page[PAGED ? NI : 1], ex[FP8 ? NI : 1], ex_old[FP8 ? NI : 1];
   const int n_before = PAGED ? paged_len(dm, a, b) : 0;   // cached tokens, all of them
   const int32_t* table = nullptr;
   uint64_t pool = 0;
@@ -329,8 +301,8 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   if constexpr (PAGED) {
     table = a.pg.table + (size_t)b * a.pg.max_pages;
     constexpr int es = FP8 ? 1 : 2;
-    pool = reinterpret_cast<uint64_t>(!K8 && set == 0 ? a.pg.k : a.pg.v) + (uint64_t)kv * a.pg.st[1] * es;
-    scales = (!K8 && set == 0 ? a.pg.k_scale : a.pg.v_scale) + ((size_t)kv << a.pg.shift);
+    pool = reinterpret_cast<uint64_t>(set == 0 ? a.pg.k : a.pg.v) + (uint64_t)kv * a.pg.st[1] * es;
+    scales = (set == 0 ? a.pg.k_scale : a.pg.v_scale) + ((size_t)kv << a.pg.shift);
     page_units = (uint32_t)(a.pg.st[0] / (16 / es));
     slot_units = (uint32_t)(a.pg.st[2] / (16 / es));
     page_scales = (uint32_t)a.pg.n_kv << a.pg.shift;
@@ -340,31 +312,15 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   const uint32_t group_mine = set == 0 ? Cfg::KG : Cfg::VG;
   const uint32_t dst_mine = lds0 + (set == 0 ? 0u : (uint32_t)Cfg::kKTileBytes) + (uint32_t)w * group_mine;
   auto stage_of = [&](int t) __attribute__((always_inline)) { return (t & 1) * Cfg::kStageBytes; };
-  // PAGED: and the lane's piece of a row (K8: of V, and of K)
-  const uint64_t pool_mine = pool + (K8 ? (uint32_t)(lane % 16 ^ v_swizzle<D>(lane / 16)) * 8u : FP8 ? cg_src / 2 : cg_src);
-  uint64_t k_pool = 0;
-  const uint8_t* k_scales = nullptr;
-  if constexpr (K8) {
-    k_pool = reinterpret_cast<uint64_t>(a.pg.k) + (uint64_t)kv * a.pg.st[1] + (uint32_t)(lane % 8 ^ k8_swizzle(8 * wave + lane / 8)) * 16u;
-    k_scales = a.pg.k_scale + ((size_t)kv << a.pg.shift);
-  }
-  typedef const Row __attribute__((address_space(1))) * global_row;
-  auto request_k8 = [&](int t) __attribute__((always_inline)) {   // K8: K of tile t
-#pragma unroll
-    for (int i = 0; i < NI; ++i)
-      dma16(reinterpret_cast<const void*>(k_pool + ((uint64_t)off[i] << 4)), lds0 + (uint32_t)stage_of(t) + (uint32_t)(wave + 8 * i) * 1024u);
-  };
+  const uint64_t pool_mine = pool + (FP8 ? cg_src / 2 : cg_src);   // PAGED
   auto request = [&](int t, int k) __attribute__((always_inline)) {   // chunk k of tile t
-    if constexpr (K8) {   // (of V: rows 4 * (k % 2) + lane / 16 of the wave's group k / 2)
-      R[k] = *(global_row)(pool_mine + ((uint64_t)row8_first(off[k / 2], k % 2) << 4));
-      return;
-    }
     if constexpr (PAGED) {
       const uint32_t o = kShare ? row16_lane(off[0], k) : off[k % NI];
       const uint64_t at = pool_mine + ((uint64_t)o << 4);
       if constexpr (DMA) {
         dma16(reinterpret_cast<const void*>(at), dst_mine + (uint32_t)stage_of(t) + 4u * k * group_mine);
       } else {
+        typedef const Row __attribute__((address_space(1))) * global_row;
         R[k] = *(global_row)at;
       }
       return;
@@ -452,7 +408,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
     const int base = max(min(t, t_end - 1), 0) * KT;
 #pragma unroll
     for (int i = 0; i < NI; ++i)
-      src[i] = *reinterpret_cast<const uint32_t*>(kidx + (uint32_t)min(base + row_in_tile(i), list_last) * 4u);
+      src[i] = *reinterpret_cast<const uint32_t*>(kidx + (uint32_t)min(base + r0 + RPI * (kShare ? lane % NLD : i), list_last) * 4u);
   };
   auto look_up_pages = [&](int t) __attribute__((always_inline)) {
     if constexpr (PAGED) {
@@ -463,7 +419,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
       const char* entries = reinterpret_cast<const char*>(table);
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int row = min(base + row_in_tile(i), last) + first_pos;   // tail slots repeat a real row
+        const int row = min(base + r0 + RPI * (kShare ? lane % NLD : i), last) + first_pos;   // tail slots repeat a real row
         pos[i] = cache && sparse ? min(src[i], idx_max) : (uint32_t)row;
         page[i] = *reinterpret_cast<const uint32_t*>(entries + min(pos[i] >> a.pg.shift, (uint32_t)(a.pg.max_pages - 1)) * 4u);
       }
@@ -500,7 +456,6 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
         if constexpr (FP8) {
           ex_old[i] = ex[i] << 23;
           ex[i] = scales[pg * page_scales + slot];
-          if constexpr (K8) k_ex[i] = k_scales[pg * page_scales + slot];
         }
       }
       return;
@@ -520,32 +475,12 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   };
   auto store = [&](int t, int k, Row row) __attribute__((always_inline)) {   // (not DMA)
     u32x4 r;
-    if constexpr (K8) {
-      r = widen_bf16(row, __uint_as_float(row8_first(ex_old[k / 2], k % 2)));
-      *(u32x4 __attribute__((address_space(3)))*)(uintptr_t)(lds0 + (uint32_t)stage_of(t) + (uint32_t)(Cfg::kKTileBytes + wave * 2048 + lane * 16) +
-                                                             (uint32_t)(k / 2 * 16384 + k % 2 * 1024)) = r;
-      return;
-    }
     if constexpr (FP8) r = widen_bf16(row, __uint_as_float(kShare ? row16_lane(ex_old[0], k) : ex_old[k % NI]));
     else r = row;
     *(u32x4 __attribute__((address_space(3)))*)(uintptr_t)(dst_mine + lane * 16u + (uint32_t)stage_of(t) + 4u * k * group_mine) = r;
   };
   // Step j takes chunk k of tile j+2 (K) or j+1 (V) to LDS; through registers it was requested a step earlier.
-  auto store_exponents = [&](int t) __attribute__((always_inline)) {   // K8: of K's rows of tile t, which has been addressed last
-    if constexpr (K8) {
-      typedef uint8_t __attribute__((address_space(3))) * byte_ptr;
-      if (lane % 8 == 0) {
-#pragma unroll
-        for (int i = 0; i < NI; ++i) *(byte_ptr)(uintptr_t)(lds0 + (uint32_t)(stage_of(t) + KT * D + row8 + 64 * i)) = (uint8_t)k_ex[i];
-      }
-    }
-  };
   auto stage = [&](int j, int k) __attribute__((always_inline)) {
-    if constexpr (K8) {   // (V: as without DMA; K's tile leaves ahead of the step's first request for V)
-      store(j + 1, k, R[k]);
-      request(j + 2, k);
-      return;
-    }
     if constexpr (!DMA) store(j + 2 - set, k, R[k]);
     request(DMA ? j + 2 - set : j + 3 - set, k);
   };
@@ -559,24 +494,9 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
     address(t_begin);
     look_up(t_begin + 1);
 #pragma unroll
-    for (int k = 0; k < (K8 ? NR : NLD); ++k) request(t_begin, k);
+    for (int k = 0; k < NLD; ++k) request(t_begin, k);
   }
-  if constexpr (K8) {
-    if (t_begin < t_end) {   // K runs one tile ahead of V
-      request_k8(t_begin);
-      store_exponents(t_begin);
-      if (t_begin + 1 < t_end) {
-        address(t_begin + 1);
-        look_up(t_begin + 2);
-        request_k8(t_begin + 1);
-        store_exponents(t_begin + 1);
-      } else {   // (no second tile whose exponents would have taken the first one's place)
-#pragma unroll
-        for (int i = 0; i < NI; ++i) ex_old[i] = ex[i] << 23;
-      }
-    }
-  }
-  if (!K8 && t_begin < t_end && set == 0) {   // K runs one tile ahead of V
+  if (t_begin < t_end && set == 0) {   // K runs one tile ahead of V
     Row first[DMA ? 1 : NLD];
     if constexpr (!DMA) {
 #pragma unroll
@@ -600,63 +520,16 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
     }
   }
   // the first tile and the queries have arrived (K of the second tile may be on its way)
-  if (K8 && t_begin + 1 < t_end) {
-    wait_vmcnt<NI>();
-  } else if (set == 0 && t_begin + 1 < t_end) {
+  if (set == 0 && t_begin + 1 < t_end) {
     if constexpr (DMA) wait_vmcnt<NLD>();
   } else {
     wait_vmcnt<0>();
   }
   __syncthreads();
   // Q operand: row tok0 + li, chunk ks + KS*hf of 8 dims
-  bf16x8 qreg[K8 ? 1 : KS];
-  typedef int i32x8 __attribute__((ext_vector_type(8)));
-  constexpr int K64 = D / 64;   // steps of 64 products
-  i32x8 q8[2][K64];             // K8: two terms, and their powers of two
-  int q_exp[2];
-  if constexpr (K8) {
-    uint32_t raw[K64][16];   // pairs of bfloat16 of pieces 2 * (2 * step) + hf and 2 * (2 * step + 1) + hf
+  bf16x8 qreg[KS];
 #pragma unroll
-    for (int q = 0; q < D / 32; ++q)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const u32x4 t = *(const u32x4 __attribute__((address_space(3)))*)(uintptr_t)(q_area(t_begin) + slot * (32 * Cfg::ROW) + li * Cfg::ROW +
-                                                                                     ((2 * (2 * q + hf) + e) ^ q_swizzle<D>(li)) * 16);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) raw[q / 2][q % 2 * 8 + 4 * e + v] = t[v];
-      }
-    float top = 0.f;
-#pragma unroll
-    for (int st = 0; st < K64; ++st)
-#pragma unroll
-      for (int v = 0; v < 16; ++v)
-        top = fmaxf(top, fmaxf(fabsf(__uint_as_float(raw[st][v] << 16)), fabsf(__uint_as_float(raw[st][v] & 0xFFFF0000u))));
-    top = fmaxf(top, other_half(top));   // of the row
-    const uint32_t e = row_exponent(top);
-    const float by = row_scale(254u - e), finer = e > 4u ? 16.f : 1.f;   // (what is left is 16 or less: sixteen times that fits)
-    q_exp[0] = (int)e;
-    q_exp[1] = (int)(e > 4u ? e - 4u : e);
-#pragma unroll
-    for (int st = 0; st < K64; ++st)
-#pragma unroll
-      for (int v = 0; v < 8; ++v) {   // four elements
-        float y[4], z[4];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          y[2 * i] = __uint_as_float(raw[st][2 * v + i] << 16) * by;
-          y[2 * i + 1] = __uint_as_float(raw[st][2 * v + i] & 0xFFFF0000u) * by;
-        }
-        int t = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-        t = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], t, true);
-        widen_f32((uint32_t)t, 1.f, z);
-        int rest = __builtin_amdgcn_cvt_pk_fp8_f32((y[0] - z[0]) * finer, (y[1] - z[1]) * finer, 0, false);
-        rest = __builtin_amdgcn_cvt_pk_fp8_f32((y[2] - z[2]) * finer, (y[3] - z[3]) * finer, rest, true);
-        q8[0][st][v] = t;
-        q8[1][st][v] = rest;
-      }
-  }
-#pragma unroll
-  for (int ks = 0; ks < (K8 ? 0 : KS); ++ks)
+  for (int ks = 0; ks < KS; ++ks)
     qreg[ks] = *(const bf16x8 __attribute__((address_space(3)))*)(uintptr_t)(q_area(t_begin) + slot * (32 * Cfg::ROW) + li * Cfg::ROW +
                                                                              ((ks + KS * hf) ^ q_swizzle<D>(li)) * 16);
   // the softmax scale and the change to base 2
@@ -687,9 +560,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   for (int v = 0; v < 16; ++v) cinit[v] = 0.f;
   const int tok = tok0 + li;
   f32x16 s[2];          // S^T of a tile's two units of 32 keys
-  bf16x8 kop[K8 ? 1 : KS];       // K operands of the unit whose S is formed next
-  i32x8 kop8[K64];      // K8: the same, and the exponent of the lane's row
-  int k_exp = 0;
+  bf16x8 kop[KS];       // K operands of the unit whose S is formed next
   s16x4 vop[2 * DB][2]; // V^T operands of the unit whose P V follows: block t2 * DB + c
   bf16x8 p[2];          // P of that unit: k-slot e of this lane is key 16*t2 + 8*(e/4) + 4*hf + e%4
 
@@ -699,13 +570,6 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   for (int q = 0; q < 4; ++q)
     ka[q] = lds0 + (uint32_t)(stage_of(w0) + (sub + li) / Cfg::RPW * Cfg::KG + li % Cfg::RPW * Cfg::ROW +
                               ((q ^ k_swizzle<D>(li % Cfg::RPW)) + KS * hf) * 16);
-  uint32_t ke = 0;    // K8: pieces 2 q + hf of row li, and its exponent
-  if constexpr (K8) {
-    ke = lds0 + (uint32_t)(stage_of(w0) + KT * D + sub + li);
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      ka[q] = lds0 + (uint32_t)(stage_of(w0) + (sub + k8_place(li)) * D + ((2 * q + hf) ^ k8_swizzle(k8_place(li))) * 16);
-  }
   // V: the lane's corner of the transposing reads of dim block c: key 4*hf + (lane%16)/4, dims 16*((lane/16)%2) + 4*(lane%4)
   uint32_t va[DB];
 #pragma unroll
@@ -722,10 +586,6 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
       ka[q] += by;
       asm volatile("" : "+v"(ka[q]));
     }
-    if constexpr (K8) {
-      ke += by;
-      asm volatile("" : "+v"(ke));
-    }
   };
   auto move_v = [&](int t) __attribute__((always_inline)) {
     const uint32_t by = (uint32_t)((t & 1) ? -Cfg::kStageBytes : Cfg::kStageBytes);
@@ -736,23 +596,9 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
     }
   };
   auto read_k = [&](int u, int i) __attribute__((always_inline)) {
-    if constexpr (K8) {   // (KS calls: a piece in every other one)
-      if (i == 1) k_exp = ((const uint8_t __attribute__((address_space(3)))*)(uintptr_t)ke)[32 * u];
-      if (i % 2 != 0) return;
-      const u32x4 t = ((const u32x4 __attribute__((address_space(3)))*)(uintptr_t)ka[i / 2])[u * (32 * D / 16)];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) kop8[i / 4][i / 2 % 2 * 4 + e] = (int)t[e];
-      return;
-    }
     kop[i] = ((const bf16x8 __attribute__((address_space(3)))*)(uintptr_t)ka[i % 4])[i / 4 * 4 + u * (32 / Cfg::RPW * Cfg::KG / 16)];
   };
   auto qk_step = [&](f32x16& sn, int i) __attribute__((always_inline)) {
-    if constexpr (K8) {   // (the first term's steps, then the second's)
-      if (i % 2 != 0) return;
-      const int term = i / 2 / K64, st = i / 2 % K64;
-      sn = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kop8[st], q8[term][st], i == 0 ? cinit : sn, 0, 0, 0, k_exp, 0, q_exp[term]);
-      return;
-    }
     sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop[i], qreg[i], i == 0 ? cinit : sn, 0, 0, 0);
   };
   // scores 2*e, 2*e+1 of a unit as probabilities: rounded to bf16, and added to the row sum as the matrix core sees them
@@ -879,13 +725,6 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   // 96.1 -> 92.8 us.)
   auto begin_step = [&](int j, auto can_be_first) __attribute__((always_inline)) {
     const bool first = decltype(can_be_first)::value && j < t_begin;   // (its barrier is the one above)
-    if constexpr (K8) {
-      if (first) return;   // (K of tile j + 2 has been requested, and V is by the same rows)
-      wait_vmcnt<NR>();    // K of tile j + 1 has arrived: behind it the last step has requested V's rows only
-      __syncthreads();
-      address(j + 2);
-      return;
-    }
     if constexpr (DMA) {
       if (first) return;
       wait_vmcnt<0>();
@@ -900,25 +739,16 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   };
   // (PAGED: the look-up is some twenty instructions, so in the loop it goes between products)
   auto look_up_next = [&](int j, auto can_be_first) __attribute__((always_inline)) {
-    if (!PAGED || ((DMA || K8) && decltype(can_be_first)::value && j < t_begin)) return;
-    look_up(K8 ? j + 3 : DMA ? j + 3 - set : j + 4 - set);
+    if (!PAGED || (DMA && decltype(can_be_first)::value && j < t_begin)) return;
+    look_up(DMA ? j + 3 - set : j + 4 - set);
   };
   auto stage_all = [&](int j, auto can_be_first) __attribute__((always_inline)) {
     if (DMA && ((decltype(can_be_first)::value && j < t_begin) || j + 2 - set >= t_end)) return;
-    if constexpr (K8) {
-      if (!(decltype(can_be_first)::value && j < t_begin)) {
-        request_k8(j + 2);
-        store_exponents(j + 2);
-      }
-    }
 #pragma unroll
-    for (int k = 0; k < (K8 ? NR : NLD); ++k) stage(j, k);
+    for (int k = 0; k < NLD; ++k) stage(j, k);
   };
   auto nothing = [](int) __attribute__((always_inline)) {};
   int j = t_begin < t_end ? t_begin - 1 : t_end;
-  auto late = [&](int i) __attribute__((always_inline)) {   // K8: before the barrier of the next step, in which they are first read
-    if (K8 && i == 2 * KS - 2) store_exponents(j + 2);
-  };
   for (; j < min(w0 - 1, t_end); ++j) {
     begin_step(j, yes{});
     look_up_next(j, yes{});
@@ -929,12 +759,6 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
     // chunks as products in it (blocks of four row blocks, d 128), of both its halves.
     auto staging = [&](int i) __attribute__((always_inline)) {
       if (i == 1) look_up_next(j, no{});
-      if constexpr (K8) {
-        constexpr int every = KS / NR;
-        if (i == 3) request_k8(j + 2);
-        if (i >= KS && (i - KS) % every == 0) stage(j, (i - KS) / every);
-        return;
-      }
       constexpr int first = NLD == KS ? 0 : KS, every = (2 * KS - first) / NLD;
       if (i >= first && (i - first) % every == 0) stage(j, (i - first) / every);
     };
@@ -973,7 +797,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
       half_qk(yes{}, s[0], s[1], 1, nothing);
       move_v(j);
       mask(s[0], j + 1, 0);
-      mx = half_pv(yes{}, s[0], s[1], 1, late);
+      mx = half_pv(yes{}, s[0], s[1], 1, nothing);
       move_reference(s[0], mx);
     }
     begin_step(j, no{});
@@ -1002,7 +826,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
     look_up_next(j, no{});
     stage_all(j, no{});
   }
-  if constexpr (DMA || K8) wait_vmcnt<0>();   // nothing may land in LDS from here on
+  if constexpr (DMA) wait_vmcnt<0>();   // nothing may land in LDS from here on
 
   // ---- merge of the two wave sets (SPLIT): set 1 hands (m, l, O) to set 0 through LDS ---------------------------
   if constexpr (SPLIT) {
