@@ -1083,8 +1083,8 @@ static hipError_t launch_variant(const Dims& dm, const attn_args<SRC>& a, hipStr
   int most_splits = a.n_splits;   // of any list
   if constexpr (SRC != kContiguous && KSPLIT) {
     // The plan's blocks, shared out by the kernels.  Their records: at most min(per_block, nrb) of a block, and nrb of a sequence and share.
-    // The first bound is kept within kMaxRecords: a plan has heads * nrb * splits of them within it, two splits at least, and groups of
-    // row blocks, filled up, are less than twice nrb, so that every group keeps a block.
+    // The first bound is kept within kMaxRecords, and every group of row blocks has a block all the same: a plan has heads * nrb * splits
+    // within it, two splits at least, and groups, filled up, are less than twice nrb; or (attn_plan, the first line) the groups fit a round of blocks of eight.
     aa.per_block = 2 * Cfg::HW;
     aa.tile_keys = Cfg::KT;
     const int of_block = aa.per_block < nrb ? aa.per_block : nrb;
@@ -1158,8 +1158,16 @@ struct AttnPlan {
   int n_splits;
 };
 
-inline AttnPlan attn_plan(const Dims& dm, bool sparse) {
+// Over pages, where a list's shares go by each sequence's length (list_shares): lists of 8192 keys and more of a batch whose blocks of eight
+// fill seven eighths of a round at most are shared by the blocks of a whole round.  (27 batches of 2 - 13 sequences, 130 - 224 blocks of
+// eight, 8400 - 31200 keys and chunk tokens together: 0.84 - 0.90 of the time of whole lists in blocks of four for equal lengths, 0.73 - 1.05 for
+// lengths and chunks up to eight times apart; fuller rounds and 2000 - 8000 keys 0.9 - 1.2, shorter lists 1.1 - 2.)
+inline AttnPlan attn_plan(const Dims& dm, bool sparse, bool paged = false) {
   const long long nrb = (long long)dm.g * ((dm.C + 31) / 32), heads = (long long)dm.n_kv * dm.b;
+  const long long eights = heads * ((nrb + 7) / 8);
+  if (paged && dm.b > 1 && dm.b <= kWave && heads * nrb * 2 > kMaxRecords && eights <= kComputeUnits * 7 / 8 &&
+      attended_cap(dm, sparse) + dm.C >= 8192 && dm.b * ((nrb + 7) / 8) <= kComputeUnits / dm.n_kv)
+    return AttnPlan{false, 2};
   if (heads * nrb * 2 > kMaxRecords) return AttnPlan{!eight_row_blocks(dm, sparse, heads * ((nrb + 7) / 8)), 1};
   struct Fit {
     float fixed, step, round, per_mb, per_split, beyond_four;   // a step is 8 row blocks x 64 keys or 4 x 128

@@ -10,7 +10,7 @@ static hipError_t launch_paged_ds(const Dims& dm, const PagedAttnArgs& a, hipStr
 }
 
 hipError_t launch_paged_attn_bf16(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st) {
-  const AttnPlan p = attn_plan(dm, a.k_idx != nullptr);
+  const AttnPlan p = attn_plan(dm, a.k_idx != nullptr, true);
   PagedAttnArgs aa = paged_attn_args(a, part);
   aa.n_splits = p.n_splits;
   auto launch = [&](auto d, auto src) {

@@ -277,6 +277,15 @@ ATTN_CASES = [
     dict(dtype="bf16", fp8=False, n_q=32, n_kv=8, d=128, page_len=16, C=333, lens=[65, 64]),
     dict(dtype="bf16", fp8=True, n_q=32, n_kv=8, d=64, page_len=16, C=1100, lens=[100]),       # more than 1024 row blocks
     dict(dtype="bf16", fp8=True, n_q=32, n_kv=8, d=128, page_len=16, C=1100, lens=[100]),
+    # more sequences than a wave has lanes; lists shared by blocks of eight and of four row blocks, by a round of blocks
+    dict(dtype="bf16", fp8=True, n_q=4, n_kv=2, d=64, page_len=16, C=2, lens=[(37 * i) % 211 for i in range(150)],
+         chunks=[(5 * i) % 3 for i in range(150)]),
+    dict(dtype="bf16", fp8=True, n_q=4, n_kv=1, d=128, page_len=32, C=20, lens=[40 * i for i in range(70)], chunks=[20 - i % 7 for i in range(70)]),
+    dict(dtype="bf16", fp8=False, n_q=4, n_kv=1, d=64, page_len=32, C=20, lens=[3000 - 40 * i for i in range(70)]),
+    dict(dtype="bf16", fp8=True, n_q=12, n_kv=4, d=128, page_len=64, C=333, lens=[6000, 700, 3100], chunks=[333, 101, 0]),
+    dict(dtype="bf16", fp8=False, n_q=12, n_kv=4, d=128, page_len=64, C=333, lens=[6000, 700, 3100], chunks=[101, 333, 279]),
+    dict(dtype="bf16", fp8=False, n_q=16, n_kv=8, d=64, page_len=64, C=1060, lens=[8000, 1500], chunks=[1060, 700]),
+    dict(dtype="bf16", fp8=True, n_q=16, n_kv=8, d=128, page_len=64, C=1060, lens=[900, 7500]),
     # float32
     dict(dtype="f32", fp8=False, n_q=4, n_kv=2, d=64, page_len=16, C=1, lens=[0, 100, 16]),
     dict(dtype="f32", fp8=True, n_q=4, n_kv=2, d=128, page_len=32, C=1, lens=[2000]),
@@ -355,6 +364,37 @@ def test_attention_of_large_logits(case):
     bound = (1.05 * 2.0 ** -8 * (weight + np.abs(want)) if case["dtype"] == "bf16" else 0.0) + 8e-4 * weight + 1e-6
     assert np.all(np.abs(got[0] - want) <= bound)
     assert np.all(np.abs(buf.lse[0].cpu().numpy() - lse) <= 8e-4)
+
+
+@pytest.mark.parametrize("C,n_kv", [(1, 2), (150, 2), (1100, 8)])
+def test_queries_and_rows_of_every_size(C, n_kv):
+    """8-bit pages, rows whose powers of two lie far apart.  Queries whose elements span 2^-30 .. 1 of the row's largest, rows of zeros, and
+    rows at the smallest powers of two that bfloat16 has; keys from 2^-6 to 1; values from 2^-60 to 2^60 (of one head each, so that the
+    small ones show)."""
+    case = dict(dtype="bf16", fp8=True, n_q=4 * n_kv, n_kv=n_kv, d=128, page_len=32, C=C, lens=[400])
+    rng = np.random.default_rng(30)
+    held = 400 + C
+    k = P.store(rng.standard_normal((held, n_kv, 128)) * np.exp2(rng.integers(-6, 1, (held, n_kv, 1))), "bf16").astype(np.float64)
+    v = P.store(rng.standard_normal((held, n_kv, 128)) * np.exp2(np.linspace(-60, 60, n_kv).astype(int)[:, None]), "bf16").astype(np.float64)
+    pool = P.Pool(rng, [k], [v], n_kv, 128, 32, "bf16", True)
+    q = rng.standard_normal((1, 4 * n_kv, C, 128)) * np.exp2(rng.integers(-30, 1, (1, 4 * n_kv, C, 128)))
+    q *= np.exp2(rng.integers(-3, 6, (1, 4 * n_kv, C, 1)))
+    q[:, 1] = 0.0
+    q[:, 2] *= 2.0 ** -120
+    q[:, 3, :, 5] = 2.0 ** 9
+    q = P.store(q, "bf16")
+    buf = _buffers(_pk(), case, pool, q, None)
+    buf.attn()
+    torch.cuda.synchronize()
+    want, lse, weight = P.attention(q[0].astype(np.float64), pool.k[0], pool.v[0], 400)
+    got = buf.out[0].float().cpu().numpy().astype(np.float64)
+    # a query is off by 2^-22 of its largest element, a logit by 2^-22 * 2^9 * 448 * 8 / sqrt(128) at most there and with float32 sums: 1e-3
+    # on the row with the outlier, 1e-4 elsewhere, and a probability by as much relatively
+    slack = np.full((4 * n_kv, 1, 1), 1e-4)
+    slack[3] = 2e-3
+    bound = 1.05 * 2.0 ** -8 * (weight + np.abs(want)) + 2 * slack * weight + 1e-30
+    assert np.all(np.abs(got - want) <= bound), np.max(np.abs(got - want) / bound)
+    assert np.all(np.abs(buf.lse[0].cpu().numpy() - lse) <= slack[:, 0])
 
 
 def test_malformed_lists_and_entries_stay_inside_the_pool():
