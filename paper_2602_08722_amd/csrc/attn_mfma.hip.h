@@ -60,9 +60,8 @@ static_assert(((long long)kMaxKv / kSub + kMaxChunk / kSub + 2) * kMaxKeySplits 
 //                would leave compute units without a block.
 // Index of the sequence whose length has descending rank `rank` among lens[0], lens[stride], ... (nb <= 64 of them; ties
 // keep batch order).  Every wave works it out for itself: one load, nb lane reads, a ballot.
-__device__ __forceinline__ int seq_of_rank(const int32_t* __restrict__ lens, int stride, int nb, int rank) {
+__device__ __forceinline__ int seq_of_rank(int mine, int nb, int rank) {   // mine: lane i's length
   const int lane = threadIdx.x & 63;
-  const int mine = lane < nb ? lens[lane * stride] : -1;
   int r = 0;
   for (int j = 0; j < nb; ++j) {
     const int other = __builtin_amdgcn_readlane(mine, j);
@@ -70,6 +69,10 @@ __device__ __forceinline__ int seq_of_rank(const int32_t* __restrict__ lens, int
   }
   const unsigned long long hit = __builtin_amdgcn_ballot_w64(lane < nb && r == rank);
   return hit ? (int)__builtin_ctzll(hit) : rank;
+}
+__device__ __forceinline__ int seq_of_rank(const int32_t* __restrict__ lens, int stride, int nb, int rank) {
+  const int lane = threadIdx.x & 63;
+  return seq_of_rank(lane < nb ? lens[lane * stride] : -1, nb, rank);
 }
 
 // Two floats as bf16, rounded to nearest even by one instruction.  (In integer arithmetic the rows' way out takes 300 more: 32/8 heads, d
@@ -80,25 +83,34 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 }
 
 // Shares of key lists in a launch over pages, whose sequences differ in length and in tokens: the fewest tiles a block with which the
-// sequences' groups of `per_block` row blocks fit the `slots` blocks of a KV head, so that blocks take about equally long whatever the
+// sequences' groups of 2^block_shift row blocks fit the `slots` blocks of a KV head, so that blocks take about equally long whatever the
 // lengths (an equal number of shares for each, 4 KV heads of 3, d 64, 101 - 333 tokens over 1237 - 9999 keys: 60 us).  More than 64
 // sequences: an equal number each.  Every wave works it out for itself, lane i for sequence i; the merge does the same.
+struct PagedSeq {
+  int C, before, n;   // chunk tokens, cached tokens, list slots attended
+};
+__device__ __forceinline__ PagedSeq paged_seq(const Dims& dm, const PagedAttnArgs& a, int kv, int b) {
+  const int before = paged_len(dm, a, b);
+  return {chunk_of(dm, a, b), before, a.k_idx != nullptr ? min(max(a.n_cache[b * dm.n_kv + kv], 0), dm.B_max) : before};
+}
 struct ListShare {
   int b, n_splits;          // b < 0: nothing to do
   uint32_t block, record;   // the block's number among the sequence's; the sequence's first record of the KV head's
+  PagedSeq seq;
 };
 struct ListShares {   // of lane i's sequence
   uint32_t n_splits, first_block, blocks, first_record;
+  PagedSeq seq;
 };
 __device__ __forceinline__ ListShares list_shares(const Dims& dm, const PagedAttnArgs& a, int kv) {
   const int lane = threadIdx.x & 63;
   uint32_t row_blocks = 0, groups = 0, tiles = 0;
+  auto of_two = [](uint32_t x, int shift) __attribute__((always_inline)) { return (x + (1u << shift) - 1u) >> shift; };   // x / 2^shift, rounded up
+  const PagedSeq seq = paged_seq(dm, a, kv, min(lane, dm.b - 1));
   if (lane < dm.b) {
-    const int C = chunk_of(dm, a, lane);
-    const int n = a.k_idx != nullptr ? min(max(a.n_cache[lane * dm.n_kv + kv], 0), dm.B_max) : paged_len(dm, a, lane);
-    row_blocks = (uint32_t)(dm.g * ((C + 31) / 32));
-    groups = (row_blocks + a.per_block - 1) / a.per_block;
-    tiles = C == 0 ? 0u : (uint32_t)((n + a.tile_keys - 1) / a.tile_keys + (C + a.tile_keys - 1) / a.tile_keys);
+    row_blocks = (uint32_t)(dm.g * ((seq.C + 31) / 32));
+    groups = of_two(row_blocks, a.block_shift);
+    tiles = seq.C == 0 ? 0u : of_two(seq.n, a.tile_shift) + of_two(seq.C, a.tile_shift);
   }
   const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan_u32(groups), 63);
   const float work = wave64_sum((float)groups * (float)tiles);
@@ -115,31 +127,37 @@ __device__ __forceinline__ ListShares list_shares(const Dims& dm, const PagedAtt
   }
   const uint32_t n = shares_of(hi);
   const uint32_t blocks = groups * n, records = row_blocks * n;
-  return {n, wave_incl_scan_u32(blocks) - blocks, blocks, wave_incl_scan_u32(records) - records};
+  return {n, wave_incl_scan_u32(blocks) - blocks, blocks, wave_incl_scan_u32(records) - records, seq};
 }
 // The share of block `slot` (b < 0: of the block itself, else of sequence b's block 0).
 __device__ __forceinline__ ListShare list_share(const Dims& dm, const PagedAttnArgs& a, int kv, int slot, int b) {
   if (dm.b > kWave) {
-    const int each = a.slots / dm.b, groups = (dm.g * ((dm.C + 31) / 32) + a.per_block - 1) / a.per_block, n = each / groups;
+    const int each = a.slots / dm.b, groups = (dm.g * ((dm.C + 31) / 32) + (1 << a.block_shift) - 1) >> a.block_shift, n = each / groups;
     if (b < 0) b = slot / each;
-    return {b < dm.b && slot % each < groups * n ? b : -1, n, (uint32_t)(slot % each), (uint32_t)(b * dm.g * ((dm.C + 31) / 32) * n)};
+    return {b < dm.b && slot % each < groups * n ? b : -1, n, (uint32_t)(slot % each), (uint32_t)(b * dm.g * ((dm.C + 31) / 32) * n),
+            paged_seq(dm, a, kv, min(b, dm.b - 1))};
   }
   const ListShares s = list_shares(dm, a, kv);
   if (b < 0) {
     const unsigned long long mine = __builtin_amdgcn_ballot_w64((uint32_t)slot >= s.first_block && (uint32_t)slot < s.first_block + s.blocks);
-    if (mine == 0) return {-1, 1, 0u, 0u};
+    if (mine == 0) return {-1, 1, 0u, 0u, {}};
     b = (int)__builtin_ctzll(mine);
   } else {
     slot = __builtin_amdgcn_readlane((int)s.first_block, b);
   }
   return {b, __builtin_amdgcn_readlane((int)s.n_splits, b), (uint32_t)(slot - __builtin_amdgcn_readlane((int)s.first_block, b)),
-          (uint32_t)__builtin_amdgcn_readlane((int)s.first_record, b)};
+          (uint32_t)__builtin_amdgcn_readlane((int)s.first_record, b),
+          {__builtin_amdgcn_readlane(s.seq.C, b), __builtin_amdgcn_readlane(s.seq.before, b), __builtin_amdgcn_readlane(s.seq.n, b)}};
 }
 
 template <int D>
 __device__ __forceinline__ int k_swizzle(int row) { return D == 128 ? row & 3 : (row >> 1) & 3; }
-template <int D>
-__device__ __forceinline__ int v_swizzle(int row) { return D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1); }
+// (FP8: where a lane stores two chunks of a row, one after the other, 16 lanes cover two rows, at d 64 four, which differ in bit 0)
+template <int D, bool FP8 = false>
+__device__ __forceinline__ int v_swizzle(int row) {
+  const int x = D == 128 ? row & 3 : (row >> 1) & 1;
+  return FP8 ? 4 * x ^ (x & 1) : 4 * x;
+}
 
 template <int D>
 __device__ __forceinline__ int q_swizzle(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
@@ -148,8 +166,10 @@ template <int D, bool SPLIT, int SRC = kContiguous>
 struct AttnCfg {
   static constexpr int KT = SPLIT ? 2 * kSub : kSub;  // keys per staged tile
   static constexpr int KS = D / 16;                   // k-steps of the QK^T product
+  static constexpr bool FP8 = SRC == kFp8Pages;
   static constexpr int CG = D / 8;                    // 16-byte chunks per row
-  static constexpr int RPI = kSetThreads / CG;        // rows per set-wide load
+  static constexpr int LPR = FP8 ? CG / 2 : CG;       // lanes that fetch a row, 16 bytes each
+  static constexpr int RPI = kSetThreads / LPR;       // rows per set-wide load
   static constexpr int NLD = KT / RPI;                // loads per thread per tile (set 0 loads K, set 1 loads V)
   static constexpr int DB = D / 32;                   // dim blocks of the PV product
   static constexpr int HW = SPLIT ? 2 : 4;            // front (= back) row blocks per block
@@ -161,17 +181,18 @@ struct AttnCfg {
   // Elsewhere the stores to LDS were what staging cost (by leaving them out, blocks of eight 7 %, of four 17 - 22 %), and direct loads take
   // them off the waves: 32/8 heads, d 128, 1024 tokens over 8192 keys 140.7 -> 133.2 us, 1024 over 983 33.6 -> 31.7, 4096 over 8192
   // 576 -> 560.  (Three stages, so that every load has two steps: 1 - 3 % slower throughout.)
-  // (8-bit rows are widened on their way, so they go through registers everywhere.)
-  static constexpr bool DMA = SRC != kFp8Pages && (D == 128 || SPLIT);
+  // (8-bit rows are widened on their way, so they go through registers everywhere; a load is two chunks, which are stored one after the
+  // other, at one address a tile but for constants: V's groups lie as K's do.)
+  static constexpr bool DMA = !FP8 && (D == 128 || SPLIT);
   static constexpr int RPW = 64 / CG, ROW = D * 2;
-  static constexpr int KG = 1024 + 64, VG = 1024;   // pitches of a group
+  static constexpr int KG = 1024 + 64, VG = FP8 ? KG : 1024;   // pitches of a group
   static constexpr int kKTileBytes = KT / RPW * KG;
   static constexpr int kStageBytes = kKTileBytes + KT / RPW * VG;   // one K tile and one V tile
   static constexpr size_t kOutBytes = (size_t)8 * 32 * (D + 8) * 2;   // what the rows go out through
   static constexpr size_t kQBytes = SPLIT ? 0 : (size_t)8 * 32 * ROW;   // (SPLIT: in the place of a V tile)
   static constexpr size_t kInBytes = (size_t)2 * kStageBytes + kQBytes;
   static constexpr size_t kLdsBytes = kInBytes > kOutBytes ? kInBytes : kOutBytes;
-  static_assert(!SPLIT || KT / RPW * VG == 4 * 32 * ROW, "the rows of four row blocks in the place of a V tile");
+  static_assert(!SPLIT || KT / RPW * VG >= 4 * 32 * ROW, "the rows of four row blocks in the place of a V tile");
   static constexpr int kRecFloats = 32 * (D + 2);     // partial of a row block: O as the registers lie, m, l
 };
 
@@ -194,7 +215,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   using Cfg = AttnCfg<D, SPLIT, SRC>;
   constexpr bool PAGED = SRC != kContiguous, FP8 = SRC == kFp8Pages;
   constexpr bool DMA = Cfg::DMA;
-  constexpr int KT = Cfg::KT, KS = Cfg::KS, CG = Cfg::CG, RPI = Cfg::RPI, NLD = Cfg::NLD,
+  constexpr int KT = Cfg::KT, KS = Cfg::KS, CG = Cfg::CG, LPR = Cfg::LPR, RPI = Cfg::RPI, NLD = Cfg::NLD,
                 DB = Cfg::DB, HW = Cfg::HW;
   extern __shared__ __align__(16) unsigned char smem[];
 
@@ -206,15 +227,28 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   // (The chunks of a prompt lie shortest first: no length to wait for.)
   int b = dm.prompt_chunks ? dm.b - 1 - (int)blockIdx.z : (int)blockIdx.z;
   [[maybe_unused]] ListShare share = {};
+  [[maybe_unused]] PagedSeq seq = {};
   if constexpr (PAGED && KSPLIT) {
     share = list_share(dm, a, kv, blockIdx.y, -1);
     if (share.b < 0) return;   // block-uniform
     b = share.b;
+    seq = share.seq;
+  } else if constexpr (PAGED) {
+    if (dm.b > 1 && dm.b <= kWave) {   // (all that is asked of the lengths is fetched at once)
+      const int l = threadIdx.x & 63;
+      const PagedSeq mine = paged_seq(dm, a, kv, min(l, dm.b - 1));
+      b = seq_of_rank(l < dm.b ? mine.n : -1, dm.b, blockIdx.z);
+      seq = {__builtin_amdgcn_readlane(mine.C, b), __builtin_amdgcn_readlane(mine.before, b), __builtin_amdgcn_readlane(mine.n, b)};
+    } else {
+      seq = paged_seq(dm, a, kv, b);
+    }
   } else if (dm.b > 1 && dm.b <= kWave && !dm.prompt_chunks)
     b = seq_of_rank(sparse ? a.n_cache + kv : a.n_cache, sparse ? dm.n_kv : dm.ls, dm.b, blockIdx.z);
   // The list's length and the arguments that the start needs, fetched together: one by one, where each is first used, they are four fetches
   // in a row.
-  const int n_given = a.n_cache[sparse ? b * dm.n_kv + kv : b * dm.ls];
+  int n_given;
+  if constexpr (PAGED) n_given = seq.n;
+  else n_given = a.n_cache[sparse ? b * dm.n_kv + kv : b * dm.ls];
   if constexpr (!PAGED)
     asm volatile("" ::"s"(dm.g), "s"(dm.C), "s"(dm.T_max), "s"(dm.B_max), "s"(dm.C_last),
                  "s"(dm.qs[0]), "s"(dm.qs[1]), "s"(dm.qs[2]), "s"(dm.kvs[0]), "s"(dm.kvs[1]), "s"(dm.kvs[2]), "s"(dm.cks[0]), "s"(dm.cks[1]),
@@ -226,7 +260,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int set = __builtin_amdgcn_readfirstlane(threadIdx.x / kSetThreads);
   const int li = lane & 31, hf = lane >> 5;
-  const int C = chunk_of(dm, a, b), g = dm.g;
+  const int C = PAGED ? seq.C : chunk_of(dm, a, b), g = dm.g;
   const int ntt = (C + 31) / 32;
   const int nrb = g * ntt;                       // row blocks of this KV head
   const int half = (nrb + 1) / 2;                // row blocks [0, half) are "front", [half, nrb) "back"
@@ -277,23 +311,35 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   const char* chunk_base = reinterpret_cast<const char*>(static_cast<const uint16_t*>(chunk_t) + b * dm.cks[0] + kv * dm.cks[1]);
   const char* kidx = sparse ? reinterpret_cast<const char*>(a.k_idx + (size_t)(b * dm.n_kv + kv) * dm.B_max) : nullptr;
   const uint32_t cache_row_bytes = (uint32_t)dm.kvs[2] * 2u, chunk_row_bytes = (uint32_t)dm.cks[2] * 2u;
-  // Staging.  Thread (r0, cg) fetches slot cg of rows r0 + RPI * k of this set's tensor, k < NLD: a load of a wave fills a group.
+  // Staging.  Thread (r0, cg) fetches slot cg of rows r0 + RPI * k of this set's tensor, k < NLD: a load of a wave fills a group (FP8: 16
+  // elements, two slots of a row; two groups).
   // Source rows of a tile are looked up a step ahead of the loads that use them, so the dependent index -> row fetch of the gather
   // never sits on the critical path.  At d 128 the 16 lanes that carry a row look up NLD rows between them, one each, and take
-  // them from each other where they are used: one register instead of NLD.
-  constexpr bool kShare = CG == 16;
+  // them from each other where they are used: one register instead of NLD.  (FP8: every four lanes.)
+  constexpr bool kShare = CG == 16 || FP8;
   constexpr int NI = kShare ? 1 : NLD;
-  const int r0 = tid / CG;
-  const uint32_t cg_src = (uint32_t)(tid % CG ^ (set == 0 ? k_swizzle<D>(lane / CG) : v_swizzle<D>(lane / CG))) * 16u;
+  const int r0 = tid / LPR;
+  const uint32_t cg_src =
+      (uint32_t)(FP8 ? tid % LPR : tid % CG ^ (set == 0 ? k_swizzle<D>(lane / CG) : v_swizzle<D>(lane / CG))) * 16u;
+  auto of_row = [&](uint32_t v, int k) __attribute__((always_inline)) {   // kShare: what the lane that looks up row k has
+    if constexpr (!FP8) return row16_lane(v, k);
+    static_assert(!FP8 || NLD == 1 || NLD == 2 || NLD == 4, "rows of four lanes");
+    if constexpr (NLD == 1) return v;
+    switch (k) {
+      case 0: return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x00, 0xF, 0xF, true);   // quad_perm
+      case 1: return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x55, 0xF, 0xF, true);
+      case 2: return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xAA, 0xF, 0xF, true);
+      default: return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xFF, 0xF, 0xF, true);
+    }
+  };
   const uint32_t idx_max = (uint32_t)max(dm.T_max - 1, 0);
   uint32_t src[NI];     // rows of the tile to be requested next, as looked up (PAGED: the list's entries of the tile after it)
   uint32_t off[NI];     // the same as byte offsets, of the tile being requested (PAGED: in 16 bytes)
-  using Row = std::conditional_t<FP8, u32x2, u32x4>;   // eight elements
-  Row R[DMA ? 1 : NLD];   // the tile in flight (not DMA)
+  u32x4 R[DMA ? 1 : NLD];   // the tile in flight (not DMA)
   // PAGED: positions and pages of the tile to be requested next; FP8: exponents of the rows of the tile in flight, and powers of two of the
   // one before
   uint32_t pos[PAGED ? NI : 1], page[PAGED ? NI : 1], ex[FP8 ? NI : 1], ex_old[FP8 ? NI : 1];
-  const int n_before = PAGED ? paged_len(dm, a, b) : 0;   // cached tokens, all of them
+  const int n_before = PAGED ? seq.before : 0;   // cached tokens, all of them
   const int32_t* table = nullptr;
   uint64_t pool = 0;
   const uint8_t* scales = nullptr;
@@ -311,23 +357,28 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
   const uint32_t group_mine = set == 0 ? Cfg::KG : Cfg::VG;
   const uint32_t dst_mine = lds0 + (set == 0 ? 0u : (uint32_t)Cfg::kKTileBytes) + (uint32_t)w * group_mine;
+  uint32_t dst_lane = 0;   // FP8: where the first of a load's chunks goes; the other's place is 16 bytes away
+  if constexpr (FP8) {
+    const int r = lane / LPR % Cfg::RPW;
+    dst_lane = dst_mine + (uint32_t)((w + lane / 32) * Cfg::KG + r * Cfg::ROW + (2 * (lane % LPR) ^ (set == 0 ? k_swizzle<D>(r) : v_swizzle<D, true>(r))) * 16);
+  }
   auto stage_of = [&](int t) __attribute__((always_inline)) { return (t & 1) * Cfg::kStageBytes; };
-  const uint64_t pool_mine = pool + (FP8 ? cg_src / 2 : cg_src);   // PAGED
+  const uint64_t pool_mine = pool + cg_src;   // PAGED
   auto request = [&](int t, int k) __attribute__((always_inline)) {   // chunk k of tile t
     if constexpr (PAGED) {
-      const uint32_t o = kShare ? row16_lane(off[0], k) : off[k % NI];
+      const uint32_t o = kShare ? of_row(off[0], k) : off[k % NI];
       const uint64_t at = pool_mine + ((uint64_t)o << 4);
       if constexpr (DMA) {
         dma16(reinterpret_cast<const void*>(at), dst_mine + (uint32_t)stage_of(t) + 4u * k * group_mine);
       } else {
-        typedef const Row __attribute__((address_space(1))) * global_row;
+        typedef const u32x4 __attribute__((address_space(1))) * global_row;
         R[k] = *(global_row)at;
       }
       return;
     }
     const uint32_t o = kShare ? row16_lane(off[0], k) + cg_src : off[k % NI];
     if constexpr (DMA) dma16(req_base, o, dst_mine + (uint32_t)stage_of(t) + 4u * k * group_mine);
-    else R[k] = *reinterpret_cast<const Row*>(req_base + o);
+    else R[k] = *reinterpret_cast<const u32x4*>(req_base + o);
   };
   auto q_area = [&](int t_first) __attribute__((always_inline)) {
     return lds0 + (uint32_t)(SPLIT ? stage_of(t_first + 1) + Cfg::kKTileBytes : 2 * Cfg::kStageBytes);
@@ -473,16 +524,28 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
       for (int i = 0; i < NI; ++i) off[i] = min(src[i], row_max) * row_bytes + cg_src;
     }
   };
-  auto store = [&](int t, int k, Row row) __attribute__((always_inline)) {   // (not DMA)
-    u32x4 r;
-    if constexpr (FP8) r = widen_bf16(row, __uint_as_float(kShare ? row16_lane(ex_old[0], k) : ex_old[k % NI]));
-    else r = row;
-    *(u32x4 __attribute__((address_space(3)))*)(uintptr_t)(dst_mine + lane * 16u + (uint32_t)stage_of(t) + 4u * k * group_mine) = r;
+  constexpr int kParts = FP8 ? 2 : 1;   // chunks of a load
+  uint32_t put[2] = {0, 0};             // FP8: their places in the tile that is stored, row r0
+  auto put_in = [&](int t) __attribute__((always_inline)) {
+    if constexpr (FP8) {
+      put[0] = dst_lane + (uint32_t)stage_of(t);
+      put[1] = put[0] ^ 16u;
+      asm volatile("" : "+v"(put[0]), "+v"(put[1]));   // (or every store works out its own address)
+    }
   };
-  // Step j takes chunk k of tile j+2 (K) or j+1 (V) to LDS; through registers it was requested a step earlier.
-  auto stage = [&](int j, int k) __attribute__((always_inline)) {
-    if constexpr (!DMA) store(j + 2 - set, k, R[k]);
-    request(DMA ? j + 2 - set : j + 3 - set, k);
+  auto store = [&](int t, int k, int part, const u32x4& row) __attribute__((always_inline)) {   // (not DMA)
+    typedef u32x4 __attribute__((address_space(3))) * lds_row;
+    if constexpr (FP8)
+      *((lds_row)(uintptr_t)put[part] + k * (RPI / Cfg::RPW) * Cfg::KG / 16) =
+          widen_bf16(part == 0 ? u32x2{row[0], row[1]} : u32x2{row[2], row[3]}, __uint_as_float(of_row(ex_old[0], k)));
+    else
+      *(lds_row)(uintptr_t)(dst_mine + lane * 16u + (uint32_t)stage_of(t) + 4u * k * group_mine) = row;
+  };
+  // Step j takes chunk i of tile j+2 (K) or j+1 (V) to LDS; through registers it was requested a step earlier.
+  constexpr int NST = NLD * kParts;
+  auto stage = [&](int j, int i) __attribute__((always_inline)) {
+    if constexpr (!DMA) store(j + 2 - set, i / kParts, i % kParts, R[i / kParts]);
+    if (i % kParts == kParts - 1) request(DMA ? j + 2 - set : j + 3 - set, i / kParts);
   };
 
   if constexpr (!KSPLIT && !PAGED) {
@@ -497,7 +560,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
     for (int k = 0; k < NLD; ++k) request(t_begin, k);
   }
   if (t_begin < t_end && set == 0) {   // K runs one tile ahead of V
-    Row first[DMA ? 1 : NLD];
+    u32x4 first[DMA ? 1 : NLD];
     if constexpr (!DMA) {
 #pragma unroll
       for (int k = 0; k < NLD; ++k) first[k] = R[k];
@@ -515,8 +578,9 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
       for (int i = 0; i < NI; ++i) ex_old[i] = ex[i] << 23;
     }
     if constexpr (!DMA) {
+      put_in(t_begin);
 #pragma unroll
-      for (int k = 0; k < NLD; ++k) store(t_begin, k, first[k]);
+      for (int i = 0; i < NST; ++i) store(t_begin, i / kParts, i % kParts, first[i / kParts]);
     }
   }
   // the first tile and the queries have arrived (K of the second tile may be on its way)
@@ -575,8 +639,12 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
 #pragma unroll
   for (int c = 0; c < DB; ++c) {
     const int r = 4 * hf + ((lane & 15) >> 2);
-    va[c] = lds0 + (uint32_t)(stage_of(w0) + Cfg::kKTileBytes + (sub + r) * Cfg::ROW +
-                              (((4 * c) ^ v_swizzle<D>(r % Cfg::RPW)) + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1));
+    if constexpr (FP8)
+      va[c] = lds0 + (uint32_t)(stage_of(w0) + Cfg::kKTileBytes + (sub + r) / Cfg::RPW * Cfg::VG + r % Cfg::RPW * Cfg::ROW +
+                                ((4 * c + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_swizzle<D, true>(r % Cfg::RPW)) * 16 + 8 * (lane & 1));
+    else
+      va[c] = lds0 + (uint32_t)(stage_of(w0) + Cfg::kKTileBytes + (sub + r) * Cfg::ROW +
+                                (((4 * c) ^ v_swizzle<D>(r % Cfg::RPW)) + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1));
   }
   // (the places move between the two stages by one addition a tile each)
   auto move_k = [&](int t) __attribute__((always_inline)) {   // from tile t to tile t + 1
@@ -622,9 +690,9 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
         qk_step(sn, i);
         __builtin_amdgcn_sched_barrier(0);
       }
-      const tr_ptr vp_c = (tr_ptr)(uintptr_t)va[i % DB] + (32 * u + 16 * (i / DB)) * Cfg::ROW / 8;
+      const tr_ptr vp_c = (tr_ptr)(uintptr_t)va[i % DB] + (32 * u + 16 * (i / DB)) / Cfg::RPW * Cfg::VG / 8;
       vop[i][0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(vp_c);
-      vop[i][1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(vp_c + Cfg::ROW);
+      vop[i][1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(vp_c + 8 / Cfg::RPW * Cfg::VG / 8);
 #pragma unroll
       for (int e = E * i; e < E * i + E; ++e) sc[e] = __builtin_amdgcn_exp2f(XS ? fmaf(sc[e], qscale, neg_m) : sc[e]);
       if (i > 0) {
@@ -735,6 +803,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
       for (int i = 0; i < NI; ++i) asm volatile("" : "+v"(src[i]));
     }
     address(DMA ? j + 2 - set : j + 3 - set);
+    put_in(j + 2 - set);
     if constexpr (!PAGED) look_up(DMA ? j + 3 - set : j + 4 - set);
   };
   // (PAGED: the look-up is some twenty instructions, so in the loop it goes between products)
@@ -745,7 +814,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   auto stage_all = [&](int j, auto can_be_first) __attribute__((always_inline)) {
     if (DMA && ((decltype(can_be_first)::value && j < t_begin) || j + 2 - set >= t_end)) return;
 #pragma unroll
-    for (int k = 0; k < NLD; ++k) stage(j, k);
+    for (int i = 0; i < NST; ++i) stage(j, i);
   };
   auto nothing = [](int) __attribute__((always_inline)) {};
   int j = t_begin < t_end ? t_begin - 1 : t_end;
@@ -759,7 +828,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
     // chunks as products in it (blocks of four row blocks, d 128), of both its halves.
     auto staging = [&](int i) __attribute__((always_inline)) {
       if (i == 1) look_up_next(j, no{});
-      constexpr int first = NLD == KS ? 0 : KS, every = (2 * KS - first) / NLD;
+      constexpr int first = NST == KS ? 0 : KS, every = (2 * KS - first) / NST;
       if (i >= first && (i - first) % every == 0) stage(j, (i - first) / every);
     };
     begin_step(j, yes{});
@@ -814,7 +883,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
       if constexpr (!KSPLIT) {   // the second unit takes the first one's place
         s[0] = s[1];
 #pragma unroll
-        for (int c = 0; c < DB; ++c) va[c] += 32 * Cfg::ROW;   // (V's groups lie one behind the other)
+        for (int c = 0; c < DB; ++c) va[c] += 32 / Cfg::RPW * Cfg::VG;
       }
     }
     half_qk(no{}, s[0], s[KSPLIT ? 1 : 0], KSPLIT ? 1 : 0, nothing);
@@ -951,15 +1020,15 @@ __global__ __launch_bounds__(64 * kMergeWaves) void attn_bf16_merge(Dims dm, att
   const int w = wave / dims, nw = (int)(blockDim.x >> 6) / dims;   // of the dim block
   const int li = lane & 31, hf = lane >> 5;
   const int x = blockIdx.x, kv = blockIdx.y % dm.n_kv, b = blockIdx.y / dm.n_kv, c = (int)blockIdx.z * dims + wave % dims;
-  int C;
-  if constexpr (SRC == kContiguous) C = dm.chunk(b);
-  else C = chunk_of(dm, a, b);
-  int n_splits = a.n_splits;
+  int C, n_splits = a.n_splits;
   const float* rec;
   if constexpr (SRC == kContiguous) {
+    C = dm.chunk(b);
     if (x >= dm.g * ((C + 31) / 32)) return;   // block-uniform
     rec = a.part + ((size_t)blockIdx.y * gridDim.x + x) * a.n_splits * REC;
   } else {
+    const ListShare share = list_share(dm, a, kv, 0, b);
+    C = share.seq.C;
     const int tok = x / dm.g * 32 + li;
     if (w == 0 && tok >= C && tok < dm.C) {   // rows past the sequence's chunk
       const int h = kv * dm.g + x % dm.g;
@@ -969,7 +1038,6 @@ __global__ __launch_bounds__(64 * kMergeWaves) void attn_bf16_merge(Dims dm, att
       if (a.lse != nullptr && hf == 0 && c == 0) a.lse[(size_t)(b * dm.n_q + h) * dm.C + tok] = -INFINITY;
     }
     if (x >= dm.g * ((C + 31) / 32)) return;   // block-uniform
-    const ListShare share = list_share(dm, a, kv, 0, b);
     n_splits = share.n_splits;
     rec = a.part + ((size_t)kv * a.records + share.record + (size_t)x * n_splits) * REC;
   }
@@ -1085,9 +1153,11 @@ static hipError_t launch_variant(const Dims& dm, const attn_args<SRC>& a, hipStr
     // The plan's blocks, shared out by the kernels.  Their records: at most min(per_block, nrb) of a block, and nrb of a sequence and share.
     // The first bound is kept within kMaxRecords, and every group of row blocks has a block all the same: a plan has heads * nrb * splits
     // within it, two splits at least, and groups, filled up, are less than twice nrb; or (attn_plan, the first line) the groups fit a round of blocks of eight.
-    aa.per_block = 2 * Cfg::HW;
-    aa.tile_keys = Cfg::KT;
-    const int of_block = aa.per_block < nrb ? aa.per_block : nrb;
+    constexpr int per_block = 2 * Cfg::HW;
+    aa.block_shift = SPLIT ? 2 : 3;
+    aa.tile_shift = SPLIT ? 7 : 6;
+    static_assert(1 << (SPLIT ? 2 : 3) == per_block && 1 << (SPLIT ? 7 : 6) == Cfg::KT, "");
+    const int of_block = per_block < nrb ? per_block : nrb;
     // (a plan of one round leaves out what would be less than one more share for every group: unequal lists can use it)
     const long long planned = (long long)grid.y * dm.b, one_more = planned + planned / a.n_splits - 1, round = kComputeUnits / dm.n_kv,
                     room = kMaxRecords / (dm.n_kv * of_block);

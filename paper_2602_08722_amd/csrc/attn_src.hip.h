@@ -13,8 +13,9 @@ constexpr int kContiguous = 0, kRawPages = 1, kFp8Pages = 2;
 struct PagedAttnArgs : AttnArgs {   // (n_cache: as in AttnArgs)
   const int32_t *kv_lens = nullptr, *chunk_lens = nullptr;
   Pages pg = {};
-  // set by the launcher of the bf16 kernel where lists are shared: blocks of a KV head and their records; row blocks of a block, keys of a tile
-  int slots = 0, records = 0, per_block = 1, tile_keys = 1;
+  // set by the launcher of the bf16 kernel where lists are shared: blocks of a KV head and their records; row blocks of a block and keys of a
+  // tile, as powers of two
+  int slots = 0, records = 0, block_shift = 0, tile_shift = 0;
 };
 inline PagedAttnArgs paged_attn_args(const PagedArgs& p, float* part) {
   PagedAttnArgs a;
