@@ -315,15 +315,16 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   // elements, two slots of a row; two groups).
   // Source rows of a tile are looked up a step ahead of the loads that use them, so the dependent index -> row fetch of the gather
   // never sits on the critical path.  At d 128 the 16 lanes that carry a row look up NLD rows between them, one each, and take
-  // them from each other where they are used: one register instead of NLD.  (FP8: every four lanes.)
-  constexpr bool kShare = CG == 16 || FP8;
+  // them from each other where they are used: one register instead of NLD.  (PAGED, whose look-ups are longer, at d 64
+  // too; every four lanes there, and FP8.)
+  constexpr bool kShare = CG == 16 || PAGED, kQuads = FP8 || CG == 8;
   constexpr int NI = kShare ? 1 : NLD;
   const int r0 = tid / LPR;
   const uint32_t cg_src =
       (uint32_t)(FP8 ? tid % LPR : tid % CG ^ (set == 0 ? k_swizzle<D>(lane / CG) : v_swizzle<D>(lane / CG))) * 16u;
   auto of_row = [&](uint32_t v, int k) __attribute__((always_inline)) {   // kShare: what the lane that looks up row k has
-    if constexpr (!FP8) return row16_lane(v, k);
-    static_assert(!FP8 || NLD == 1 || NLD == 2 || NLD == 4, "rows of four lanes");
+    if constexpr (!kQuads) return row16_lane(v, k);
+    static_assert(!kQuads || NLD == 1 || NLD == 2 || NLD == 4, "rows of four lanes");
     if constexpr (NLD == 1) return v;
     switch (k) {
       case 0: return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x00, 0xF, 0xF, true);   // quad_perm
