@@ -85,7 +85,8 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 // Shares of key lists in a launch over pages, whose sequences differ in length and in tokens: the fewest tiles a block with which the
 // sequences' groups of 2^block_shift row blocks fit the `slots` blocks of a KV head, so that blocks take about equally long whatever the
 // lengths (an equal number of shares for each, 4 KV heads of 3, d 64, 101 - 333 tokens over 1237 - 9999 keys: 60 us).  More than 64
-// sequences: an equal number each.  Every wave works it out for itself, lane i for sequence i; the merge does the same.
+// sequences: an equal number each.  Every wave works it out for itself, lane i for sequence i; a sequence's first block leaves what the
+// merge needs of it.
 struct PagedSeq {
   int C, before, n;   // chunk tokens, cached tokens, list slots attended
 };
@@ -129,22 +130,18 @@ __device__ __forceinline__ ListShares list_shares(const Dims& dm, const PagedAtt
   const uint32_t blocks = groups * n, records = row_blocks * n;
   return {n, wave_incl_scan_u32(blocks) - blocks, blocks, wave_incl_scan_u32(records) - records, seq};
 }
-// The share of block `slot` (b < 0: of the block itself, else of sequence b's block 0).
-__device__ __forceinline__ ListShare list_share(const Dims& dm, const PagedAttnArgs& a, int kv, int slot, int b) {
+// The share of block `slot`.
+__device__ __forceinline__ ListShare list_share(const Dims& dm, const PagedAttnArgs& a, int kv, int slot) {
   if (dm.b > kWave) {
     const int each = a.slots / dm.b, groups = (dm.g * ((dm.C + 31) / 32) + (1 << a.block_shift) - 1) >> a.block_shift, n = each / groups;
-    if (b < 0) b = slot / each;
+    const int b = slot / each;
     return {b < dm.b && slot % each < groups * n ? b : -1, n, (uint32_t)(slot % each), (uint32_t)(b * dm.g * ((dm.C + 31) / 32) * n),
             paged_seq(dm, a, kv, min(b, dm.b - 1))};
   }
   const ListShares s = list_shares(dm, a, kv);
-  if (b < 0) {
-    const unsigned long long mine = __builtin_amdgcn_ballot_w64((uint32_t)slot >= s.first_block && (uint32_t)slot < s.first_block + s.blocks);
-    if (mine == 0) return {-1, 1, 0u, 0u, {}};
-    b = (int)__builtin_ctzll(mine);
-  } else {
-    slot = __builtin_amdgcn_readlane((int)s.first_block, b);
-  }
+  const unsigned long long mine = __builtin_amdgcn_ballot_w64((uint32_t)slot >= s.first_block && (uint32_t)slot < s.first_block + s.blocks);
+  if (mine == 0) return {-1, 1, 0u, 0u, {}};
+  const int b = (int)__builtin_ctzll(mine);
   return {b, __builtin_amdgcn_readlane((int)s.n_splits, b), (uint32_t)(slot - __builtin_amdgcn_readlane((int)s.first_block, b)),
           (uint32_t)__builtin_amdgcn_readlane((int)s.first_record, b),
           {__builtin_amdgcn_readlane(s.seq.C, b), __builtin_amdgcn_readlane(s.seq.before, b), __builtin_amdgcn_readlane(s.seq.n, b)}};
@@ -229,9 +226,10 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   [[maybe_unused]] ListShare share = {};
   [[maybe_unused]] PagedSeq seq = {};
   if constexpr (PAGED && KSPLIT) {
-    share = list_share(dm, a, kv, blockIdx.y, -1);
+    share = list_share(dm, a, kv, blockIdx.y);
     if (share.b < 0) return;   // block-uniform
     b = share.b;
+    if (share.block == 0 && threadIdx.x == 0) a.shares[kv * dm.b + b] = u32x2{(uint32_t)share.n_splits, share.record};
     seq = share.seq;
   } else if constexpr (PAGED) {
     if (dm.b > 1 && dm.b <= kWave) {   // (all that is asked of the lengths is fetched at once)
@@ -1028,8 +1026,8 @@ __global__ __launch_bounds__(64 * kMergeWaves) void attn_bf16_merge(Dims dm, att
     if (x >= dm.g * ((C + 31) / 32)) return;   // block-uniform
     rec = a.part + ((size_t)blockIdx.y * gridDim.x + x) * a.n_splits * REC;
   } else {
-    const ListShare share = list_share(dm, a, kv, 0, b);
-    C = share.seq.C;
+    const u32x2 share = a.shares[kv * dm.b + b];   // (a sequence without a token in this chunk has none, and uses none)
+    C = chunk_of(dm, a, b);
     const int tok = x / dm.g * 32 + li;
     if (w == 0 && tok >= C && tok < dm.C) {   // rows past the sequence's chunk
       const int h = kv * dm.g + x % dm.g;
@@ -1039,8 +1037,8 @@ __global__ __launch_bounds__(64 * kMergeWaves) void attn_bf16_merge(Dims dm, att
       if (a.lse != nullptr && hf == 0 && c == 0) a.lse[(size_t)(b * dm.n_q + h) * dm.C + tok] = -INFINITY;
     }
     if (x >= dm.g * ((C + 31) / 32)) return;   // block-uniform
-    n_splits = share.n_splits;
-    rec = a.part + ((size_t)kv * a.records + share.record + (size_t)x * n_splits) * REC;
+    n_splits = (int)share[0];
+    rec = a.part + ((size_t)kv * a.records + share[1] + (size_t)x * n_splits) * REC;
   }
   const int s0 = n_splits * w / nw, s1 = n_splits * (w + 1) / nw;
   float m = -INFINITY, l = 0.f;

@@ -14,7 +14,8 @@ struct PagedAttnArgs : AttnArgs {   // (n_cache: as in AttnArgs)
   const int32_t *kv_lens = nullptr, *chunk_lens = nullptr;
   Pages pg = {};
   // set by the launcher of the bf16 kernel where lists are shared: blocks of a KV head and their records; row blocks of a block and keys of a
-  // tile, as powers of two
+  // tile, as powers of two; number of shares and first record of every KV head's and sequence's list
+  u32x2* shares = nullptr;
   int slots = 0, records = 0, block_shift = 0, tile_shift = 0;
 };
 inline PagedAttnArgs paged_attn_args(const PagedArgs& p, float* part) {

@@ -146,7 +146,8 @@ struct PagedArgs {
   float* lse;                            // may be nullptr
   Pages pg;
 };
-hipError_t launch_paged_attn_bf16(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st);   // (partials as attn_bf16)
+size_t paged_attn_bf16_ws_floats(const Dims& dm);
+hipError_t launch_paged_attn_bf16(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st);
 // up to 32 query rows per KV head
 size_t paged_decode_ws_floats(const Dims& dm);
 hipError_t launch_paged_decode(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st);

@@ -102,7 +102,7 @@ static hipError_t launch_paged_f32(const Dims& dm, const PagedArgs& a, float* pa
 
 size_t paged_attn_ws_floats(const Dims& dm, int dtype) {
   if (dtype != QUOKA_BF16) return attn_f32_ws_floats(dm);
-  return attn_decode_applies(dm) ? paged_decode_ws_floats(dm) : attn_bf16_ws_floats(dm);
+  return attn_decode_applies(dm) ? paged_decode_ws_floats(dm) : paged_attn_bf16_ws_floats(dm);
 }
 
 hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float* part, hipStream_t st) {
