@@ -3,6 +3,7 @@
 
     python3 profile_summary.py trace <workload> <rocprofv3 output dir> <bench.py stdout file>
     python3 profile_summary.py cases <dir holding one rocprofv3 output dir per case, named like it>
+    python3 profile_summary.py operators <the same, of perf/operators.py's cases>
     python3 profile_summary.py traffic <workload> <dir holding one rocprofv3 output dir per pass>
     python3 profile_summary.py counters <title> <kernel substring> <rocprofv3 output dir> [<dir> ...]
 
@@ -84,14 +85,15 @@ def trace(workload, out_dir, bench_log):
     print("\n".join(out))
 
 
-def cases(base):
-    """Kernel traces of perf/cases.py's cases: every pass launches the same kernels, the first tenth is left out."""
-    out = ["# rocprofv3 kernel traces of the timed cases (perf/cases.py), one pass after another", "",
+def cases(base, module="cases"):
+    """Kernel traces of perf/cases.py's (perf/operators.py's) cases: every pass launches the same kernels, the first tenth is left out."""
+    own = "c.own = True; " if module == "operators" else ""
+    out = [f"# rocprofv3 kernel traces of the timed cases (perf/{module}.py), one pass after another", "",
            "Commands (run from /tmp with TMPDIR=/tmp, repository root = $R, one run per case):",
            "    rocprofv3 --kernel-trace --stats --output-format csv -d <base>/<case> -o kt -- python3 -c \"import sys, torch; "
-           "sys.path.insert(0, '$R'); from perf import cases as c; s = c.prepare(next(x for x in c.listed() if x['name'] == "
+           f"sys.path.insert(0, '$R'); from perf import {module} as c; {own}s = c.prepare(next(x for x in c.listed() if x['name'] == "
            "'<case>'), 1); [c.run(s) for _ in range(40)]; torch.cuda.synchronize()\"",
-           "    python3 $R/profile_summary.py cases <base>", "",
+           f"    python3 $R/profile_summary.py {module} <base>", "",
            "Launches per pass, and durations in us (the gaps between the launches of a pass are not in them)."]
     for d in sorted(x for x in os.listdir(base) if os.path.isdir(os.path.join(base, x))):
         rows = [r for r in csv.DictReader(open(_find(os.path.join(base, d), "*kernel_trace.csv"))) if _is_ours(r["Kernel_Name"])]
@@ -223,8 +225,8 @@ def main():
     mode = sys.argv[1]
     if mode == "trace" and len(sys.argv) == 5:
         trace(sys.argv[2], sys.argv[3], sys.argv[4])
-    elif mode == "cases" and len(sys.argv) == 3:
-        cases(sys.argv[2])
+    elif mode in ("cases", "operators") and len(sys.argv) == 3:
+        cases(sys.argv[2], mode)
     elif mode == "traffic" and len(sys.argv) == 4:
         traffic(sys.argv[2], sys.argv[3])
     elif mode == "counters" and len(sys.argv) >= 5:
