@@ -147,14 +147,14 @@ __device__ __forceinline__ ListShare list_share(const Dims& dm, const PagedAttnA
           {__builtin_amdgcn_readlane(s.seq.C, b), __builtin_amdgcn_readlane(s.seq.before, b), __builtin_amdgcn_readlane(s.seq.n, b)}};
 }
 
-template <int D>
-__device__ __forceinline__ int k_swizzle(int row) { return D == 128 ? row & 3 : (row >> 1) & 3; }
-// (FP8: where a lane stores two chunks of a row, one after the other, 16 lanes cover two rows, at d 64 four, which differ in bit 0)
+// FP8: a lane stores two chunks of a row, one after the other, and eight lanes of a store have to cover 128 bytes: their chunks, every other
+// one of a row, at d 64 of two, go to even and odd slots (d 128: by bit 3 of the chunk, d 64: by bit 0 of the row).
 template <int D, bool FP8 = false>
-__device__ __forceinline__ int v_swizzle(int row) {
-  const int x = D == 128 ? row & 3 : (row >> 1) & 1;
-  return FP8 ? 4 * x ^ (x & 1) : 4 * x;
-}
+__device__ __forceinline__ int k_swizzle(int row) { return D == 128 ? row & 3 : FP8 ? ((row >> 1) & 3) ^ (row & 1) : (row >> 1) & 3; }
+template <int D, bool FP8 = false>
+__device__ __forceinline__ int v_swizzle(int row) { return D == 128 ? 4 * (row & 3) : FP8 ? 4 * ((row >> 1) & 1) ^ (row & 1) : 4 * ((row >> 1) & 1); }
+template <int D, bool FP8>
+__device__ __forceinline__ int even_odd(int chunk) { return FP8 && D == 128 ? chunk >> 3 : 0; }
 
 template <int D>
 __device__ __forceinline__ int q_swizzle(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
@@ -359,7 +359,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   uint32_t dst_lane = 0;   // FP8: where the first of a load's chunks goes; the other's place is 16 bytes away
   if constexpr (FP8) {
     const int r = lane / LPR % Cfg::RPW;
-    dst_lane = dst_mine + (uint32_t)((w + lane / 32) * Cfg::KG + r * Cfg::ROW + (2 * (lane % LPR) ^ (set == 0 ? k_swizzle<D>(r) : v_swizzle<D, true>(r))) * 16);
+    dst_lane = dst_mine + (uint32_t)((w + lane / 32) * Cfg::KG + r * Cfg::ROW + (2 * (lane % LPR) ^ even_odd<D, true>(2 * (lane % LPR)) ^ (set == 0 ? k_swizzle<D, true>(r) : v_swizzle<D, true>(r))) * 16);
   }
   auto stage_of = [&](int t) __attribute__((always_inline)) { return (t & 1) * Cfg::kStageBytes; };
   const uint64_t pool_mine = pool + cg_src;   // PAGED
@@ -632,7 +632,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
 #pragma unroll
   for (int q = 0; q < 4; ++q)
     ka[q] = lds0 + (uint32_t)(stage_of(w0) + (sub + li) / Cfg::RPW * Cfg::KG + li % Cfg::RPW * Cfg::ROW +
-                              ((q ^ k_swizzle<D>(li % Cfg::RPW)) + KS * hf) * 16);
+                              ((q ^ k_swizzle<D, FP8>(li % Cfg::RPW) ^ even_odd<D, FP8>(KS * hf)) + KS * hf) * 16);
   // V: the lane's corner of the transposing reads of dim block c: key 4*hf + (lane%16)/4, dims 16*((lane/16)%2) + 4*(lane%4)
   uint32_t va[DB];
 #pragma unroll
@@ -640,7 +640,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
     const int r = 4 * hf + ((lane & 15) >> 2);
     if constexpr (FP8)
       va[c] = lds0 + (uint32_t)(stage_of(w0) + Cfg::kKTileBytes + (sub + r) / Cfg::RPW * Cfg::VG + r % Cfg::RPW * Cfg::ROW +
-                                ((4 * c + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_swizzle<D, true>(r % Cfg::RPW)) * 16 + 8 * (lane & 1));
+                                ((4 * c + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ even_odd<D, true>(4 * c) ^ v_swizzle<D, true>(r % Cfg::RPW)) * 16 + 8 * (lane & 1));
     else
       va[c] = lds0 + (uint32_t)(stage_of(w0) + Cfg::kKTileBytes + (sub + r) * Cfg::ROW +
                                 (((4 * c) ^ v_swizzle<D>(r % Cfg::RPW)) + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1));

@@ -34,15 +34,14 @@ struct PdCfg {
   static constexpr int NLD = kPdTile * LPR / 64;       // rows of a group of lanes
   static constexpr int LD = D + 8;         // K rows in LDS: 16 bytes of padding (conflict-free 16-byte reads)
   static constexpr int LDV = D + 32;       // V rows: 64 bytes apart modulo 256 (transposing reads)
-  // The first row of a group of lanes.  8-bit rows: 16 lanes store 16 bytes of LDS at a time, of two rows (D = 64: four), so neighbouring
-  // groups have rows that are 128 (64) bytes apart modulo 256; a lane's two pieces of K lie half a row apart (the contraction index may
-  // be permuted: Q follows), and of V side by side, the other way round in every other group of eight (D = 64: four) rows.
+  // The first row of a group of lanes.  8-bit rows: eight lanes of a store to LDS have to cover 128 bytes, and are one row (D = 64: two,
+  // whose places of K are 64 bytes apart modulo 128).  A lane's two pieces of K lie half a row apart (the contraction index may
+  // be permuted: Q follows), and of V side by side, the other way round in the upper half of a row (D = 64: in every other four rows).
   __device__ static __forceinline__ int first_row(int group) {
     if constexpr (!FP8) return group * NLD;
-    if constexpr (D == 128) return 8 * (group & 3) + 4 * (group >> 2);
+    if constexpr (D == 128) return group * NLD;
     return 4 * (group & 7) + 2 * (group >> 3);
   }
-  static constexpr int kTurn = D == 128 ? 8 : 4;
   static constexpr size_t kKBytes = (size_t)kPdTile * LD * 2;
   static constexpr size_t kWaveBytes = kKBytes + (size_t)kPdTile * LDV * 2;
   static constexpr int kRec = 32 * (D + 2);   // floats of a block's partial: O[32][D], m[32], l[32]
@@ -187,7 +186,7 @@ __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs
     };
     uint16_t* kt = reinterpret_cast<uint16_t*>(smem + (size_t)w * Cfg::kWaveBytes);
     uint16_t* vt = reinterpret_cast<uint16_t*>(smem + (size_t)w * Cfg::kWaveBytes + Cfg::kKBytes);
-    const int turn = (row0 / Cfg::kTurn) % 2 * 8;   // FP8: where a lane's first piece of V goes
+    const int turn = (D == 128 ? c / 4 : row0 / 4) % 2 * 8;   // FP8: where a lane's first piece of V goes
     auto to_lds = [&](const Rows& r) __attribute__((always_inline)) {
       const uint32_t both = FP8 ? r.k_ex | r.v_ex << 8 : 0u;
 #pragma unroll
@@ -280,9 +279,9 @@ __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs
       }
       l_run += psum;
       // ---- O^T += V^T P^T ----
-      // (FP8, rows in which pieces are the other way round: D = 128 rows 8 .. 15 of 16, D = 64 rows 4 .. 7 of 8)
+      // (FP8, where pieces are the other way round: D = 128 dims 64 .. 127, D = 64 rows 4 .. 7 of 8)
       const int v_at = (4 * hf + ((lane & 15) >> 2)) * LDV + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-      const tr_ptr vtr = (tr_ptr)(vt + (FP8 && D == 64 ? v_at ^ (8 * hf) : v_at)), vtr_hi = (tr_ptr)(vt + (!FP8 ? v_at : D == 64 ? v_at ^ (8 * hf) : v_at ^ 8));
+      const tr_ptr vtr = (tr_ptr)(vt + (FP8 && D == 64 ? v_at ^ (8 * hf) : v_at)), vtr_upper = (tr_ptr)(vt + (FP8 && D == 128 ? v_at ^ 8 : v_at));
 #pragma unroll
       for (int t2 = 0; t2 < 2; ++t2) {
         bf16x8 p;
@@ -291,8 +290,9 @@ __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
           const int e0 = 16 * t2 * LDV + db * 32;
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(vtr + e0 / 4);
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(vtr_hi + (e0 + 8 * LDV) / 4);
+          const tr_ptr at_v = (FP8 && D == 128 && db >= 2 ? vtr_upper : vtr) + e0 / 4;
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at_v);
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at_v + 8 * LDV / 4);
           const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
           o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), p, o[db], 0, 0, 0);
         }
