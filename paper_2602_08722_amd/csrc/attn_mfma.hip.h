@@ -84,7 +84,7 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 
 // Shares of key lists in a launch over pages, whose sequences differ in length and in tokens: the fewest tiles a block with which the
 // sequences' groups of 2^block_shift row blocks fit the `slots` blocks of a KV head, so that blocks take about equally long whatever the
-// lengths (an equal number of shares for each, 4 KV heads of 3, d 64, 101 - 333 tokens over 1237 - 9999 keys: 60 us).  More than 64
+// lengths (an equal number of shares for each, 4 KV heads of 3, d 64, 101 - 333 tokens over 1237 - 9999 keys: 60 us; now 47).  More than 64
 // sequences: an equal number each.  Every wave works it out for itself, lane i for sequence i; a sequence's first block leaves what the
 // merge needs of it.
 struct PagedSeq {
@@ -207,6 +207,10 @@ struct AttnCfg {
 // are blocks of eight at d 64 (1 - 1.5 % in launches of many rounds).  (As a run-time choice it cost all others 2 - 5 %.)
 // SRC = kRawPages, kFp8Pages: every row, the chunk's own among them, is found through the page table, and the row sums are those of the
 // probabilities before they are rounded (the sums are what `lse` shows; elsewhere they are of the rounded ones, in half the instructions).
+// What that costs, 32/8 heads, d 128, us: 1024 tokens over 8192 keys 139 from contiguous tensors with the scale in float32, 140 from 16-bit
+// pages, 155 from 8-bit ones (970 and 880 TFLOP/s of the visible products; of the 15 more, by leaving the staging out, all are loads, 32
+// conversions and 8 stores a tile and wave); 4096 over lists of 8192 595, 597 and 605 (1.14 PFLOP/s).  K stays in bfloat16, widened: products
+// of 8-bit operands drop what lies below 2^-13 of the largest product of a sum, so logits would not be sums in 32 bits (589 and 145 us).
 template <int D, bool SPLIT, bool XS, bool KSPLIT, bool WHOLE, int SRC = kContiguous>
 __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_args<SRC> a) {
   using Cfg = AttnCfg<D, SPLIT, SRC>;

@@ -5,7 +5,9 @@
 namespace quoka {
 
 // Short lists of a few tokens, as attn_f32_short: one wave per query row, lanes take 64 keys at a time for the logits and own D / 64
-// output dims each for the values.
+// output dims each for the values.  Bound by a chain of fetches (length, page, rows) and one step a key.  Measured (attn_f32 -> this kernel, rows as
+// they are): 32/8 heads, d 128, 1 token over 8 keys 9.2 -> 5.3 us, 8 tokens over 16 9.8 -> 8.3, 1 over 40, the longest, 9.6 -> 10.0; d 64, 1 over 16
+// 6.6 -> 6.0; 8-bit pages 10.1 -> 5.6, 10.8 -> 7.9, 7.3 -> 5.8.
 constexpr int kPsThreads = 256;
 
 template <bool FP8, int D>

@@ -3,7 +3,11 @@
 //
 // Bound by memory: every row is read once and written once.  A row is D / 8 lanes of eight elements, so the largest magnitude of a row,
 // which sets the power of two of an 8-bit row, is found inside one row of 16 (D = 128) or 8 (D = 64) lanes with cross-lane moves, in
-// registers; a thread has `U` rows of K and of V on the way at once.
+// registers; a thread has `U` rows on the way at once.  An 8-bit element is rounded once, to nearest even, by the conversion (the
+// multiplication by a power of two before it is exact); widening is exact.
+// Measured: 8 sequences of 2048 tokens, 8 heads of 128, bf16 to 8 bits 18.1 us (5.6 TB/s read and written), as they are 22.3 (6.0); 131072
+// rows of 8 heads of 128 back from 8 bits 79 us (5.1 TB/s), 3 sequences up to 19999 of 4 heads of 64 as they are, K and V, 15.2 (5.9).  One
+// token of 16 sequences 3 us, of which the launch and a chain of arguments, length, page and row are all.
 #include "pages.hip.h"
 
 namespace quoka {
@@ -155,6 +159,8 @@ __global__ __launch_bounds__(kPgThreads) void cache_read(Dims dm, Pages pg, cons
 template <typename T, bool FP8, int D>
 static hipError_t launch_write_d(const Dims& dm, const Pages& pg, const void* k, const void* v, const int32_t* kv_lens,
                                  const int32_t* chunk_lens, hipStream_t st) {
+  // (1, 2, 4: the first two launches above 18.2, 18.1, 17.7 and 22.5, 22.3, 20.9 us; one token of 16 sequences 3.0 with 2 and 3.4 with 4, 3
+  // sequences of 57 - 333 float32 rows of 3 heads of 64 as they are 3.4 and 4.1)
   constexpr int U = 2, ROWS = kPgThreads / (D / 8) * U;
   hipLaunchKernelGGL((cache_write<T, FP8, D, U>), dim3((dm.C + ROWS - 1) / ROWS, dm.b * dm.n_kv), dim3(kPgThreads), 0, st, dm, pg,
                      static_cast<const T*>(k), static_cast<const T*>(v), kv_lens, chunk_lens);
@@ -163,7 +169,7 @@ static hipError_t launch_write_d(const Dims& dm, const Pages& pg, const void* k,
 
 template <typename T, bool FP8, int D>
 static hipError_t launch_read_d(const Dims& dm, const Pages& pg, const int32_t* kv_lens, void* k, void* v, hipStream_t st) {
-  constexpr int U = 4, ROWS = kPgThreads / (D / 8) * U;
+  constexpr int U = 4, ROWS = kPgThreads / (D / 8) * U;   // (2, 4, 8: 87.2, 79.8, 80.5 us and 15.2, 15.4, 16.0)
   hipLaunchKernelGGL((cache_read<T, FP8, D, U>), dim3((dm.T_max + ROWS - 1) / ROWS, dm.b * dm.n_kv, k != nullptr && v != nullptr ? 2 : 1),
                      dim3(kPgThreads), 0, st, dm, pg, kv_lens, static_cast<T*>(k), static_cast<T*>(v));
   return hipGetLastError();
