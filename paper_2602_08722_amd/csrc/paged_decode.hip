@@ -14,8 +14,8 @@
 // 0.5 pages, 1 the first rows, then one or two tiles and the merge of the block's waves), the rest the second launch.
 //
 // The tiles of all sequences lie one behind the other, and every block of a KV head takes as many of them: the end of one
-// sequence, whole ones, the beginning of another.  A part of a sequence leaves a partial.  (With an equal number of blocks for each
-// sequence the 32 above took 262 us.)
+// sequence, whole ones, the beginning of another, or, where that costs nothing, a part of one (PdPlan).  A part of a sequence leaves a
+// partial.  (With an equal number of blocks for each sequence the 32 above took 262 us.)
 #include <type_traits>
 
 #include "pages.hip.h"
@@ -72,39 +72,59 @@ __device__ __forceinline__ uint32_t group_lane(uint32_t v, int i) {
 struct PdSeq {
   int n_list, n_before, C;   // entries (cached tokens) attended, cached tokens, chunk tokens
 };
-__device__ __forceinline__ PdSeq pd_seq(const Dims& dm, const PagedArgs& a, int b, int kv) {
+// `sparse`: whether there are lists, where that is known when it is compiled (a value less to keep).
+__device__ __forceinline__ PdSeq pd_seq(const Dims& dm, const PagedArgs& a, int b, int kv, bool sparse) {
   PdSeq s;
   s.C = a.chunk_lens == nullptr ? dm.C : max(min(a.chunk_lens[b], dm.C), 0);
   s.n_before = min(max(a.kv_lens[b], 0), dm.T_max);
-  s.n_list = a.k_idx == nullptr ? s.n_before : max(min(a.k_cnt[b * dm.n_kv + kv], dm.B_max), 0);
+  s.n_list = !sparse ? s.n_before : max(min(a.k_cnt[b * dm.n_kv + kv], dm.B_max), 0);
   return s;
 }
 
-// 64 sequences (from b0 on) in a line of tiles: lane i has those of sequence b0 + i and where they end (a sequence without a token in
-// this chunk has none).  Every wave works it out for itself.
+// 64 sequences from b0 on, one a lane, and their tiles (a sequence without a token in this chunk has none).
 struct PdLine {
   PdSeq seq;
-  uint32_t tiles, end;
+  uint32_t end;   // and where their room in the line of tiles ends (pd_place)
   int b0;
+  __device__ __forceinline__ uint32_t tiles() const { return seq.C > 0 ? (uint32_t)(seq.n_list + seq.C + kPdTile - 1) / kPdTile : 0u; }
 };
-__device__ __forceinline__ PdLine pd_line(const Dims& dm, const PagedArgs& a, int kv, int b0, uint32_t before) {
+__device__ __forceinline__ PdLine pd_line(const Dims& dm, const PagedArgs& a, int kv, int b0, bool sparse) {
   PdLine line;
   line.b0 = b0;
   const int b = b0 + (threadIdx.x & 63);
-  line.seq = dm.b == 1 ? pd_seq(dm, a, 0, kv) : pd_seq(dm, a, min(b, dm.b - 1), kv);   // (one sequence: scalar fetches)
-  line.tiles = b < dm.b && line.seq.C > 0 ? (uint32_t)(line.seq.n_list + line.seq.C + kPdTile - 1) / kPdTile : 0u;
-  line.end = before + (dm.b == 1 ? (uint32_t)__builtin_amdgcn_readfirstlane((int)line.tiles) : wave_incl_scan_u32(line.tiles));
+  line.seq = dm.b == 1 ? pd_seq(dm, a, 0, kv, sparse) : pd_seq(dm, a, min(b, dm.b - 1), kv, sparse);   // (one sequence: scalar fetches)
+  if (b >= dm.b) line.seq.C = 0;
   return line;
 }
 __device__ __forceinline__ uint32_t last_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); }
-__device__ __forceinline__ uint32_t pd_total(const Dims& dm, const PagedArgs& a, int kv, const PdLine& start) {   // start: b0 = 0
-  uint32_t total = last_lane(start.end);
-  for (int b0 = kWave; b0 < dm.b; b0 += kWave) total = last_lane(pd_line(dm, a, kv, b0, total).end);
-  return total;
+// (both below 2^23: the float quotient's integer part is the quotient's)
+__device__ __forceinline__ uint32_t blocks_of(uint32_t tiles, uint32_t quota) { return (uint32_t)((float)(tiles + quota - 1) / (float)quota); }
+
+// Tiles of a block, `quota`, and how many the line has.  All tiles over the blocks, at least one for each wave; or, where that takes no wave
+// another tile, a whole number of blocks for each sequence, since a block's second part is another chain of fetches (one token, 8-bit rows, us:
+// 16 sequences of 60 keys, 16/4 heads of 128 12.4 -> 10.9, 16 of 1100, 32/8 heads 17.5 -> 16.5, 8 of 3000 19.1 -> 18.4; with another tile a
+// wave 32 of 200 - 2000 31.6 -> 32.7).
+struct PdPlan {
+  uint32_t quota, total;
+  bool whole;
+};
+__device__ __forceinline__ PdPlan pd_plan(const Dims& dm, const PagedArgs& a, int kv, const PdLine& start, int n_slots, bool sparse) {   // start: b0 = 0
+  uint32_t total = dm.b == 1 ? (uint32_t)__builtin_amdgcn_readfirstlane((int)start.tiles()) : last_lane(wave_incl_scan_u32(start.tiles()));
+  for (int b0 = kWave; b0 < dm.b; b0 += kWave) total += last_lane(wave_incl_scan_u32(pd_line(dm, a, kv, b0, sparse).tiles()));
+  const uint32_t even = max((total + (uint32_t)n_slots - 1) / (uint32_t)n_slots, 1u);
+  if (dm.b > 1 && dm.b <= kWave && 2 * dm.b <= n_slots) {   // (with more sequences it is rarely so, and the question costs 2 - 3 %)
+    const uint32_t quota = (even + kPdWaves - 1) / kPdWaves * kPdWaves, blocks = last_lane(wave_incl_scan_u32(blocks_of(start.tiles(), quota)));
+    if (blocks <= (uint32_t)n_slots) return {quota, blocks * quota, true};
+  }
+  return {max(even, (uint32_t)kPdWaves), total, false};
 }
-// Tiles of a block: all of them over the blocks, at least one for each wave.
-__device__ __forceinline__ uint32_t pd_quota(uint32_t total, int n_slots) {
-  return max((total + (uint32_t)n_slots - 1) / (uint32_t)n_slots, (uint32_t)kPdWaves);
+// The room that a sequence's tiles take.
+__device__ __forceinline__ uint32_t pd_room(const PdPlan& plan, uint32_t tiles) {
+  return plan.whole ? blocks_of(tiles, plan.quota) * plan.quota : tiles;
+}
+__device__ __forceinline__ void pd_place(const Dims& dm, const PdPlan& plan, PdLine& line, uint32_t before) {
+  const uint32_t room = pd_room(plan, line.tiles());
+  line.end = before + (dm.b == 1 ? (uint32_t)__builtin_amdgcn_readfirstlane((int)room) : wave_incl_scan_u32(room));
 }
 
 // part: [n_kv, n_slots + batch, kRec] float32.  The partial of sequence b from block s is s + b: along the line of tiles either grows with every
@@ -120,25 +140,29 @@ __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 31, hf = lane >> 5;
   const int g = dm.g;
-  PdLine line = pd_line(dm, a, kv, 0, 0u);
-  const uint32_t total = pd_total(dm, a, kv, line), quota = pd_quota(total, n_slots);
-  uint32_t at = blockIdx.x * quota;   // (blocks x quota < total + a block's share: 32 bits)
-  const uint32_t at_end = min(at + quota, total);
+  PdLine line = pd_line(dm, a, kv, 0, LIST);
+  const PdPlan plan = pd_plan(dm, a, kv, line, n_slots, LIST);
+  pd_place(dm, plan, line, 0u);
+  uint32_t at = blockIdx.x * plan.quota;   // (blocks x quota < total + a block's share: 32 bits)
+  const uint32_t at_end = min(at + plan.quota, plan.total);
   while (at < at_end) {   // block-uniform: the sequences that the block has a part of
     unsigned long long hit;
-    while ((hit = __builtin_amdgcn_ballot_w64(at >= line.end - line.tiles && at < line.end)) == 0)   // (at < total: some sequence has it)
-      line = pd_line(dm, a, kv, line.b0 + kWave, last_lane(line.end));
+    while ((hit = __builtin_amdgcn_ballot_w64(at < line.end)) == 0) {   // (at < total: some sequence has it)
+      const uint32_t before = last_lane(line.end);
+      line = pd_line(dm, a, kv, line.b0 + kWave, LIST);
+      pd_place(dm, {0u, 0u, false}, line, before);   // (more than 64 sequences: not by whole blocks)
+    }
     const int of = (int)__builtin_ctzll(hit), b = line.b0 + of;
     PdSeq seq;
     seq.n_list = __builtin_amdgcn_readlane(line.seq.n_list, of);
     seq.n_before = __builtin_amdgcn_readlane(line.seq.n_before, of);
     seq.C = __builtin_amdgcn_readlane(line.seq.C, of);
-    const uint32_t end = (uint32_t)__builtin_amdgcn_readlane((int)line.end, of),
-                   first = end - (uint32_t)__builtin_amdgcn_readlane((int)line.tiles, of);
+    const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)(line.end - pd_room(plan, line.tiles())), of),
+                   end = first + (uint32_t)__builtin_amdgcn_readlane((int)line.tiles(), of);
     const int n_list = seq.n_list, n_keys = n_list + seq.C, n_rows = seq.C * g;   // n_rows <= 32, checked by the launcher
     const int t_end = (int)(min(at_end, end) - first);
     int t = (int)(at - first) + w;   // this wave's tiles: every fourth
-    at = first + t_end;
+    at = plan.whole ? at_end : first + t_end;
 
     const int32_t* table = pg.table + (size_t)b * pg.max_pages;
     const int32_t* list = LIST ? a.k_idx + (size_t)(b * dm.n_kv + kv) * dm.B_max : nullptr;
@@ -397,11 +421,16 @@ __global__ __launch_bounds__(kPdThreads) void paged_decode_merge(Dims dm, PagedA
     }
   };
   auto find = [&]() __attribute__((always_inline)) {   // the sequence's partials: n of them from s_first + b on
-    PdLine line = pd_line(dm, a, kv, 0, 0u);
-    const uint32_t quota = pd_quota(pd_total(dm, a, kv, line), n_slots);
-    while (line.b0 + kWave <= b) line = pd_line(dm, a, kv, line.b0 + kWave, last_lane(line.end));
-    const uint32_t end = (uint32_t)__builtin_amdgcn_readlane((int)line.end, b - line.b0),
-                   first = end - (uint32_t)__builtin_amdgcn_readlane((int)line.tiles, b - line.b0);
+    PdLine line = pd_line(dm, a, kv, 0, a.k_idx != nullptr);
+    const PdPlan plan = pd_plan(dm, a, kv, line, n_slots, a.k_idx != nullptr);
+    pd_place(dm, plan, line, 0u);
+    while (line.b0 + kWave <= b) {
+      const uint32_t before = last_lane(line.end);
+      line = pd_line(dm, a, kv, line.b0 + kWave, a.k_idx != nullptr);
+      pd_place(dm, {0u, 0u, false}, line, before);
+    }
+    const uint32_t quota = plan.quota, first = (uint32_t)__builtin_amdgcn_readlane((int)(line.end - pd_room(plan, line.tiles())), b - line.b0),
+                   end = first + (uint32_t)__builtin_amdgcn_readlane((int)line.tiles(), b - line.b0);
     s_first = (int)(first / quota);
     n = (int)((end - 1) / quota) - s_first + 1;
   };
@@ -485,7 +514,7 @@ hipError_t launch_paged_decode(const Dims& dm, bool fp8, const PagedArgs& a, flo
   const int n_slots = pd_slots(dm);
   const long long tiles = ((long long)attended_cap(dm, a.k_idx != nullptr) + dm.C + kPdTile - 1) / kPdTile;
   if (dm.b * tiles >= 1ll << 31) return hipErrorInvalidValue;   // (refused by the entry point)
-  const long long most = (dm.b * tiles + kPdWaves - 1) / kPdWaves;   // (blocks that short lists leave without work)
+  const long long most = dm.b * ((tiles + kPdWaves - 1) / kPdWaves);   // (blocks that short lists leave without work)
   auto launch = [&](auto d, auto eight_bit, auto is_list) -> hipError_t {
     constexpr int D = decltype(d)::value;
     constexpr bool FP8 = decltype(eight_bit)::value, LIST = decltype(is_list)::value;

@@ -286,6 +286,11 @@ ATTN_CASES = [
     dict(dtype="bf16", fp8=False, n_q=12, n_kv=4, d=128, page_len=64, C=333, lens=[6000, 700, 3100], chunks=[101, 333, 279]),
     dict(dtype="bf16", fp8=False, n_q=16, n_kv=8, d=64, page_len=64, C=1060, lens=[8000, 1500], chunks=[1060, 700]),
     dict(dtype="bf16", fp8=True, n_q=16, n_kv=8, d=128, page_len=64, C=1060, lens=[900, 7500]),
+    # single tokens: blocks with parts of several sequences; whole blocks for each
+    dict(dtype="bf16", fp8=True, n_q=32, n_kv=8, d=128, page_len=16, C=1, lens=[(61 * i) % 517 for i in range(40)]),
+    dict(dtype="bf16", fp8=False, n_q=16, n_kv=8, d=128, page_len=16, C=2, lens=[(97 * i) % 1301 for i in range(35)], chunks=[i % 3 for i in range(35)]),
+    dict(dtype="bf16", fp8=True, n_q=8, n_kv=8, d=64, page_len=32, C=4, lens=[(211 * i) % 2003 for i in range(30)]),
+    dict(dtype="bf16", fp8=False, n_q=8, n_kv=8, d=128, page_len=32, C=1, lens=[40, 0, 5000, 129, 127, 128]),
     # float32
     dict(dtype="f32", fp8=False, n_q=4, n_kv=2, d=64, page_len=16, C=1, lens=[0, 100, 16]),
     dict(dtype="f32", fp8=True, n_q=4, n_kv=2, d=128, page_len=32, C=1, lens=[2000]),
