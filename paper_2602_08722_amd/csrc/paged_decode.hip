@@ -72,7 +72,7 @@ __device__ __forceinline__ uint32_t group_lane(uint32_t v, int i) {
 struct PdSeq {
   int n_list, n_before, C;   // entries (cached tokens) attended, cached tokens, chunk tokens
 };
-// `sparse`: whether there are lists, where that is known when it is compiled (a value less to keep).
+// `sparse`: whether there are lists.
 __device__ __forceinline__ PdSeq pd_seq(const Dims& dm, const PagedArgs& a, int b, int kv, bool sparse) {
   PdSeq s;
   s.C = a.chunk_lens == nullptr ? dm.C : max(min(a.chunk_lens[b], dm.C), 0);
@@ -128,9 +128,10 @@ __device__ __forceinline__ void pd_place(const Dims& dm, const PdPlan& plan, PdL
 }
 
 // part: [n_kv, n_slots + batch, kRec] float32.  The partial of sequence b from block s is s + b: along the line of tiles either grows with every
-// part of a sequence.
+// part of a sequence.  parts: [n_kv, batch], the block of a sequence's first part and how many there are, for the merge.
 template <int D, bool FP8, bool LIST>
-__global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs a, float* __restrict__ part, int n_slots) {
+__global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs a, float* __restrict__ part, u32x2* __restrict__ parts,
+                                                              int n_slots) {
   using Cfg = PdCfg<D, FP8>;
   constexpr int KS = Cfg::KS, DB = Cfg::DB, LPR = Cfg::LPR, NLD = Cfg::NLD, LD = Cfg::LD, LDV = Cfg::LDV, LDO = Cfg::LDO;
   extern __shared__ __align__(16) unsigned char smem[];
@@ -161,6 +162,7 @@ __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs
                    end = first + (uint32_t)__builtin_amdgcn_readlane((int)line.tiles(), of);
     const int n_list = seq.n_list, n_keys = n_list + seq.C, n_rows = seq.C * g;   // n_rows <= 32, checked by the launcher
     const int t_end = (int)(min(at_end, end) - first);
+    if (at == first && tid == 0) parts[kv * dm.b + b] = u32x2{blockIdx.x, (end - 1) / plan.quota - blockIdx.x + 1};
     int t = (int)(at - first) + w;   // this wave's tiles: every fourth
     at = plan.whole ? at_end : first + t_end;
 
@@ -381,10 +383,11 @@ __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs
   }
 }
 
-// One block per (row, KV head, sequence).  Threads weigh a partial each, or two; thread (four dims c4, group sg) adds up the outputs of
+// Many partials a sequence: one block per (row, KV head, sequence).  Threads weigh a partial each, or two; thread (four dims c4, group sg) adds up the outputs of
 // every NG-th split, four of them on the way at a time, and the groups' sums meet in LDS, in a fixed order.
 template <int D>
-__global__ __launch_bounds__(kPdThreads) void paged_decode_merge(Dims dm, PagedArgs a, const float* __restrict__ part, int n_slots) {
+__global__ __launch_bounds__(kPdThreads) void paged_decode_merge(Dims dm, PagedArgs a, const float* __restrict__ part,
+                                                               const u32x2* __restrict__ parts, int n_slots) {
   constexpr int TPR = D / 4, NG = kPdThreads / TPR, RUN = 4;
   static_assert(kPdMaxSlots <= 2 * kPdThreads, "two partials a thread");
   constexpr size_t REC = PdCfg<D, false>::kRec;
@@ -420,30 +423,12 @@ __global__ __launch_bounds__(kPdThreads) void paged_decode_merge(Dims dm, PagedA
       l_s[u] = rec[32 + r];
     }
   };
-  auto find = [&]() __attribute__((always_inline)) {   // the sequence's partials: n of them from s_first + b on
-    PdLine line = pd_line(dm, a, kv, 0, a.k_idx != nullptr);
-    const PdPlan plan = pd_plan(dm, a, kv, line, n_slots, a.k_idx != nullptr);
-    pd_place(dm, plan, line, 0u);
-    while (line.b0 + kWave <= b) {
-      const uint32_t before = last_lane(line.end);
-      line = pd_line(dm, a, kv, line.b0 + kWave, a.k_idx != nullptr);
-      pd_place(dm, {0u, 0u, false}, line, before);
-    }
-    const uint32_t quota = plan.quota, first = (uint32_t)__builtin_amdgcn_readlane((int)(line.end - pd_room(plan, line.tiles())), b - line.b0),
-                   end = first + (uint32_t)__builtin_amdgcn_readlane((int)line.tiles(), b - line.b0);
-    s_first = (int)(first / quota);
-    n = (int)((end - 1) / quota) - s_first + 1;
-  };
-  if (dm.b == 1) {   // the partials begin at the first whatever the length is: they are requested beside it
-    load_weights();
-    load(sg);
-    __builtin_amdgcn_sched_barrier(0);
-    find();
-  } else {
-    find();
-    load_weights();
-    load(sg);
-  }
+  // the sequence's partials: n of them from s_first + b on
+  if (dm.b > 1) s_first = (int)parts[kv * dm.b + b][0];   // (of one sequence they begin at the first: requested beside their number)
+  load_weights();
+  load(sg);
+  __builtin_amdgcn_sched_barrier(0);
+  n = (int)parts[kv * dm.b + b][1];
 #pragma unroll
   for (int u = 0; u < 2; ++u)
     if (tid + u * kPdThreads >= n) {
@@ -505,13 +490,77 @@ __global__ __launch_bounds__(kPdThreads) void paged_decode_merge(Dims dm, PagedA
   }
 }
 
+// Few partials a sequence: a thread adds up four dims of a row over all of them, eight on the way at a time, and D / 4 threads are a row, so that
+// a block has eight rows (d 64: 16), which counts in large batches.  The two launches, the other's time first, us: 128 sequences of 500 keys,
+// 32/8 heads of 128 8.8 and 4.1, 32/4 of 64 10.6 and 3.6; 32 of 500 4.0 and 3.9, 5.0 and 3.7; one of 500 (five partials) 3.6 and 3.4, of
+// 2000 (16) 3.8 and 4.8; batches of 2 - 8 of 2000 (9 - 16) 3.7 - 4.2 and 4.0 - 4.8.
+template <int D>
+__global__ __launch_bounds__(kPdThreads) void paged_decode_merge_few(Dims dm, PagedArgs a, const float* __restrict__ part,
+                                                                   const u32x2* __restrict__ parts, int n_slots) {
+  constexpr int TPR = D / 4, RUN = 8;
+  constexpr size_t REC = PdCfg<D, false>::kRec;
+  const int r = (int)blockIdx.x * (kPdThreads / TPR) + (int)threadIdx.x / TPR, c4 = threadIdx.x % TPR, kv = blockIdx.y, b = blockIdx.z;
+  if (r >= dm.C * dm.g) return;
+  const int C = a.chunk_lens == nullptr ? dm.C : max(min(a.chunk_lens[b], dm.C), 0);
+  const u32x2 of = parts[kv * dm.b + b];   // (a sequence without a token in this chunk has none, and uses none)
+  const int tok = r / dm.g, h = kv * dm.g + r % dm.g;
+  uint16_t* orow = static_cast<uint16_t*>(a.out) + b * dm.os[0] + h * dm.os[1] + (size_t)tok * dm.os[2];
+  float* lse = a.lse != nullptr && c4 == 0 ? a.lse + (size_t)(b * dm.n_q + h) * dm.C + tok : nullptr;
+  if (tok >= C) {   // a row past the sequence's chunk
+    *reinterpret_cast<u32x2*>(orow + 4 * c4) = u32x2{0u, 0u};
+    if (lse != nullptr) *lse = -INFINITY;
+    return;
+  }
+  const int n = (int)of[1];
+  const float* rec = part + ((size_t)kv * (n_slots + dm.b) + of[0] + b) * REC;
+  float m = -INFINITY, l = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s0 = 0; s0 < n; s0 += RUN) {
+    float ms[RUN], ls[RUN];
+    float4 x[RUN];
+#pragma unroll
+    for (int u = 0; u < RUN; ++u) {
+      const float* p = rec + (size_t)min(s0 + u, n - 1) * REC;
+      ms[u] = p[32 * D + r];
+      ls[u] = p[32 * D + 32 + r];
+      x[u] = *reinterpret_cast<const float4*>(p + r * D + 4 * c4);
+    }
+    float m_new = m;
+#pragma unroll
+    for (int u = 0; u < RUN; ++u) m_new = fmaxf(m_new, s0 + u < n ? ms[u] : -INFINITY);
+    const float m_fin = m_new == -INFINITY ? 0.f : m_new, old = __builtin_amdgcn_exp2f(m - m_fin);
+    m = m_new;
+    l *= old;
+    acc.x *= old;
+    acc.y *= old;
+    acc.z *= old;
+    acc.w *= old;
+#pragma unroll
+    for (int u = 0; u < RUN; ++u) {
+      if (s0 + u < n) {
+        const float w = __builtin_amdgcn_exp2f(ms[u] - m_fin);
+        l += w * ls[u];
+        acc.x += w * x[u].x;
+        acc.y += w * x[u].y;
+        acc.z += w * x[u].z;
+        acc.w += w * x[u].w;
+      }
+    }
+  }
+  const bf16x2 lo = {(__bf16)(acc.x / l), (__bf16)(acc.y / l)}, hi = {(__bf16)(acc.z / l), (__bf16)(acc.w / l)};
+  *reinterpret_cast<u32x2*>(orow + 4 * c4) = u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+  if (lse != nullptr) *lse = (m + log2f(l)) * 0.6931471805599453f;
+}
+
 // ---------------------------------------------------------------------------------------------
 static int pd_slots(const Dims& dm) { return (kPdMaxSlots + dm.n_kv - 1) / dm.n_kv; }
 
-size_t paged_decode_ws_floats(const Dims& dm) { return (size_t)dm.n_kv * (pd_slots(dm) + dm.b) * 32 * (dm.d + 2); }
+static size_t pd_part_floats(const Dims& dm) { return (size_t)dm.n_kv * (pd_slots(dm) + dm.b) * 32 * (dm.d + 2); }
+size_t paged_decode_ws_floats(const Dims& dm) { return pd_part_floats(dm) + (size_t)2 * dm.n_kv * dm.b; }
 
 hipError_t launch_paged_decode(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st) {
   const int n_slots = pd_slots(dm);
+  u32x2* parts = reinterpret_cast<u32x2*>(part + pd_part_floats(dm));
   const long long tiles = ((long long)attended_cap(dm, a.k_idx != nullptr) + dm.C + kPdTile - 1) / kPdTile;
   if (dm.b * tiles >= 1ll << 31) return hipErrorInvalidValue;   // (refused by the entry point)
   const long long most = dm.b * ((tiles + kPdWaves - 1) / kPdWaves);   // (blocks that short lists leave without work)
@@ -523,8 +572,15 @@ hipError_t launch_paged_decode(const Dims& dm, bool fp8, const PagedArgs& a, flo
     const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&paged_decode<D, FP8, LIST>), lds, lds_done);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((paged_decode<D, FP8, LIST>), dim3(n_slots < most ? n_slots : (int)most, dm.n_kv), dim3(kPdThreads), lds, st, dm, a,
-                       part, n_slots);
-    hipLaunchKernelGGL((paged_decode_merge<D>), dim3(dm.C * dm.g, dm.n_kv, dm.b), dim3(kPdThreads), 0, st, dm, a, part, n_slots);
+                       part, parts, n_slots);
+    const int rows = dm.C * dm.g, of_block = kPdThreads / (D / 4);
+    // partials of a sequence: at most those of the longest list there can be; on the mean one more than its share of the blocks
+    const long long of_list = (tiles + kPdWaves - 1) / kPdWaves, of_batch = n_slots / dm.b + 1;
+    if ((of_list < of_batch ? of_list : of_batch) <= 8)
+      hipLaunchKernelGGL((paged_decode_merge_few<D>), dim3((rows + of_block - 1) / of_block, dm.n_kv, dm.b), dim3(kPdThreads), 0, st, dm, a, part,
+                         parts, n_slots);
+    else
+      hipLaunchKernelGGL((paged_decode_merge<D>), dim3(rows, dm.n_kv, dm.b), dim3(kPdThreads), 0, st, dm, a, part, parts, n_slots);
     return hipGetLastError();
   };
   using std::false_type;
