@@ -65,6 +65,7 @@ __device__ __forceinline__ FaRow fa_row(int r, int g) { return {r / g, r % g}; }
 // 16.7), and at d 64, with half the lines, 4 - 7 % throughout: those take the operands as they come.
 // SRC = kRawPages, kFp8Pages: every row is found through the page table, an entry of a list two units ahead of its page and the page a unit
 // ahead of the rows; offsets are numbers of 16 bytes.  8-bit rows are widened in registers, exactly, and never staged: a row is one line.
+// (8/2 heads, d 128, 512 tokens over 4096 keys: 89 us from tensors, 94 from pages, 92 from 8-bit ones.)
 template <int D, bool STAGED, int SRC = kContiguous>
 __global__ __launch_bounds__(kFaThreads, 2) void attn_f32(Dims dm, attn_args<SRC> a, float* __restrict__ part, int n_splits) {
   using Cfg = FaCfg<D, SRC>;
