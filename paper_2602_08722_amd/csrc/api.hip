@@ -601,11 +601,11 @@ static quoka_status check_pages(const quoka_shape& s, const quoka_pages* p, quok
     if (p->stride[i] < 0 || p->stride[i] % 16 != 0) return QUOKA_EINVAL;
   if (p->stride[2] < s.head_dim) return QUOKA_EINVAL;
   if ((long long)p->max_pages * p->page_len < s.max_kv_len) return QUOKA_EINVAL;
-  // kernels number rows, in 16 bytes, and scales with 32 bits
-  const unsigned __int128 last_row =
-      (unsigned __int128)(p->n_pages - 1) * (uint64_t)p->stride[0] + (unsigned __int128)(p->page_len - 1) * (uint64_t)p->stride[2];
+  // kernels number the 16-byte pieces of a head's rows, to the end of its last one, and scales with 32 bits
+  const unsigned __int128 rows_end =
+      (unsigned __int128)(p->n_pages - 1) * (uint64_t)p->stride[0] + (unsigned __int128)(p->page_len - 1) * (uint64_t)p->stride[2] + s.head_dim;
   const int es = p->format == QUOKA_PAGES_FP8 ? 1 : s.dtype == QUOKA_BF16 ? 2 : 4;
-  if (last_row * es / 16 >= (1ull << 32) || (unsigned __int128)p->n_pages * (uint64_t)p->page_len * (uint64_t)s.n_kv_heads > (1ull << 32))
+  if (rows_end * es > (1ull << 36) || (unsigned __int128)p->n_pages * (uint64_t)p->page_len * (uint64_t)s.n_kv_heads > (1ull << 32))
     return QUOKA_EUNSUPPORTED;
   out->k = p->k;
   out->v = p->v;

@@ -119,3 +119,28 @@ def test_the_binding_refuses_tensors_that_do_not_fit(monkeypatch):
             bare.read(*args)
     with pytest.raises(TypeError):
         pk.PagedBuffers(_cache(torch.float32), [1, 2], 60).read(out)
+
+
+def _pages_accepted(shape, pages):
+    """Whether the entry points take the pages: with a null pointer, which they look at last, the refusal is another one."""
+    lib = pk.load_library()
+    s, p = ctypes.byref(shape), ctypes.byref(pages)
+    codes = (lib.quoka_cache_write(s, p, None, AT, AT, None, None), lib.quoka_cache_read(s, p, None, AT, AT, None),
+             lib.quoka_paged_attn(s, p, None, AT, None, None, None, AT, None, WS, BIG, None))
+    assert codes in ((1,) * 3, (2,) * 3)
+    return codes[0] == 1
+
+
+@pytest.mark.parametrize("fmt,dtype,es", [("fp8", "bf16", 1), ("fp8", "f32", 1), ("raw", "bf16", 2), ("raw", "f32", 4)])
+@pytest.mark.parametrize("d,token", [(128, 144), (128, 128), (64, 80), (64, 208)])
+def test_the_last_row_of_a_head_ends_within_64_gib(fmt, dtype, es, d, token):
+    """Pages of 16 tokens; the page stride brings the end of the last row to 64 GiB exactly, then one step of 16 elements past it."""
+    shape = _shape(pk, head_dim=d, dtype=pk.QUOKA_BF16 if dtype == "bf16" else pk.QUOKA_F32)
+    limit = (64 << 30) // es
+    for n_pages in (2, 5, 65):
+        # (the page stride is a multiple of 16 elements: n_pages - 1 divides what is left of the limit, or the next smaller one is taken)
+        room = limit - d - 15 * token
+        stride = room // (n_pages - 1) // 16 * 16
+        how = dict(n_pages=n_pages, max_pages=63, format=pk.QUOKA_PAGES_FP8 if fmt == "fp8" else pk.QUOKA_PAGES_RAW)
+        assert _pages_accepted(shape, _pages(stride=(stride, 16 * token, token), **how))
+        assert not _pages_accepted(shape, _pages(stride=(stride + 16, 16 * token, token), **how))
