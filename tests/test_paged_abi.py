@@ -144,3 +144,17 @@ def test_the_last_row_of_a_head_ends_within_64_gib(fmt, dtype, es, d, token):
         how = dict(n_pages=n_pages, max_pages=63, format=pk.QUOKA_PAGES_FP8 if fmt == "fp8" else pk.QUOKA_PAGES_RAW)
         assert _pages_accepted(shape, _pages(stride=(stride, 16 * token, token), **how))
         assert not _pages_accepted(shape, _pages(stride=(stride + 16, 16 * token, token), **how))
+
+
+def test_the_number_of_scales_and_of_keys_is_limited():
+    # 2^32 scales: 2 KV heads, 65536 tokens a page, 2^15 pages (and rows that lie in the same places, for a span below 64 GiB)
+    flat = dict(stride=(128, 128, 128), page_len=65536, max_pages=1)
+    assert _pages_accepted(_shape(pk), _pages(n_pages=1 << 15, **flat))
+    assert not _pages_accepted(_shape(pk), _pages(n_pages=(1 << 15) + 1, **flat))
+    # batch * (max_kv_len + chunk_len + 32) below 2^36
+    lib = pk.load_library()
+    pages = ctypes.byref(_pages(n_pages=100, page_len=65536, max_pages=256))
+    for batch, chunk, code in ((4096, 63, 1), (4096, 64, 2), (4097, 63, 2), (4095, 64, 1)):
+        shape = _shape(pk, batch=batch, max_kv_len=(1 << 24) - 96, chunk_len=chunk, max_budget=0)
+        shape.kv_stride = (ctypes.c_int64 * 3)(0, 0, 128)
+        assert lib.quoka_paged_attn(ctypes.byref(shape), pages, AT, AT, None, None, None, AT, None, None, BIG, None) == code
