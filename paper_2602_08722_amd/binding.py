@@ -397,13 +397,30 @@ class PagedCache:
     """A pool of pages and the page table of a batch (the caller's tensors, kept alive here).
 
     k_pages / v_pages [n_pages, n_KV, page_len, d] (torch.float8_e4m3fn with scales, or the dtype of the queries), page_table
-    [b, max_pages] int32: the page of every sequence's tokens 0 .. page_len - 1, page_len .. 2 * page_len - 1 and so on.
+    [b, max_pages] int32: the page of every sequence's tokens 0 .. page_len - 1, page_len .. 2 * page_len - 1 and so on.  A longer
+    (or shorter) table of the same batch may take page_table's place; another pool is another PagedCache.
     """
 
     def __init__(self, k_pages, v_pages, page_table, k_scale=None, v_scale=None):
-        self.k_pages, self.v_pages, self.page_table = k_pages, v_pages, page_table
-        self.k_scale, self.v_scale = k_scale, v_scale
-        self.pages = make_pages(k_pages, v_pages, page_table, k_scale, v_scale)
+        self._pool, self._page_table = (k_pages, v_pages, k_scale, v_scale), page_table
+        self.pages = make_pages(k_pages, v_pages, page_table, k_scale, v_scale)   # (addresses: of the tensors that are kept here)
+
+    k_pages = property(lambda self: self._pool[0])
+    v_pages = property(lambda self: self._pool[1])
+    k_scale = property(lambda self: self._pool[2])
+    v_scale = property(lambda self: self._pool[3])
+
+    @property
+    def page_table(self):
+        return self._page_table
+
+    @page_table.setter
+    def page_table(self, page_table):
+        k_pages, v_pages, k_scale, v_scale = self._pool
+        pages = make_pages(k_pages, v_pages, page_table, k_scale, v_scale)
+        if page_table.shape[0] != self._page_table.shape[0]:
+            raise ValueError("a page table that takes another's place is of the same batch")
+        self._page_table, self.pages = page_table, pages
 
     @classmethod
     def allocate(cls, n_pages, page_len, n_kv, head_dim, page_table, dtype=torch.float8_e4m3fn):

@@ -556,3 +556,32 @@ def test_the_example_runs():
     spec.loader.exec_module(mod)
     # an 8-bit element is off by 2^-4 at most, 0.027 (root mean square) of itself: K's and V's errors add up to 0.04 or so
     assert mod.main(prompt=700, tokens=5, chunk=256) < 0.06
+
+
+@pytest.mark.parametrize("C", [1, 70])
+def test_a_page_table_that_takes_anothers_place_is_the_one_used(C):
+    """A sequence grows past its table: the longer one is given to the cache, and write, read and attention use it.  The old one is kept here
+    and names other pages by then, so that a call that still used it would show."""
+    pk = _pk()
+    case = dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=16, C=C, lens=[300])
+    rng, pool, q, chunks, lists = _attn_problem(case, 31)
+    short = pool.dev_table[:, :10].clone()   # 160 tokens
+    cache = pk.PagedCache(pool.k_pages, pool.v_pages, short, pool.k_scale, pool.v_scale)
+    tq = P.to_dev(q, "bf16", DEV)
+    # (what the pages hold: written again they stand for the same, though a row whose largest element was rounded up to a power of two's 448
+    # may get a smaller one)
+    new = [P.to_dev(x[0][300:].transpose(1, 0, 2)[None], "bf16", DEV) for x in (pool.k, pool.v)]
+    first = pk.PagedBuffers(cache, [100], 160, q=tq[:, :, :1], k_chunk=new[0][:, :, :1], v_chunk=new[1][:, :, :1])
+    first.read(*(torch.empty(1, 2, 160, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2)))
+    cache.page_table = pool.dev_table
+    short.fill_(0)
+    buf = pk.PagedBuffers(cache, [300], 300, q=tq, k_chunk=new[0], v_chunk=new[1])
+    buf.write()
+    buf.attn()
+    back = [torch.empty(1, 2, 300 + C, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    pk.PagedBuffers(cache, [300 + C], 300 + C).read(*back)
+    torch.cuda.synchronize()
+    for got, want in zip(back, (pool.k, pool.v)):
+        same = np.array_equal(got[0].float().cpu().numpy().astype(np.float64), want[0].transpose(1, 0, 2))
+        assert same
+    _check(case, buf, pool, q, chunks, lists)

@@ -158,3 +158,24 @@ def test_the_number_of_scales_and_of_keys_is_limited():
         shape = _shape(pk, batch=batch, max_kv_len=(1 << 24) - 96, chunk_len=chunk, max_budget=0)
         shape.kv_stride = (ctypes.c_int64 * 3)(0, 0, 128)
         assert lib.quoka_paged_attn(ctypes.byref(shape), pages, AT, AT, None, None, None, AT, None, None, BIG, None) == code
+
+
+def test_a_cache_describes_the_tensors_that_it_has():
+    """A page table may be replaced (sequences grow), and calls see the new one; one that does not fit is refused and changes
+    nothing; pools stay what they are."""
+    cache = _cache()
+    first = cache.page_table
+    assert cache.pages.page_table == first.data_ptr() and cache.pages.max_pages == 4
+    grown = torch.zeros((2, 9), dtype=torch.int32)
+    cache.page_table = grown
+    assert cache.page_table is grown
+    assert cache.pages.page_table == grown.data_ptr() and cache.pages.max_pages == 9
+    for bad in (grown[0], grown.long(), grown[:, ::2], torch.zeros((3, 9), dtype=torch.int32), torch.zeros((1, 9), dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            cache.page_table = bad
+        assert cache.page_table is grown and cache.pages.page_table == grown.data_ptr() and cache.pages.max_pages == 9
+    for name in ("k_pages", "v_pages", "k_scale", "v_scale"):
+        held = getattr(cache, name)
+        with pytest.raises(AttributeError):
+            setattr(cache, name, held.clone())
+        assert getattr(cache, name) is held and getattr(cache.pages, name[:1] if name.endswith("pages") else name) == held.data_ptr()
