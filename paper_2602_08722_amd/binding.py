@@ -129,6 +129,11 @@ def _strides3(t: torch.Tensor):
     return (ctypes.c_int64 * 3)(t.stride(0), t.stride(1), t.stride(2))
 
 
+def _ints(x, dev) -> torch.Tensor:
+    """Lengths or budgets as kernels read them: int32, on `dev`, dense (a tensor that is so already stays the caller's own)."""
+    return torch.as_tensor(x, dtype=torch.int32).to(dev).contiguous()
+
+
 QUOKA_SCORE_DOT, QUOKA_SCORE_MEAN, QUOKA_SELECT_UNIFORM, QUOKA_SCORE_QBAR_BF16, QUOKA_ATTN_SCALE_F32 = 1, 2, 4, 8, 16   # quoka.h
 
 
@@ -346,8 +351,8 @@ class ChunkBuffers:
         b, n_q, C, d = q.shape
         n_kv, t_max = k_cache.shape[1], k_cache.shape[2]
         self.q, self.k_cache, self.v_cache, self.k_chunk, self.v_chunk = q, k_cache, v_cache, k_chunk, v_chunk
-        self.kv_lens = torch.as_tensor(kv_lens, dtype=torch.int32).to(dev)
-        self.budgets = torch.as_tensor(budgets, dtype=torch.int32).to(dev)
+        self.kv_lens = _ints(kv_lens, dev)
+        self.budgets = _ints(budgets, dev)
         if max_budget is None:
             max_budget = min(int(max(budgets)), t_max) if len(budgets) else 0
         self.out = torch.empty_like(q)
@@ -454,8 +459,8 @@ class PagedBuffers:
         dev = pages.device
         n_kv, d = pages.shape[1], pages.shape[3]
         self.cache, self.q, self.k_chunk, self.v_chunk = cache, q, k_chunk, v_chunk
-        self.kv_lens = torch.as_tensor(kv_lens, dtype=torch.int32).to(dev)
-        self.chunk_lens = None if chunk_lens is None else torch.as_tensor(chunk_lens, dtype=torch.int32).to(dev)
+        self.kv_lens = _ints(kv_lens, dev)
+        self.chunk_lens = None if chunk_lens is None else _ints(chunk_lens, dev)
         b = self.kv_lens.numel()
         if cache.page_table.shape[0] != b or (self.chunk_lens is not None and self.chunk_lens.numel() != b):
             raise ValueError("page_table, kv_lens and chunk_lens are of one batch")
@@ -471,7 +476,7 @@ class PagedBuffers:
                 raise ValueError("q [b, n_Q, C, d], k_chunk and v_chunk [b, n_KV, C, d] share batch, chunk length, head size and dtype")
         if (k_chunk is None) != (v_chunk is None) or (k_chunk is not None and k_chunk.stride() != v_chunk.stride()):
             raise ValueError("k_chunk and v_chunk are given together and share strides")
-        self.budgets = None if budgets is None else torch.as_tensor(budgets, dtype=torch.int32).to(dev)
+        self.budgets = None if budgets is None else _ints(budgets, dev)
         if self.budgets is not None:
             if q is None or k_chunk is None or chunk_lens is not None or k_idx is not None:
                 raise ValueError("a selection of keys needs q, k_chunk and v_chunk, whole chunks and no lists of its own")

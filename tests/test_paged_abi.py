@@ -179,3 +179,24 @@ def test_a_cache_describes_the_tensors_that_it_has():
         with pytest.raises(AttributeError):
             setattr(cache, name, held.clone())
         assert getattr(cache, name) is held and getattr(cache.pages, name[:1] if name.endswith("pages") else name) == held.data_ptr()
+
+
+def test_lengths_and_budgets_may_be_views_of_any_strides():
+    """Kernels read dense arrays: what lies between the entries of a strided view must not be taken for lengths."""
+    cache = _cache()
+    q, kc = torch.zeros(2, 4, 3, 64, dtype=torch.bfloat16), torch.zeros(2, 2, 3, 64, dtype=torch.bfloat16)
+    pairs = torch.tensor([[5, 100], [6, 200]], dtype=torch.int32)
+    for view in (pairs[:, 0], pairs.t()[0], pairs[:, :1], pairs[:, 0].flip(0).flip(0)):
+        buf = pk.PagedBuffers(cache, view, 60, q=q, k_chunk=kc, v_chunk=kc, chunk_lens=view)
+        for t in (buf.kv_lens, buf.chunk_lens):
+            assert t.is_contiguous() and t.flatten().tolist() == [5, 6]
+        buf = pk.PagedBuffers(cache, view, 60, q=q, k_chunk=kc, v_chunk=kc, budgets=view)
+        assert buf.budgets.is_contiguous() and buf.budgets.flatten().tolist() == [5, 6] and buf.shape.max_budget == 6
+    alone = torch.tensor([3], dtype=torch.int32).expand(2)   # one length for all
+    buf = pk.PagedBuffers(cache, alone, 60, q=q)
+    assert buf.kv_lens.is_contiguous() and buf.kv_lens.tolist() == [3, 3]
+    dense = torch.tensor([5, 6], dtype=torch.int32)          # a program's own tensor stays the one that is read
+    assert pk.PagedBuffers(cache, dense, 60, q=q).kv_lens.data_ptr() == dense.data_ptr()
+    one = torch.zeros(2, 2, 60, 64, dtype=torch.bfloat16)
+    buf = pk.ChunkBuffers(q, one, one, kc, kc, pairs[:, 0], pairs[:, 0], 1)
+    assert buf.kv_lens.is_contiguous() and buf.budgets.is_contiguous() and buf.kv_lens.tolist() == buf.budgets.tolist() == [5, 6]
