@@ -480,6 +480,8 @@ class PagedBuffers:
         if self.budgets is not None:
             if q is None or k_chunk is None or chunk_lens is not None or k_idx is not None:
                 raise ValueError("a selection of keys needs q, k_chunk and v_chunk, whole chunks and no lists of its own")
+            if self.budgets.numel() != b:
+                raise ValueError("kv_lens and budgets are of one batch")
             max_budget = max(0, min(int(max(budgets)), self.max_kv_len))
             k_idx = torch.empty((b, n_kv, max(max_budget, 1)), dtype=torch.int32, device=dev)
             k_cnt = torch.empty((b, n_kv), dtype=torch.int32, device=dev)

@@ -200,3 +200,10 @@ def test_lengths_and_budgets_may_be_views_of_any_strides():
     one = torch.zeros(2, 2, 60, 64, dtype=torch.bfloat16)
     buf = pk.ChunkBuffers(q, one, one, kc, kc, pairs[:, 0], pairs[:, 0], 1)
     assert buf.kv_lens.is_contiguous() and buf.budgets.is_contiguous() and buf.kv_lens.tolist() == buf.budgets.tolist() == [5, 6]
+
+
+def test_budgets_of_another_batch_are_refused():
+    q, kc = torch.zeros(2, 4, 3, 64, dtype=torch.bfloat16), torch.zeros(2, 2, 3, 64, dtype=torch.bfloat16)
+    for budgets in ([3], [3, 3, 3]):
+        with pytest.raises(ValueError):
+            pk.PagedBuffers(_cache(), [1, 2], 60, q=q, k_chunk=kc, v_chunk=kc, budgets=budgets)
