@@ -178,6 +178,8 @@ def make_pages(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.T
         for t in (k_scale, v_scale):
             if t is None or t.dtype != torch.uint8 or t.shape != k_pages.shape[:3] or not t.is_contiguous():
                 raise ValueError("8-bit pages need dense uint8 scales [n_pages, n_KV, page_len]")
+    if any(t.device != k_pages.device for t in (v_pages, page_table) + ((k_scale, v_scale) if fp8 else ())):
+        raise ValueError("pages, scales and page table are on one device")
     p = QuokaPages()
     p.stride = _strides3(k_pages)
     p.n_pages, _, p.page_len, _ = k_pages.shape
@@ -464,6 +466,8 @@ class PagedBuffers:
         b = self.kv_lens.numel()
         if cache.page_table.shape[0] != b or (self.chunk_lens is not None and self.chunk_lens.numel() != b):
             raise ValueError("page_table, kv_lens and chunk_lens are of one batch")
+        if any(t is not None and t.device != dev for t in (q, k_chunk, v_chunk, k_idx, k_cnt)):
+            raise ValueError("queries, new keys and values and key lists are on the pages' device")
         self.max_kv_len = int(max_kv_len)
         new = q if q is not None else k_chunk
         dtype = new.dtype if new is not None else (torch.bfloat16 if pages.dtype == torch.float8_e4m3fn else pages.dtype)
@@ -522,19 +526,21 @@ class PagedBuffers:
     def read(self, k_out, v_out=None):
         """k_out, v_out [b, n_KV, max_kv_len, d], bfloat16 or float32; rows past a sequence's length stay as they are."""
         some = k_out if k_out is not None else v_out
-        layout = (some.dtype, some.shape, some.stride())
+        layout = (some.dtype, some.shape, some.stride(), some.device)
         if layout != self._read_layout:   # (the description of a layout, not of a tensor: any tensors of it may follow)
             s, pages = self.shape, self.cache.k_pages
             if pages.dtype not in (torch.float8_e4m3fn, some.dtype) or some.dtype not in (torch.float32, torch.bfloat16):
                 raise TypeError(f"pages of {pages.dtype} as {some.dtype}")
             if some.shape != (s.batch, s.n_kv_heads, self.max_kv_len, s.head_dim):
                 raise ValueError(f"expected [b, n_KV, max_kv_len, d], got {tuple(some.shape)}")
+            if some.device != pages.device:
+                raise ValueError("k_out and v_out are on the pages' device")
             r = QuokaShape.from_buffer_copy(s)
             r.dtype = QUOKA_BF16 if some.dtype == torch.bfloat16 else QUOKA_F32
             r.kv_stride = _strides3(some)
             self._read_shape, self._read_layout = r, layout
-        if k_out is not None and v_out is not None and (v_out.dtype, v_out.shape, v_out.stride()) != layout:
-            raise ValueError("k_out and v_out share shape, strides and dtype")
+        if k_out is not None and v_out is not None and (v_out.dtype, v_out.shape, v_out.stride(), v_out.device) != layout:
+            raise ValueError("k_out and v_out share shape, strides, dtype and device")
         if self.max_kv_len > 0:
             quoka_cache_read(self._read_shape, self.cache.pages, self.kv_lens, k_out, v_out)
 

@@ -207,3 +207,29 @@ def test_budgets_of_another_batch_are_refused():
     for budgets in ([3], [3, 3, 3]):
         with pytest.raises(ValueError):
             pk.PagedBuffers(_cache(), [1, 2], 60, q=q, k_chunk=kc, v_chunk=kc, budgets=budgets)
+
+
+def test_tensors_on_another_device_are_refused():
+    """An address is read on the GPU whatever device it is of: a list left on the host would fault there.  (Tensors without storage stand for
+    those of another device.)"""
+    table, scale = torch.zeros((2, 4), dtype=torch.int32), torch.zeros(10, 2, 16, dtype=torch.uint8)
+    pool = torch.zeros(10, 2, 16, 64, dtype=torch.bfloat16)
+    pool8 = pool.to(torch.float8_e4m3fn)
+    there = lambda x: x.to("meta")  # noqa: E731
+    for args in ((pool, there(pool), table), (pool, pool, there(table)), (pool8, pool8, table, scale, there(scale)),
+                 (pool8, pool8, table, there(scale), scale)):
+        with pytest.raises(ValueError):
+            pk.make_pages(*args)
+    cache = _cache()
+    with pytest.raises(ValueError):
+        cache.page_table = there(table)
+    q, kc = torch.zeros(2, 4, 3, 64, dtype=torch.bfloat16), torch.zeros(2, 2, 3, 64, dtype=torch.bfloat16)
+    idx, cnt = torch.zeros(2, 2, 5, dtype=torch.int32), torch.zeros(2, 2, dtype=torch.int32)
+    for how in (dict(q=there(q)), dict(q=q, k_chunk=there(kc), v_chunk=kc), dict(q=q, k_chunk=kc, v_chunk=there(kc)),
+                dict(q=q, k_idx=there(idx), k_cnt=cnt), dict(q=q, k_idx=idx, k_cnt=there(cnt))):
+        with pytest.raises(ValueError):
+            pk.PagedBuffers(cache, [1, 2], 60, **how)
+    out = torch.zeros(2, 2, 60, 64, dtype=torch.bfloat16)
+    for args in ((there(out),), (out, there(out)), (None, there(out))):
+        with pytest.raises(ValueError):
+            pk.PagedBuffers(cache, [1, 2], 60).read(*args)
