@@ -471,6 +471,8 @@ class PagedBuffers:
         self.max_kv_len = int(max_kv_len)
         new = q if q is not None else k_chunk
         dtype = new.dtype if new is not None else (torch.bfloat16 if pages.dtype == torch.float8_e4m3fn else pages.dtype)
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"unsupported dtype {dtype}")
         if pages.dtype not in (torch.float8_e4m3fn, dtype):
             raise TypeError(f"pages of {pages.dtype} with a chunk of {dtype}")
         C = 1 if new is None else new.shape[2]

@@ -233,3 +233,10 @@ def test_tensors_on_another_device_are_refused():
     for args in ((there(out),), (out, there(out)), (None, there(out))):
         with pytest.raises(ValueError):
             pk.PagedBuffers(cache, [1, 2], 60).read(*args)
+
+
+def test_chunks_of_other_dtypes_are_refused_as_such():
+    for dtype in (torch.float16, torch.float64):
+        for how in (dict(q=torch.zeros(2, 4, 3, 64, dtype=dtype)), dict(k_chunk=torch.zeros(2, 2, 3, 64, dtype=dtype), v_chunk=torch.zeros(2, 2, 3, 64, dtype=dtype))):
+            with pytest.raises(TypeError):
+                pk.PagedBuffers(_cache(), [1, 2], 60, **how)
