@@ -528,6 +528,8 @@ class PagedBuffers:
     def read(self, k_out, v_out=None):
         """k_out, v_out [b, n_KV, max_kv_len, d], bfloat16 or float32; rows past a sequence's length stay as they are."""
         some = k_out if k_out is not None else v_out
+        if some is None:
+            raise ValueError("nothing to read into")
         layout = (some.dtype, some.shape, some.stride(), some.device)
         if layout != self._read_layout:   # (the description of a layout, not of a tensor: any tensors of it may follow)
             s, pages = self.shape, self.cache.k_pages

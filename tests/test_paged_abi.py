@@ -240,3 +240,8 @@ def test_chunks_of_other_dtypes_are_refused_as_such():
         for how in (dict(q=torch.zeros(2, 4, 3, 64, dtype=dtype)), dict(k_chunk=torch.zeros(2, 2, 3, 64, dtype=dtype), v_chunk=torch.zeros(2, 2, 3, 64, dtype=dtype))):
             with pytest.raises(TypeError):
                 pk.PagedBuffers(_cache(), [1, 2], 60, **how)
+
+
+def test_a_read_into_nothing_is_refused():
+    with pytest.raises(ValueError):
+        pk.PagedBuffers(_cache(), [1, 2], 60).read(None)
