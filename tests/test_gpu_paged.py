@@ -585,3 +585,74 @@ def test_a_page_table_that_takes_anothers_place_is_the_one_used(C):
         same = np.array_equal(got[0].float().cpu().numpy().astype(np.float64), want[0].transpose(1, 0, 2))
         assert same
     _check(case, buf, pool, q, chunks, lists)
+
+
+# Float32 calls of a few tokens over short lists have a kernel of their own: at most 16 tokens, and the longest list and twice the tokens
+# together at most 26 (d 64) or 42 (d 128).
+SHORT_CASES = [
+    dict(n_q=8, n_kv=2, d=128, page_len=16, C=1, lens=[40, 0, 7]),
+    dict(n_q=8, n_kv=2, d=128, page_len=8, C=16, lens=[10, 0, 9], chunks=[16, 3, -2]),
+    dict(n_q=4, n_kv=4, d=128, page_len=1, C=5, lens=[32, 31], chunks=[0, 5]),
+    dict(n_q=6, n_kv=2, d=64, page_len=4, C=1, lens=[24, 1, 0, 23]),
+    dict(n_q=16, n_kv=1, d=64, page_len=16, C=5, lens=[16, 3], chunks=[5, 0]),
+    dict(n_q=2, n_kv=2, d=64, page_len=32, C=13, lens=[0], chunks=[12]),
+    dict(n_q=8, n_kv=2, d=128, page_len=16, C=8, lens=[300], budgets=[26]),
+    dict(n_q=12, n_kv=4, d=128, page_len=32, C=3, lens=[5000, 0, 20], budgets=[36, 4, 36], chunks=[2, 3, 1]),
+    dict(n_q=4, n_kv=2, d=64, page_len=16, C=2, lens=[100, 30], budgets=[22, 1]),
+    dict(n_q=4, n_kv=1, d=64, page_len=64, C=4, lens=[700, 90], budgets=[0, 18], chunks=[4, -1]),
+]
+
+
+@pytest.mark.parametrize("fp8", [True, False], ids=["fp8", "raw"])
+@pytest.mark.parametrize("layout", ["heads", "tokens"])
+@pytest.mark.parametrize("case", SHORT_CASES, ids=_ids)
+def test_short_float32_lists(case, layout, fp8):
+    case = dict(case, dtype="f32", fp8=fp8)
+    longest = max(case.get("budgets") or case["lens"])
+    assert case["C"] <= 16 and longest + 2 * case["C"] <= (26 if case["d"] == 64 else 42)
+    _, pool, q, chunks, lists = _attn_problem(case, 32, layout=layout, tail_entries=2 ** 31 - 1,
+                                              table_cols=-(-(max(case["lens"]) + case["C"]) // case["page_len"]) + 3)
+    buf = _buffers(_pk(), case, pool, q, lists, q_layout=layout)
+    buf.attn() if lists is None else buf.sparse_attn()
+    torch.cuda.synchronize()
+    _check(case, buf, pool, q, chunks, lists)
+
+
+@pytest.mark.parametrize("d,fp8", [(64, True), (64, False), (128, True), (128, False)])
+def test_short_float32_lists_stay_inside_the_pool_and_leave_nan_out(d, fp8):
+    """Entries of a list outside the cache and of a table outside the pool are cut to some row.  Keys and values of tokens that a row does not
+    see are not used, NaN or not."""
+    pk = _pk()
+    case = dict(dtype="f32", fp8=fp8, n_q=4, n_kv=2, d=d, page_len=4, C=3, lens=[20], budgets=[12])
+    _, pool, q, chunks, lists = _attn_problem(case, 33)
+    want = [P.attention(q[0, :, :2].astype(np.float64), pool.k[0][:22], pool.v[0][:22], 20, x) for x in (None, lists[0])]
+    # the last token's own row: the first two tokens do not see it
+    page, slot = int(pool.table[0, 22 // 4]), 22 % 4
+    if fp8:
+        for t in (pool.k_pages, pool.v_pages):
+            t.view(torch.uint8)[page, :, slot] = 0x7F
+    else:
+        for t in (pool.k_pages, pool.v_pages):
+            t[page, :, slot] = float("nan")
+    buf = _buffers(pk, case, pool, q, lists)
+    for run, (out, lse, weight) in zip((buf.attn, buf.sparse_attn), want):
+        got = run()[0, :, :2].cpu().numpy()
+        assert np.all(np.abs(got - out) <= 1e-4 * weight + 1e-7)
+        assert np.all(np.abs(buf.lse[0, :, :2].cpu().numpy() - lse) <= 1e-4)
+    # every row of the pool the same: whatever is taken in place of a wrong entry, the output is known
+    if fp8:
+        pool.k_pages.view(torch.uint8).fill_(0x30)   # 0.5
+        pool.v_pages.view(torch.uint8).fill_(0x28)   # 0.25
+        pool.k_scale.fill_(127)
+        pool.v_scale.fill_(127)
+    else:
+        pool.k_pages.fill_(0.5)
+        pool.v_pages.fill_(0.25)
+    buf.k_idx[0, 0, ::3] = 2 ** 31 - 1
+    buf.k_idx[0, 1, ::2] = -5
+    pool.dev_table[0, 1::2] = -9
+    pool.dev_table[0, 2::4] = 10 ** 9
+    for run in (buf.attn, buf.sparse_attn):
+        out = run()
+        torch.cuda.synchronize()
+        assert torch.all(torch.abs(out - 0.25) <= 1e-6)
