@@ -656,3 +656,73 @@ def test_short_float32_lists_stay_inside_the_pool_and_leave_nan_out(d, fp8):
         out = run()
         torch.cuda.synchronize()
         assert torch.all(torch.abs(out - 0.25) <= 1e-6)
+
+
+@pytest.mark.parametrize("C,fp8", [(1, True), (1, False), (50, True), (50, False)])
+def test_replays_read_and_attend_what_is_in_the_pages_by_then(C, fp8):
+    """A recorded step (write, attention, read of keys and values) whose lengths move on between replays: every replay reads back rows that the
+    one before has written, into buffers that hold something else."""
+    pk = _pk()
+    case = dict(dtype="bf16", fp8=fp8, n_q=8, n_kv=2, d=128, page_len=16, C=C, lens=[400, 90])
+    rng, pool, q, _, _ = _attn_problem(case, 34, table_cols=40, n_pages=90)
+    # pages for all tokens that are going to be written
+    table = torch.from_numpy(rng.permutation(90)[:80].reshape(2, 40).astype(np.int32)).to(DEV)
+    cache = pk.PagedCache(pool.k_pages, pool.v_pages, table, pool.k_scale, pool.v_scale)
+    whole = [torch.randn(2, 2, 640, 128, device=DEV).bfloat16() for _ in range(2)]
+    lens = torch.zeros(2, dtype=torch.int32, device=DEV)
+    pk.PagedBuffers(cache, lens, 0, k_chunk=whole[0][:, :, :400], v_chunk=whole[1][:, :, :400], chunk_lens=case["lens"]).write()
+    tq = P.to_dev(q, "bf16", DEV)
+    new = [torch.empty(2, 2, C, 128, device=DEV, dtype=torch.bfloat16) for _ in range(2)]
+    buf = pk.PagedBuffers(cache, case["lens"], 600, q=tq, k_chunk=new[0], v_chunk=new[1])
+    back = [torch.empty(2, 2, 600, 128, device=DEV, dtype=torch.bfloat16) for _ in range(2)]
+
+    def step():
+        buf.write()
+        buf.attn()
+        buf.read(*back)
+
+    def clear():
+        for t in back:
+            t.fill_(7.0)
+        buf.out.fill_(float("nan"))
+        buf.lse.fill_(float("nan"))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for t, x in zip(new, whole):
+        t.copy_(torch.stack([x[i, :, n:n + C] for i, n in enumerate(case["lens"])]))
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    torch.cuda.synchronize()
+    at = list(case["lens"])
+    for rep in range(4):
+        for t, x in zip(new, whole):
+            t.copy_(torch.stack([x[i, :, n:n + C] for i, n in enumerate(at)]))
+        tq.copy_(torch.randn_like(tq))
+        clear()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (buf.out, buf.lse, *back)]
+        for t, x in zip(back, whole):
+            for i, n in enumerate(at):
+                rows = x[i, :, :n].float()
+                if fp8:
+                    y, e = P.quantise(rows.cpu().numpy())
+                    rows = torch.from_numpy(np.ldexp(y, (e - 127)[..., None])).float().to(DEV)
+                same = torch.equal(t[i, :, :n].float(), rows)
+                assert same, f"replay {rep}, sequence {i}: rows"
+                assert bool((t[i, :, n:] == 7.0).all()), f"replay {rep}, sequence {i}: past the length"
+        float(torch.randn(1 << 16, device=DEV).sum())
+        clear()
+        step()
+        torch.cuda.synchronize()
+        for x, y in zip(got, (buf.out, buf.lse, *back)):
+            assert not bool(torch.isnan(x).any())
+            same = torch.equal(x, y)
+            assert same, f"replay {rep}"
+        buf.kv_lens += C
+        at = [n + C for n in at]
