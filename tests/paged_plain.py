@@ -116,3 +116,22 @@ def attention(q, k, v, n_before, lists=None):
         out[h], weight[h] = p @ vv, p @ np.abs(vv)
         lse[h] = (top + np.log(total))[:, 0]
     return out, lse, weight
+
+
+def attention_spread(q, k, v, n_before, lists=None):
+    """As `attention`: sqrt(sum_j P_j^2 V_j^2) of every element, what independent relative errors of the probabilities are multiplied
+    with, and the largest magnitude of a visible logit of every row."""
+    n_q, n, d = q.shape
+    spread, top = np.zeros((n_q, n, d)), np.zeros((n_q, n))
+    hidden = np.triu(np.ones((n, n), dtype=bool), 1)
+    for h in range(n_q):
+        kv = h // (n_q // k.shape[1])
+        old = np.arange(n_before) if lists is None else np.asarray(lists[kv], dtype=np.int64)
+        rows = np.concatenate([old, n_before + np.arange(n)])
+        z = q[h] @ k[rows, kv].T / np.sqrt(d)
+        z[:, len(old):][hidden] = -np.inf
+        p = np.exp(z - z.max(axis=1, keepdims=True))
+        p /= p.sum(axis=1, keepdims=True)
+        spread[h] = np.sqrt(p ** 2 @ v[rows, kv] ** 2)
+        top[h] = np.abs(np.where(np.isinf(z), 0.0, z)).max(axis=1)
+    return spread, top

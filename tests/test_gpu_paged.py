@@ -726,3 +726,97 @@ def test_replays_read_and_attend_what_is_in_the_pages_by_then(C, fp8):
             assert same, f"replay {rep}"
         buf.kv_lens += C
         at = [n + C for n in at]
+
+
+def _whole(rng, shape, low, high):
+    return rng.integers(low, high + 1, shape).astype(np.float64)
+
+
+LSE_CASES = [
+    dict(dtype="bf16", fp8=True, n_q=32, n_kv=8, d=128, page_len=16, C=1, lens=[7, 40, 1, 90]),
+    dict(dtype="bf16", fp8=False, n_q=8, n_kv=2, d=64, page_len=16, C=4, lens=[33, 0, 12]),
+    dict(dtype="bf16", fp8=False, n_q=8, n_kv=2, d=128, page_len=16, C=2, lens=[300], budgets=[37]),
+    dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=16, C=70, lens=[20, 5]),
+    dict(dtype="bf16", fp8=False, n_q=8, n_kv=2, d=64, page_len=16, C=70, lens=[20, 55], chunks=[70, 9]),
+    dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=64, page_len=16, C=70, lens=[600], budgets=[50]),
+    dict(dtype="bf16", fp8=False, n_q=32, n_kv=8, d=128, page_len=16, C=1100, lens=[9]),   # whole lists
+    dict(dtype="f32", fp8=False, n_q=4, n_kv=2, d=128, page_len=16, C=40, lens=[60]),
+    dict(dtype="f32", fp8=True, n_q=4, n_kv=2, d=64, page_len=16, C=2, lens=[90]),
+    dict(dtype="f32", fp8=True, n_q=4, n_kv=2, d=128, page_len=16, C=3, lens=[20]),
+]
+
+
+@pytest.mark.parametrize("case", LSE_CASES, ids=_ids)
+def test_row_sums_are_of_unrounded_probabilities(case):
+    """Queries and keys are small whole numbers, so that a product <q, k> is exact in float32 and what is left is the arithmetic behind it.  In
+    units of 2^-24, of a row with N visible keys and logits up to z: the scale in float32 3 z, the argument of the exponential 2 z, the
+    exponential 2, the sum N, the joining of partial sums 8, the logarithm 11, its sum with the reference point 11, the change of base 20: 5 z +
+    N + 52, here with 60.  Sums of probabilities that have been rounded to bfloat16 lie well outside."""
+    n_q, n_kv, d, C, lens, b = case["n_q"], case["n_kv"], case["d"], case["C"], case["lens"], len(case["lens"])
+    rng = np.random.default_rng(35)
+    chunks = [C] * b if case.get("chunks") is None else case["chunks"]
+    k, v = ([_whole(rng, (t + c, n_kv, d), -2, 2) for t, c in zip(lens, chunks)] for _ in range(2))
+    pool = P.Pool(rng, k, v, n_kv, d, case["page_len"], case["dtype"], case["fp8"])
+    q = _whole(rng, (b, n_q, C, d), -1, 1)
+    lists = None
+    if case.get("budgets") is not None:
+        lists = [[np.sort(rng.choice(t, size=n, replace=False)) for _ in range(n_kv)] for t, n in zip(lens, case["budgets"])]
+    buf = _buffers(_pk(), case, pool, q, lists)
+    buf.attn() if lists is None else buf.sparse_attn()
+    torch.cuda.synchronize()
+    got = buf.lse.cpu().numpy().astype(np.float64)
+    seen_by_rounded = False
+    for i, n in enumerate(chunks):
+        mine = None if lists is None else lists[i]
+        _, lse, _ = P.attention(q[i, :, :n], pool.k[i], pool.v[i], lens[i], mine)
+        _, top = P.attention_spread(q[i, :, :n], pool.k[i], pool.v[i], lens[i], mine)
+        keys = (lens[i] if lists is None else len(mine[0])) + 1 + np.arange(n)
+        tol = 2.0 ** -24 * (5 * top + keys + 60)
+        assert np.all(np.abs(got[i, :, :n] - lse) <= tol), np.max(np.abs(got[i, :, :n] - lse) / tol)
+        # what the sums of rounded probabilities would give
+        for h in range(n_q):
+            kv = h // (n_q // n_kv)
+            rows = np.concatenate([np.arange(lens[i]) if lists is None else mine[kv], lens[i] + np.arange(n)]).astype(int)
+            z = q[i, h, :n] @ pool.k[i][rows, kv].T / np.sqrt(d)
+            z[np.arange(len(rows))[None] >= keys[:, None]] = -np.inf
+            p = P.store(np.exp(z - z.max(axis=1, keepdims=True)), "bf16").astype(np.float64)
+            rounded = z.max(axis=1) + np.log(p.sum(axis=1))
+            seen_by_rounded |= bool(np.any(np.abs(rounded - lse[h]) > 4 * tol[h]))
+    assert seen_by_rounded
+
+
+NORM_CASES = [
+    dict(dtype="bf16", fp8=True, n_q=32, n_kv=8, d=128, page_len=64, C=1, lens=[6000]),
+    dict(dtype="bf16", fp8=False, n_q=32, n_kv=8, d=64, page_len=16, C=2, lens=[700, 2500, 301]),
+    dict(dtype="bf16", fp8=False, n_q=32, n_kv=4, d=128, page_len=16, C=1, lens=[9000, 400], budgets=[1100, 300]),
+    dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=64, C=100, lens=[3000]),
+    dict(dtype="bf16", fp8=False, n_q=12, n_kv=4, d=64, page_len=16, C=100, lens=[1237, 999], chunks=[100, 31]),
+    dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=64, page_len=64, C=70, lens=[9000], budgets=[5000]),
+    dict(dtype="bf16", fp8=True, n_q=32, n_kv=8, d=128, page_len=16, C=1100, lens=[300]),
+]
+
+
+@pytest.mark.parametrize("case", NORM_CASES, ids=_ids)
+def test_errors_are_those_of_independent_roundings(case):
+    """A rounding to bfloat16 is off by 2^-8 of the value at most and evenly spread, 2^-8 / sqrt(3) of it in the root mean square at most.  Every
+    probability and the output is rounded once, independently, so over hundreds of keys the errors' 2-norm is 2^-8 sqrt(sum P^2 V^2 + O^2) / sqrt(3)
+    at most, summed over all elements (1.05 of it here, for float32 arithmetic and chance).  Sixteen rows of V in each other's place lie outside."""
+    _, pool, q, chunks, lists = _attn_problem(case, 36)
+    buf = _buffers(_pk(), case, pool, q, lists)
+    buf.attn() if lists is None else buf.sparse_attn()
+    torch.cuda.synchronize()
+    got = buf.out.float().cpu().numpy().astype(np.float64)
+    for i, n in enumerate(chunks):
+        mine = None if lists is None else lists[i]
+        args = (q[i, :, :n].astype(np.float64), pool.k[i], pool.v[i], case["lens"][i], mine)
+        want, _, _ = P.attention(*args)
+        spread, _ = P.attention_spread(*args)
+        bound = 1.05 * 2.0 ** -8 * np.sqrt((np.sum(spread ** 2) + np.sum(want ** 2)) / 3)
+        off = np.linalg.norm(got[i, :, :n] - want)
+        assert off <= bound, off / bound
+        moved = pool.v[i].copy()
+        for kv in range(case["n_kv"]):
+            of = np.arange(16) if mine is None else mine[kv][:16]
+            moved[of, kv] = np.roll(moved[of, kv], 1, axis=0)
+        other, _, _ = P.attention(args[0], args[1], moved, *args[3:])
+        assert np.linalg.norm(got[i, :, :n] - other) > 2 * bound
