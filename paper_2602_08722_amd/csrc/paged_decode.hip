@@ -30,6 +30,7 @@ constexpr int kPdWaves = 4;
 constexpr int kPdThreads = 64 * kPdWaves;
 constexpr int kPdTile = 32;        // list slots a wave handles at a time
 constexpr int kPdMaxSlots = 512;   // blocks per KV head: two for every compute unit, which are resident together
+constexpr int kPdFew = 16;         // partials of a sequence that one thread adds up
 
 template <int D, bool FP8>
 struct PdCfg {
@@ -383,18 +384,18 @@ __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs
   }
 }
 
-// Many partials a sequence: one block per (row, KV head, sequence).  Threads weigh a partial each, or two; thread (four dims c4, group sg) adds up the outputs of
+// Many partials: a block merges row r of sequence b.  Threads weigh a partial each, or two; thread (four dims c4, group sg) adds up the outputs of
 // every NG-th split, four of them on the way at a time, and the groups' sums meet in LDS, in a fixed order.
 template <int D>
-__global__ __launch_bounds__(kPdThreads) void paged_decode_merge(Dims dm, PagedArgs a, const float* __restrict__ part,
-                                                               const u32x2* __restrict__ parts, int n_slots) {
+__device__ __forceinline__ void merge_row(const Dims& dm, const PagedArgs& a, const float* __restrict__ part, const u32x2* __restrict__ parts,
+                                          int n_slots, int r, int kv, int b) {
   constexpr int TPR = D / 4, NG = kPdThreads / TPR, RUN = 4;
   static_assert(kPdMaxSlots <= 2 * kPdThreads, "two partials a thread");
   constexpr size_t REC = PdCfg<D, false>::kRec;
   __shared__ float wgt[2 * kPdThreads];
   __shared__ float4 red[NG][TPR];
   __shared__ float wm[kPdWaves], wl[kPdWaves];
-  const int r = blockIdx.x, kv = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+  const int tid = threadIdx.x;
   const int C = a.chunk_lens == nullptr ? dm.C : max(min(a.chunk_lens[b], dm.C), 0);
   if (r >= C * dm.g) {   // block-uniform: a row past the sequence's chunk
     const int tok = r / dm.g, h = kv * dm.g + r % dm.g;
@@ -490,19 +491,64 @@ __global__ __launch_bounds__(kPdThreads) void paged_decode_merge(Dims dm, PagedA
   }
 }
 
+// The sequence of a KV head that is number `rank` of those with more than kPdFew partials, or -1.  Every wave finds it for itself, 256
+// sequences at a time.
+__device__ __forceinline__ int long_sequence(const Dims& dm, const PagedArgs& a, const u32x2* __restrict__ parts, int kv, int rank) {
+  constexpr int RUN = 4;
+  const int lane = threadIdx.x & 63;
+  for (int b0 = 0; b0 < dm.b; b0 += RUN * kWave) {
+    bool is_long[RUN];
+#pragma unroll
+    for (int u = 0; u < RUN; ++u) {
+      const int b = b0 + u * kWave + lane, at = min(b, dm.b - 1);
+      const int C = a.chunk_lens == nullptr ? dm.C : a.chunk_lens[at];   // (without a token the parts are not this call's)
+      is_long[u] = b < dm.b && C > 0 && (int)parts[kv * dm.b + at][1] > kPdFew;
+    }
+#pragma unroll
+    for (int u = 0; u < RUN; ++u) {
+      unsigned long long hits = __builtin_amdgcn_ballot_w64(is_long[u]);
+      const int n = (int)__builtin_popcountll(hits);
+      if (rank < n) {
+        for (; rank > 0; --rank) hits &= hits - 1;
+        return b0 + u * kWave + (int)__builtin_ctzll(hits);
+      }
+      rank -= n;
+    }
+  }
+  return -1;
+}
+
+// Many partials a sequence: one block per (row, KV head, sequence).
+template <int D>
+__global__ __launch_bounds__(kPdThreads) void paged_decode_merge(Dims dm, PagedArgs a, const float* __restrict__ part,
+                                                               const u32x2* __restrict__ parts, int n_slots) {
+  merge_row<D>(dm, a, part, parts, n_slots, blockIdx.x, blockIdx.y, blockIdx.z);
+}
+
 // Few partials a sequence: a thread adds up four dims of a row over all of them, eight on the way at a time, and D / 4 threads are a row, so that
 // a block has eight rows (d 64: 16), which counts in large batches.  The two launches, the other's time first, us: 128 sequences of 500 keys,
 // 32/8 heads of 128 8.8 and 4.1, 32/4 of 64 10.6 and 3.6; 32 of 500 4.0 and 3.9, 5.0 and 3.7; one of 500 (five partials) 3.6 and 3.4, of
 // 2000 (16) 3.8 and 4.8; batches of 2 - 8 of 2000 (9 - 16) 3.7 - 4.2 and 4.0 - 4.8.
+// Few on the mean, that is: a sequence far longer than the others has nearly all blocks' partials.  Those of more than kPdFew are left to the
+// launch's first `n_long` layers, where a block is a row as above (one sequence of 100000 keys among 73 of 100, whole calls, 16/1 heads of 128
+// 70.9 -> 24.9 us, 16/2 49.0 -> 26.8, 32/4 of 64 41.8 -> 29.4, 32/8 68.8 -> 63.8; 32 - 128 of 500 the same within 1 %, and so with kPdFew 8 or 32).
 template <int D>
 __global__ __launch_bounds__(kPdThreads) void paged_decode_merge_few(Dims dm, PagedArgs a, const float* __restrict__ part,
-                                                                   const u32x2* __restrict__ parts, int n_slots) {
+                                                                   const u32x2* __restrict__ parts, int n_slots, int n_long) {
   constexpr int TPR = D / 4, RUN = 8;
   constexpr size_t REC = PdCfg<D, false>::kRec;
-  const int r = (int)blockIdx.x * (kPdThreads / TPR) + (int)threadIdx.x / TPR, c4 = threadIdx.x % TPR, kv = blockIdx.y, b = blockIdx.z;
-  if (r >= dm.C * dm.g) return;
+  const int kv = blockIdx.y, rows = dm.C * dm.g;
+  if ((int)blockIdx.z < n_long) {
+    const int unit = (int)blockIdx.z * (int)gridDim.x + (int)blockIdx.x, rank = unit / rows;
+    const int b = long_sequence(dm, a, parts, kv, rank);
+    if (b >= 0) merge_row<D>(dm, a, part, parts, n_slots, unit - rank * rows, kv, b);   // block-uniform
+    return;
+  }
+  const int r = (int)blockIdx.x * (kPdThreads / TPR) + (int)threadIdx.x / TPR, c4 = threadIdx.x % TPR, b = (int)blockIdx.z - n_long;
+  if (r >= rows) return;
   const int C = a.chunk_lens == nullptr ? dm.C : max(min(a.chunk_lens[b], dm.C), 0);
   const u32x2 of = parts[kv * dm.b + b];   // (a sequence without a token in this chunk has none, and uses none)
+  if (n_long > 0 && C > 0 && (int)of[1] > kPdFew) return;
   const int tok = r / dm.g, h = kv * dm.g + r % dm.g;
   uint16_t* orow = static_cast<uint16_t*>(a.out) + b * dm.os[0] + h * dm.os[1] + (size_t)tok * dm.os[2];
   float* lse = a.lse != nullptr && c4 == 0 ? a.lse + (size_t)(b * dm.n_q + h) * dm.C + tok : nullptr;
@@ -576,11 +622,17 @@ hipError_t launch_paged_decode(const Dims& dm, bool fp8, const PagedArgs& a, flo
     const int rows = dm.C * dm.g, of_block = kPdThreads / (D / 4);
     // partials of a sequence: at most those of the longest list there can be; on the mean one more than its share of the blocks
     const long long of_list = (tiles + kPdWaves - 1) / kPdWaves, of_batch = n_slots / dm.b + 1;
-    if ((of_list < of_batch ? of_list : of_batch) <= 8)
-      hipLaunchKernelGGL((paged_decode_merge_few<D>), dim3((rows + of_block - 1) / of_block, dm.n_kv, dm.b), dim3(kPdThreads), 0, st, dm, a, part,
-                         parts, n_slots);
-    else
+    if ((of_list < of_batch ? of_list : of_batch) <= 8) {
+      // Sequences of more than kPdFew: each has kPdFew - 1 blocks or more of the n_slots to itself.  (A list's tiles may lie in one block more than
+      // they fill.)
+      const int blocks = (rows + of_block - 1) / of_block, most_long = of_list < kPdFew || n_slots <= kPdFew ? 0 : n_slots / (kPdFew - 1);
+      int n_long = ((most_long < dm.b ? most_long : dm.b) * rows + blocks - 1) / blocks;
+      if (n_long + dm.b > 65535) n_long = 0;   // (layers of a grid)
+      hipLaunchKernelGGL((paged_decode_merge_few<D>), dim3(blocks, dm.n_kv, n_long + dm.b), dim3(kPdThreads), 0, st, dm, a, part, parts,
+                         n_slots, n_long);
+    } else {
       hipLaunchKernelGGL((paged_decode_merge<D>), dim3(rows, dm.n_kv, dm.b), dim3(kPdThreads), 0, st, dm, a, part, parts, n_slots);
+    }
     return hipGetLastError();
   };
   using std::false_type;

@@ -820,3 +820,61 @@ def test_errors_are_those_of_independent_roundings(case):
             moved[of, kv] = np.roll(moved[of, kv], 1, axis=0)
         other, _, _ = P.attention(args[0], args[1], moved, *args[3:])
         assert np.linalg.norm(got[i, :, :n] - other) > 2 * bound
+
+
+def _skewed(n_kv, g, d, b, C, long_at, fp8=True, chunks=None, long=20000):
+    lens = [(37 * i) % 90 for i in range(b)]
+    for i in long_at:
+        lens[i] = long
+    return dict(dtype="bf16", fp8=fp8, n_q=n_kv * g, n_kv=n_kv, d=d, page_len=64, C=C, lens=lens, chunks=chunks)
+
+
+SKEWED_CASES = [
+    _skewed(1, 16, 128, 74, 1, [40]),
+    _skewed(1, 4, 64, 300, 2, [0, 299], fp8=False, long=9000),               # more sequences than are looked at together
+    _skewed(2, 8, 128, 40, 2, [3], chunks=[(i + 1) % 3 for i in range(40)], long=9000),     # the long one has one token of two
+    _skewed(2, 3, 128, 40, 4, [0, 7, 39], chunks=[4 - i % 5 for i in range(40)], long=9000),  # and some have none
+    _skewed(4, 4, 128, 36, 1, [35], fp8=False, long=9000),
+]
+
+
+@pytest.mark.parametrize("stale", [0x00, 0x7F, 0xFF])
+@pytest.mark.parametrize("case", SKEWED_CASES, ids=lambda c: f"{c['n_kv']}x{c['n_q']}-{len(c['lens'])}-C{c['C']}")
+def test_one_long_sequence_among_many_short_ones(case, stale):
+    """Nearly all partial results of a batch are one sequence's, or a few sequences'; whatever the workspace held before."""
+    _, pool, q, chunks, lists = _attn_problem(case, 37)
+    buf = _buffers(_pk(), case, pool, q, lists)
+    buf.workspace.fill_(stale)
+    buf.attn()
+    torch.cuda.synchronize()
+    _check(case, buf, pool, q, chunks, lists)
+
+
+def test_short_sequences_beside_a_long_one_cost_little():
+    """One sequence of 100000 tokens by itself and among 73 of 100: a call takes at most twice as long for them (1.3 times; 3.7 with a merge
+    that has one thread add up all partial results of a row's four dims)."""
+    pk = _pk()
+    cache = pk.PagedCache.allocate(1700, 64, 1, 128, torch.arange(1600, dtype=torch.int32, device=DEV)[None])
+    for t in (cache.k_pages, cache.v_pages):
+        t.view(torch.uint8).fill_(0x28)
+    cache.k_scale.fill_(127)
+    cache.v_scale.fill_(127)
+    took = []
+    for lens in ([100000], [100000] + [100] * 73):
+        table = cache.page_table.expand(len(lens), -1).contiguous()
+        buf = pk.PagedBuffers(pk.PagedCache(cache.k_pages, cache.v_pages, table, cache.k_scale, cache.v_scale), lens, 100000,
+                              q=torch.randn(len(lens), 16, 1, 128, device=DEV).bfloat16())
+        for _ in range(20):
+            buf.attn()
+        best = float("inf")
+        for _ in range(7):
+            start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            start.record()
+            for _ in range(100):
+                buf.attn()
+            end.record()
+            torch.cuda.synchronize()
+            best = min(best, start.elapsed_time(end) * 10)
+        took.append(best)
+    print("us a call:", took)
+    assert took[1] <= 2 * took[0], took
