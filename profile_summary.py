@@ -88,11 +88,12 @@ def trace(workload, out_dir, bench_log):
 def cases(base, module="cases"):
     """Kernel traces of perf/cases.py's (perf/operators.py's) cases: every pass launches the same kernels, the first tenth is left out."""
     own = "c.own = True; " if module == "operators" else ""
+    passes = 1000 if module == "operators" else 40   # (the clock settles over the first 10 - 20 ms of a busy card)
     out = [f"# rocprofv3 kernel traces of the timed cases (perf/{module}.py), one pass after another", "",
            "Commands (run from /tmp with TMPDIR=/tmp, repository root = $R, one run per case):",
            "    rocprofv3 --kernel-trace --stats --output-format csv -d <base>/<case> -o kt -- python3 -c \"import sys, torch; "
            f"sys.path.insert(0, '$R'); from perf import {module} as c; {own}s = c.prepare(next(x for x in c.listed() if x['name'] == "
-           "'<case>'), 1); [c.run(s) for _ in range(40)]; torch.cuda.synchronize()\"",
+           f"'<case>'), 1); [c.run(s) for _ in range({passes})]; torch.cuda.synchronize()\"",
            f"    python3 $R/profile_summary.py {module} <base>", "",
            "Launches per pass, and durations in us (the gaps between the launches of a pass are not in them)."]
     for d in sorted(x for x in os.listdir(base) if os.path.isdir(os.path.join(base, x))):
