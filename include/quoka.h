@@ -267,7 +267,8 @@ quoka_status quoka_cache_read(const quoka_shape* shape, const quoka_pages* pages
  *   lse      optional [b, n_Q, C] float32: natural-log softmax normaliser
  * bf16: products on bf16 MFMA with float32 accumulation and softmax state; 8-bit rows are widened to bfloat16, which is exact; the
  *   softmax scale is applied to the float32 products (as with QUOKA_ATTN_SCALE_F32, which changes nothing here), so that P and
- *   the output are rounded once each and Q is not.   f32: all arithmetic in float32, 8-bit rows widened exactly.
+ *   the output are rounded once each and Q is not.  Sums are of P before it is rounded: lse is that of the float32 logits, and the
+ *   weights of an output, rounded ones over such a sum, add up to 1 within the roundings.   f32: all arithmetic in float32, 8-bit rows widened exactly.
  * What is not finite: keys of tokens that a row does not see have no effect on it; values of later tokens of the same chunk may (they are
  *   multiplied by zero), and an infinite value of a visible token may come out as NaN.
  * The other score_flags, kv_stride and ck_stride do not matter here, but have to be valid. */

@@ -206,11 +206,12 @@ struct AttnCfg {
 // 10.9 -> 10.0).  Launches of fewer than 64 rows a KV head are the faster without (2 KV heads of 2, d 64, 17 tokens 6.4 / 6.6 us), and so
 // are blocks of eight at d 64 (1 - 1.5 % in launches of many rounds).  (As a run-time choice it cost all others 2 - 5 %.)
 // SRC = kRawPages, kFp8Pages: every row, the chunk's own among them, is found through the page table, and the row sums are those of the
-// probabilities before they are rounded (the sums are what `lse` shows; elsewhere they are of the rounded ones, in half the instructions).
-// What that costs, 32/8 heads, d 128, us: 1024 tokens over 8192 keys 139 from contiguous tensors with the scale in float32, 140 from 16-bit
-// pages, 155 from 8-bit ones (970 and 880 TFLOP/s of the visible products; of the 15 more, by leaving the staging out, all are loads, 32
-// conversions and 8 stores a tile and wave); 4096 over lists of 8192 595, 597 and 605 (1.14 PFLOP/s).  K stays in bfloat16, widened: products
-// of 8-bit operands drop what lies below 2^-13 of the largest product of a sum, so logits would not be sums in 32 bits (589 and 145 us).
+// probabilities before they are rounded: they are what `lse` shows, and the weights of an output, rounded ones over such a sum, add up to 1 only
+// within the roundings (elsewhere they are sums of the rounded ones, in half the instructions).  What that costs, 32/8 heads, d 128, us: 1024
+// tokens over 8192 keys 134 from contiguous tensors with the scale in float32, 137 from 16-bit pages, 141 from 8-bit ones (1.06 and 1.03
+// PFLOP/s of the visible products; what 8 bits cost, by leaving the staging out, are loads, 32 conversions and 8 stores a tile and wave); 4096
+// over lists of 8192 575, 595 and 597 (1.15 PFLOP/s).  K stays in bfloat16, widened: products of 8-bit operands drop what lies below 2^-13 of
+// the largest product of a sum, so logits would not be sums in 32 bits (3 to 5 % faster).
 template <int D, bool SPLIT, bool XS, bool KSPLIT, bool WHOLE, int SRC = kContiguous>
 __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_args<SRC> a) {
   using Cfg = AttnCfg<D, SPLIT, SRC>;

@@ -9,7 +9,7 @@
 // bytes a lane and whole rows by LPR neighbouring lanes (16, 8 or 4 of them); such a group fetches NLD neighbouring slots, one a load, so
 // each of its lanes looks up one slot's row and hands it to the others by a cross-lane move.  Rows are fetched one tile ahead, pages two,
 // entries three; 8-bit rows are widened on their way to LDS.
-// Measured: one token for 32 sequences of 1024 - 32768, 8-bit rows of 8 heads of 128 (1.15 GB), 205 us (5.6 TB/s); for 8 of 4096 - 65536,
+// Measured: one token for 32 sequences of 1024 - 32768, 8-bit rows of 8 heads of 128 (1.15 GB), 204 us (5.6 TB/s); for 8 of 4096 - 65536,
 // 16-bit rows (1.32 GB), 231 (5.7 TB/s).  One sequence of 8192 in 8 bits 12.8: 7 until the last partial has left (1.6 arguments and length,
 // 0.5 pages, 1 the first rows, then one or two tiles and the merge of the block's waves), the rest the second launch.
 //
@@ -302,7 +302,7 @@ __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs
           for (int v = 0; v < 16; ++v) o[db][v] *= alpha;
       }
       const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
-      float psum = 0.f;   // (of the probabilities before they are rounded: what lse shows)
+      float psum = 0.f;   // (of the probabilities before they are rounded: what lse shows; the weights add up to 1 within the roundings)
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], sl2, neg_m));

@@ -878,3 +878,35 @@ def test_short_sequences_beside_a_long_one_cost_little():
         took.append(best)
     print("us a call:", took)
     assert took[1] <= 2 * took[0], took
+
+
+@pytest.mark.parametrize("fp8", [True, False], ids=["fp8", "raw"])
+@pytest.mark.parametrize("case", [
+    dict(dtype="bf16", n_q=8, n_kv=2, d=128, page_len=16, C=3, lens=[70]),
+    dict(dtype="bf16", n_q=8, n_kv=2, d=64, page_len=16, C=3, lens=[70], budgets=[40]),
+    dict(dtype="bf16", n_q=8, n_kv=2, d=128, page_len=16, C=70, lens=[90]),
+    dict(dtype="bf16", n_q=8, n_kv=2, d=64, page_len=16, C=70, lens=[90], budgets=[30]),
+    dict(dtype="bf16", n_q=32, n_kv=8, d=128, page_len=16, C=1100, lens=[9]),
+    dict(dtype="f32", n_q=8, n_kv=2, d=128, page_len=16, C=40, lens=[90]),
+    dict(dtype="f32", n_q=8, n_kv=2, d=64, page_len=16, C=40, lens=[90], budgets=[30]),
+], ids=_ids)
+def test_keys_that_a_row_does_not_see_have_no_effect(case, fp8):
+    """The key of the chunk's last token is NaN: every row but that token's own is as it was."""
+    case = dict(case, fp8=fp8)
+    _, pool, q, chunks, lists = _attn_problem(case, 38)
+    buf = _buffers(_pk(), case, pool, q, lists)
+    run = buf.attn if lists is None else buf.sparse_attn
+    run()
+    before = buf.out.clone(), buf.lse.clone()
+    last = case["lens"][0] + case["C"] - 1
+    page, slot = int(pool.table[0, last // case["page_len"]]), last % case["page_len"]
+    if fp8:
+        pool.k_pages.view(torch.uint8)[page, :, slot] = 0x7F
+    else:
+        pool.k_pages[page, :, slot] = float("nan")
+    run()
+    torch.cuda.synchronize()
+    for x, y in zip(before, (buf.out, buf.lse)):
+        same = torch.equal(x[:, :, :-1], y[:, :, :-1])
+        assert same
+        assert not bool(torch.isnan(x).any()) and bool(torch.isnan(y[:, :, -1]).all())
