@@ -12,6 +12,8 @@
  *                                                         (Alg. 2, attention step; Eq. 2-3).
  * A dense chunked-prefill attention (Eq. 2) is provided as the baseline, and for caches kept in pages, in 8 bits or as they
  * are, the write of a chunk's rows, their way back and the attention over them (quoka_cache_write and what follows it).
+ * For generation from such caches: attention over an encoder's states (quoka_cross_attn), verification of drafted tokens
+ * (quoka_verify_draft), and the upkeep of the pages (quoka_pages_resize, quoka_pages_fork, quoka_cache_copy, quoka_cache_compact).
  *
  * Conventions that hold for every entry point
  *   - `shape` is a host pointer, read during the call, never retained.
@@ -276,6 +278,96 @@ quoka_status quoka_paged_workspace_bytes(const quoka_shape* shape, size_t* out_b
 quoka_status quoka_paged_attn(const quoka_shape* shape, const quoka_pages* pages, const void* q, const int32_t* kv_lens,
                               const int32_t* chunk_lens, const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse,
                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* Cross attention: attention of a chunk's queries over cached rows that are not the chunk's own -- an encoder's states, or a prefix that
+ * several sequences share -- written by quoka_cache_write like any others.  For q-head h (KV head kv) and chunk position i < chunk_lens[b]:
+ *   O[b,h,i] = sum_t softmax_t(<Q[b,h,i], K_t> / sqrt(d)) V_t over the positions t < kv_lens[b], without a mask.
+ * Rows i >= chunk_lens[b], and all rows of a sequence of kv_lens[b] == 0, are written as zeros, their lse as -infinity.
+ * Arguments, workspace (quoka_paged_workspace_bytes), limits and arithmetic as in quoka_paged_attn. */
+quoka_status quoka_cross_attn(const quoka_shape* shape, const quoka_pages* pages, const void* q, const int32_t* kv_lens,
+                              const int32_t* chunk_lens, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rows of one cache into the pages of another, or into other pages of the same pool, exactly as they are kept (scales included).  `src` and
+ * `dst` share format, shape.dtype, n_KV and d; page_len, strides and pool may differ.  No row that is written may be one that is read, and
+ * no two of them the same row of the pool; rows without a page are dropped, as by a write.  No workspace.
+ *
+ * quoka_cache_compact: the listed rows of every KV head, one behind the other (a cache that keeps what quoka_topk_keys chose).
+ *   k_idx, k_cnt  in  [b, n_KV, B_max], [b, n_KV]: the row at position k_idx[b,kv,j] of src goes to position j of dst, j < k_cnt[b,kv].
+ *                     Any order, repeated entries too; entries are cut to [0, max_kv_len) as by quoka_paged_attn
+ *   src holds max_kv_len positions or more, dst max_budget.
+ * quoka_cache_copy: rows first[b] <= t < lens[b], at most max_rows of them, of sequence parents[b] of src to the same positions of
+ * sequence b of dst (what quoka_pages_fork leaves to be copied, or whole sequences).
+ *   parents  in  [b]: sequences of src, of which there are n_parents; others: nothing is copied.  NULL: sequence b itself
+ *   first    in  [b], NULL: 0.   lens  in  [b]: negative numbers count as 0.   shape.max_kv_len does not matter here, but has to be valid */
+quoka_status quoka_cache_compact(const quoka_shape* shape, const quoka_pages* src, const quoka_pages* dst, const int32_t* k_idx,
+                                 const int32_t* k_cnt, void* stream);
+quoka_status quoka_cache_copy(const quoka_shape* shape, const quoka_pages* src, const quoka_pages* dst, const int32_t* parents,
+                              int32_t n_parents, const int32_t* first, const int32_t* lens, int32_t max_rows, void* stream);
+
+/* ---- Who holds the pages --------------------------------------------------------------------------------------------------------------
+ * The sequences of a batch hold the first held[b] entries of their rows of page_table; ref counts the holders of every page, over all
+ * batches and tables of the pool: 0, a free one.  (One table serves the caches of all layers.)  Start with ref 0, held 0, and any page_table;
+ * the two calls below keep all three, and write -1 into entries that a sequence gives back.  Held entries are pages of the pool; others (and a
+ * held that is not in [0, max_pages], which is cut to that) give a wrong count or none, never an access outside the arrays.
+ * Free pages are handed out lowest first, sequence after sequence, entry after entry, so that the same call has the same result every time.
+ * When there are not enough, those at the end get none: *lacking is how many.
+ * Calls over the same ref are to be ordered (one stream, or events).
+ * Limits: batch * max_pages < 2^31, n_pages <= 2^30, batch <= 65535. */
+typedef struct quoka_page_owners {
+  int32_t* ref;        /* device: [n_pages]                                       */
+  int32_t* page_table; /* device: [batch, max_pages]                              */
+  int32_t* held;       /* device: [batch]                                         */
+  int32_t n_pages;
+  int32_t page_len;    /* a power of two, at most 65536                           */
+  int32_t max_pages;
+  int32_t batch;
+} quoka_page_owners;
+quoka_status quoka_pages_workspace_bytes(const quoka_page_owners* owners, size_t* out_bytes);
+
+/* Every sequence holds the pages for its first lens[b] positions, and no others: pages behind them are given back (and may be handed out by
+ * the same call), lacking ones are handed out.  lens is cut to [0, max_pages * page_len].
+ *   lens  in  [b] int32;  lacking  out  one int32 */
+quoka_status quoka_pages_resize(const quoka_page_owners* owners, const int32_t* lens, int32_t* lacking, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/* Sequences that go on from others: child b, from sequence parents[b] of `from`, of which lens[parents[b]] tokens are cached (cut to the
+ * pages that it holds, and to the child's max_pages).  Whole pages are shared; for a last page that is not full the child gets a page of its
+ * own, whose rows quoka_cache_copy brings from the parent's (in every layer's cache).  So no page that is written to has two holders.
+ * Pages that the child held before are given back first.  A parent outside [0, from->batch): no pages, length 0.
+ * `from` and `children` share ref, n_pages and page_len, and have tables of their own.
+ *   lens        in   [from->batch] int32;  parents  in  [children->batch] int32, repeated ones too
+ *   first       out  [children->batch]: the first position of a row that is to be copied (the whole pages' end)
+ *   child_lens  out  [children->batch]: cached tokens; where the last page is lacking, those of the whole pages
+ *   workspace   of quoka_pages_workspace_bytes(children) */
+quoka_status quoka_pages_fork(const quoka_page_owners* from, const quoka_page_owners* children, const int32_t* parents, const int32_t* lens,
+                              int32_t* first, int32_t* child_lens, int32_t* lacking, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
+/* ---- Verification of drafted tokens ---------------------------------------------------------------------------------------------------
+ * Sequence b has drafted tokens x_0 .. x_(n-1), n = draft_lens[b] (cut to [0, n_draft]; NULL: n_draft), each from a distribution q_i; p_i is
+ * the target's distribution of token i, p_n that of the token after all of them.  Token i is accepted while
+ *   uniform[b,i] * q_i(x_i) < p_i(x_i),
+ * and a of them are until the first that is not.  The token after them, y, is drawn with uniform[b,n_draft] (cut to [0, 1)): the lowest v
+ * of positive weight w_v with w_0 + .. + w_v > uniform[b,n_draft] * (w_0 + w_1 + ..), where
+ *   w_v = max(p_a(v) - q_a(v), 0) for a < n, or p_a(v) should all of these be 0;   w_v = p_n(v) for a == n.
+ * So the tokens are distributed as the target's, whatever drafted them.  Distributions need not add up to 1; entries that are no positive
+ * number (NaN, infinities) weigh nothing and are not accepted, nor is a token outside [0, vocab).  All of it is in float64.
+ *   target      in   [b, n_draft + 1, vocab] (dtype), the last axis contiguous, others by strides (elements, may be 0)
+ *   draft       in   [b, n_draft, vocab] (dtype); NULL: q_i is 1 at x_i (tokens that were looked up)
+ *   tokens      in   [b, n_draft] int32;  uniform  in  [b, n_draft + 1] float32
+ *   n_accepted  out  [b] int32: a
+ *   tokens_out  out  [b, n_draft + 1] int32: x_0 .. x_(a-1), y (-1 if nothing weighs anything), and -1 behind it
+ * Limits: batch <= 65535, n_draft <= 65535, vocab <= 2^24. */
+typedef struct quoka_draft_shape {
+  int32_t batch, n_draft, vocab;
+  int32_t dtype;            /* quoka_dtype of target and draft */
+  int64_t target_stride[2]; /* sequence and token strides      */
+  int64_t draft_stride[2];
+} quoka_draft_shape;
+quoka_status quoka_verify_workspace_bytes(const quoka_draft_shape* shape, size_t* out_bytes);
+quoka_status quoka_verify_draft(const quoka_draft_shape* shape, const void* target, const void* draft, const int32_t* tokens,
+                                const float* uniform, const int32_t* draft_lens, int32_t* n_accepted, int32_t* tokens_out,
+                                void* workspace, size_t workspace_bytes, void* stream);
 
 /* quoka_topk_keys for callers that cannot allocate device memory and have no workspace to pass: code under HIP
  * graph capture, tight serving loops, harnesses that forbid hipMalloc.  Same arguments minus the workspace, same

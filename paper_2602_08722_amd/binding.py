@@ -27,6 +27,8 @@ EXPORTS = (
     "quoka_workspace_bytes", "quoka_select_queries", "quoka_score_keys", "quoka_topk_keys", "quoka_select_keys",
     "quoka_sparse_attn", "quoka_dense_attn", "quoka_chunk_attn", "quoka_prefill_workspace_bytes", "quoka_prefill_attn",
     "quoka_topk_keys_noalloc", "quoka_cache_write", "quoka_cache_read", "quoka_paged_workspace_bytes", "quoka_paged_attn",
+    "quoka_cross_attn", "quoka_cache_compact", "quoka_cache_copy", "quoka_pages_workspace_bytes", "quoka_pages_resize",
+    "quoka_pages_fork", "quoka_verify_workspace_bytes", "quoka_verify_draft",
     "quoka_probe_mfma", "quoka_probe_read", "quoka_probe_attn_mix", "quoka_probe_attn_plan", "quoka_status_string", "quoka_version",
 )
 _STATUS_EXPORTS = EXPORTS[:-2]   # everything that returns a quoka_status
@@ -61,6 +63,20 @@ class QuokaPages(ctypes.Structure):
     ]
 
 
+class QuokaPageOwners(ctypes.Structure):
+    _fields_ = [
+        ("ref", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("held", ctypes.c_void_p),
+        ("n_pages", ctypes.c_int32), ("page_len", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("batch", ctypes.c_int32),
+    ]
+
+
+class QuokaDraftShape(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("n_draft", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("target_stride", ctypes.c_int64 * 2), ("draft_stride", ctypes.c_int64 * 2),
+    ]
+
+
 def library_path() -> str:
     return os.path.join(os.path.dirname(os.path.abspath(__file__)), _LIB_NAME)
 
@@ -92,6 +108,15 @@ def load_library() -> ctypes.CDLL:
     lib.quoka_cache_read.argtypes = [SH, PG, I32P, P, P, P]
     lib.quoka_paged_workspace_bytes.argtypes = [SH, ctypes.POINTER(ctypes.c_size_t)]
     lib.quoka_paged_attn.argtypes = [SH, PG, P, I32P, I32P, I32P, I32P, P, F32P, P, SZ, P]
+    lib.quoka_cross_attn.argtypes = [SH, PG, P, I32P, I32P, P, F32P, P, SZ, P]
+    lib.quoka_cache_compact.argtypes = [SH, PG, PG, I32P, I32P, P]
+    lib.quoka_cache_copy.argtypes = [SH, PG, PG, I32P, ctypes.c_int32, I32P, I32P, ctypes.c_int32, P]
+    OW, DS = ctypes.POINTER(QuokaPageOwners), ctypes.POINTER(QuokaDraftShape)
+    lib.quoka_pages_workspace_bytes.argtypes = [OW, ctypes.POINTER(ctypes.c_size_t)]
+    lib.quoka_pages_resize.argtypes = [OW, I32P, I32P, P, SZ, P]
+    lib.quoka_pages_fork.argtypes = [OW, OW, I32P, I32P, I32P, I32P, I32P, P, SZ, P]
+    lib.quoka_verify_workspace_bytes.argtypes = [DS, ctypes.POINTER(ctypes.c_size_t)]
+    lib.quoka_verify_draft.argtypes = [DS, P, P, I32P, F32P, I32P, I32P, I32P, P, SZ, P]
     lib.quoka_probe_mfma.argtypes = [ctypes.c_int, ctypes.c_int, F32P, P]
     lib.quoka_probe_read.argtypes = [P, SZ, F32P, P]
     lib.quoka_probe_attn_mix.argtypes = [ctypes.c_int, ctypes.c_int, F32P, P]
@@ -309,6 +334,54 @@ def quoka_paged_attn(shape, pages, q, kv_lens, chunk_lens, k_idx, k_cnt, out, ls
         _ptr(lse), _ptr(workspace), workspace.numel(), _stream(stream)))
 
 
+def quoka_cross_attn(shape, pages, q, kv_lens, chunk_lens, out, lse, workspace, stream=None) -> None:
+    _check("quoka_cross_attn", load_library().quoka_cross_attn(
+        ctypes.byref(shape), ctypes.byref(pages), _ptr(q), _ptr(kv_lens), _ptr(chunk_lens), _ptr(out), _ptr(lse), _ptr(workspace),
+        workspace.numel(), _stream(stream)))
+
+
+def quoka_cache_compact(shape, src, dst, k_idx, k_cnt, stream=None) -> None:
+    _check("quoka_cache_compact", load_library().quoka_cache_compact(
+        ctypes.byref(shape), ctypes.byref(src), ctypes.byref(dst), _ptr(k_idx), _ptr(k_cnt), _stream(stream)))
+
+
+def quoka_cache_copy(shape, src, dst, parents, n_parents, first, lens, max_rows, stream=None) -> None:
+    _check("quoka_cache_copy", load_library().quoka_cache_copy(
+        ctypes.byref(shape), ctypes.byref(src), ctypes.byref(dst), _ptr(parents), n_parents, _ptr(first), _ptr(lens), max_rows,
+        _stream(stream)))
+
+
+def quoka_pages_workspace_bytes(owners: QuokaPageOwners) -> int:
+    n = ctypes.c_size_t(0)
+    _check("quoka_pages_workspace_bytes",
+           load_library().quoka_pages_workspace_bytes(ctypes.byref(owners), ctypes.byref(n)))
+    return int(n.value)
+
+
+def quoka_pages_resize(owners, lens, lacking, workspace, stream=None) -> None:
+    _check("quoka_pages_resize", load_library().quoka_pages_resize(
+        ctypes.byref(owners), _ptr(lens), _ptr(lacking), _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+def quoka_pages_fork(source, children, parents, lens, first, child_lens, lacking, workspace, stream=None) -> None:
+    _check("quoka_pages_fork", load_library().quoka_pages_fork(
+        ctypes.byref(source), ctypes.byref(children), _ptr(parents), _ptr(lens), _ptr(first), _ptr(child_lens), _ptr(lacking),
+        _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+def quoka_verify_workspace_bytes(shape: QuokaDraftShape) -> int:
+    n = ctypes.c_size_t(0)
+    _check("quoka_verify_workspace_bytes",
+           load_library().quoka_verify_workspace_bytes(ctypes.byref(shape), ctypes.byref(n)))
+    return int(n.value)
+
+
+def quoka_verify_draft(shape, target, draft, tokens, uniform, draft_lens, n_accepted, tokens_out, workspace, stream=None) -> None:
+    _check("quoka_verify_draft", load_library().quoka_verify_draft(
+        ctypes.byref(shape), _ptr(target), _ptr(draft), _ptr(tokens), _ptr(uniform), _ptr(draft_lens), _ptr(n_accepted),
+        _ptr(tokens_out), _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
 class PrefillBuffers:
     """Device buffers for chunked prefill of a whole prompt (allocation only; torch owns the memory).
 
@@ -409,7 +482,7 @@ class PagedCache:
     """
 
     def __init__(self, k_pages, v_pages, page_table, k_scale=None, v_scale=None):
-        self._pool, self._page_table = (k_pages, v_pages, k_scale, v_scale), page_table
+        self._pool, self._page_table, self._shape = (k_pages, v_pages, k_scale, v_scale), page_table, None
         self.pages = make_pages(k_pages, v_pages, page_table, k_scale, v_scale)   # (addresses: of the tensors that are kept here)
 
     k_pages = property(lambda self: self._pool[0])
@@ -439,6 +512,54 @@ class PagedCache:
             scales = [torch.empty(shape[:3], dtype=torch.uint8, device=dev) for _ in range(2)]
         return cls(torch.empty(shape, dtype=dtype, device=dev), torch.empty(shape, dtype=dtype, device=dev), page_table, *scales)
 
+    def _moves(self, source, max_kv_len, max_budget):
+        """The description of a call that brings rows of `source` here."""
+        mine, theirs = self.k_pages, source.k_pages
+        if theirs.dtype != mine.dtype:
+            raise TypeError(f"pages of {theirs.dtype} into pages of {mine.dtype}")
+        if theirs.shape[1] != mine.shape[1] or theirs.shape[3] != mine.shape[3] or theirs.device != mine.device:
+            raise ValueError("caches that rows move between share KV heads, head size and device")
+        s = self._shape
+        if s is None:
+            _, n_kv, _, d = mine.shape
+            s = self._shape = QuokaShape()
+            s.n_q_heads = s.n_kv_heads = n_kv
+            s.head_dim, s.chunk_len, s.n_retain = d, 1, 1
+            s.dtype = QUOKA_F32 if mine.dtype == torch.float32 else QUOKA_BF16
+            s.q_stride = s.kv_stride = s.ck_stride = s.o_stride = (ctypes.c_int64 * 3)(0, 0, d)
+        s.batch, s.max_kv_len, s.max_budget = self._page_table.shape[0], max_kv_len, max_budget
+        return s
+
+    def compact(self, source, k_idx, k_cnt):
+        """The rows that k_idx [b, n_KV, B_max] lists, k_cnt [b, n_KV] of them, from the pages of `source`, another PagedCache of the same
+        batch, one behind the other into the pages of this one."""
+        b, n_kv = self._page_table.shape[0], self.k_pages.shape[1]
+        for t, dims in ((k_idx, 3), (k_cnt, 2)):
+            if t.dtype != torch.int32 or t.dim() != dims or t.shape[:2] != (b, n_kv) or not t.is_contiguous():
+                raise ValueError("k_idx [b, n_KV, B_max] and k_cnt [b, n_KV] are dense int32 tensors")
+            if t.device != self.k_pages.device:
+                raise ValueError("key lists are on the pages' device")
+        if source.page_table.shape[0] != b:
+            raise ValueError("caches that rows move between are of one batch")
+        # (the positions that the source's table has, as far as there are such caches)
+        room = min(source.pages.max_pages * source.pages.page_len, (1 << 24) - 1, (1 << 32) // (4 * self.k_pages.shape[3]) - 1)
+        quoka_cache_compact(self._moves(source, room, k_idx.shape[2]), source.pages, self.pages, k_idx, k_cnt)
+
+    def copy(self, source, parents=None, first=None, lens=None, max_rows=None):
+        """Rows first[b] .. lens[b] - 1 of sequence parents[b] of `source`, another PagedCache, to the same positions of sequence b.  (After
+        PagedSequences.fork: its parents, first and lens.)  parents None: sequence b itself; first None: 0.  No sequence has more than
+        max_rows of them (None: page_len, what a fork leaves to be copied)."""
+        b, n_parents, dev = self._page_table.shape[0], source.page_table.shape[0], self.k_pages.device
+        if lens is None:
+            raise ValueError("no lengths")
+        for t in (parents, first, lens):
+            if t is not None and (t.dtype != torch.int32 or t.shape != (b,) or not t.is_contiguous() or t.device != dev):
+                raise ValueError("parents, first and lens [b] are dense int32 tensors on the pages' device")
+        if parents is None and n_parents < b:
+            raise ValueError("a source of fewer sequences needs parents")
+        quoka_cache_copy(self._moves(source, 0, 0), source.pages, self.pages, parents, n_parents, first, lens,
+                         self.pages.page_len if max_rows is None else int(max_rows))
+
 
 class PagedBuffers:
     """Device buffers for one chunk over a cache in pages (allocation only; torch owns the memory).
@@ -451,6 +572,7 @@ class PagedBuffers:
         buf.write()        the chunk's rows into the pages
         buf.attn()         attention over all cached rows and the chunk's       (the chunk's rows have been written)
         buf.sparse_attn()  over the listed rows and the chunk's
+        buf.cross_attn()   over all cached rows and no others: kv_lens states of an encoder (or a prefix) that the cache holds
         buf.chunk_attn()   the method's step over pages: write, read K back, select keys, sparse_attn
         buf.read(k, v)     the cached rows as contiguous tensors; either may be None
     """
@@ -563,6 +685,12 @@ class PagedBuffers:
             raise ValueError("no key lists")
         return self._attend(self.k_idx, self.k_cnt)
 
+    def cross_attn(self):
+        if self.q is None:
+            raise ValueError("no queries")
+        quoka_cross_attn(self.shape, self.cache.pages, self.q, self.kv_lens, self.chunk_lens, self.out, self.lse, self.workspace)
+        return self.out
+
     def chunk_attn(self):
         if self.budgets is None:
             raise ValueError("no budgets")
@@ -573,3 +701,114 @@ class PagedBuffers:
         quoka_select_keys(self.shape, self.qbar, self.k_back, self.kv_lens, self.budgets, self.scores, self.k_idx, self.k_cnt,
                           self.workspace)
         return self.sparse_attn()
+
+
+class PagedSequences:
+    """The pages that the sequences of a batch hold (the caller's tensors, kept alive here).
+
+    ref [n_pages] int32: holders of every page of the pool, over all batches, 0 for a free one.  page_table [b, max_pages] int32, held [b]
+    int32: entries of each row that are in use.  page_table is what a PagedCache (of every layer) takes.
+
+        seqs.resize(lens)                   pages for the first lens[b] positions of every sequence; what lies behind is given back
+        children.fork(seqs, parents, lens)  children go on from sequences parents[b] of `seqs`, of which lens tokens are cached: whole pages
+                                            are shared, and PagedCache.copy(.., parents, children.first, children.lens) brings the rest
+
+    lacking [1]: how many pages the last call would have needed beyond those that were free.  first, lens [b]: of the last fork.
+    """
+
+    def __init__(self, ref, page_table, held, page_len):
+        for t, dims in ((ref, 1), (page_table, 2), (held, 1)):
+            if t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous() or t.device != ref.device:
+                raise ValueError("ref [n_pages], page_table [b, max_pages] and held [b] are dense int32 tensors on one device")
+        if held.shape[0] != page_table.shape[0]:
+            raise ValueError("page_table and held are of one batch")
+        self._tensors = (ref, page_table, held)
+        o = self.owners = QuokaPageOwners()   # (addresses: of the tensors that are kept here)
+        o.ref, o.page_table, o.held = ref.data_ptr(), page_table.data_ptr(), held.data_ptr()
+        o.n_pages, o.page_len, o.max_pages, o.batch = ref.shape[0], int(page_len), page_table.shape[1], page_table.shape[0]
+        self.workspace = torch.empty(quoka_pages_workspace_bytes(o), dtype=torch.uint8, device=ref.device)
+        self.lacking = torch.zeros(1, dtype=torch.int32, device=ref.device)
+        self.first, self.lens = (torch.zeros_like(held) for _ in range(2))
+
+    ref = property(lambda self: self._tensors[0])
+    page_table = property(lambda self: self._tensors[1])
+    held = property(lambda self: self._tensors[2])
+
+    @classmethod
+    def allocate(cls, n_pages, page_len, batch, max_pages, device="cuda"):
+        """Sequences that hold nothing, over a pool of which every page is free."""
+        ref = torch.zeros(n_pages, dtype=torch.int32, device=device)
+        return cls._empty(ref, page_len, batch, max_pages)
+
+    def another(self, batch, max_pages=None):
+        """Sequences of another batch that hold nothing, over the same pool."""
+        o = self.owners
+        return self._empty(self.ref, o.page_len, batch, o.max_pages if max_pages is None else max_pages)
+
+    @classmethod
+    def _empty(cls, ref, page_len, batch, max_pages):
+        table = torch.full((batch, max_pages), -1, dtype=torch.int32, device=ref.device)
+        return cls(ref, table, torch.zeros(batch, dtype=torch.int32, device=ref.device), page_len)
+
+    def _lens(self, x, n):
+        if x.dtype != torch.int32 or x.shape != (n,) or not x.is_contiguous() or x.device != self.ref.device:
+            raise ValueError("lengths and parents are dense int32 tensors, one for each sequence, on the pages' device")
+        return x
+
+    def resize(self, lens):
+        o = self.owners
+        quoka_pages_resize(o, self._lens(lens, o.batch), self.lacking, self.workspace)
+
+    def fork(self, source, parents, lens):
+        """parents [b]: sequences of `source` (others: no parent).  lens: cached tokens of the sequences of `source`, each."""
+        o, theirs = self.owners, source.owners
+        quoka_pages_fork(theirs, o, self._lens(parents, o.batch), self._lens(lens, theirs.batch), self.first, self.lens, self.lacking,
+                         self.workspace)
+
+
+class DraftBuffers:
+    """Device buffers for the verification of drafted tokens (allocation only; torch owns the memory).
+
+    target [b, n + 1, vocab]: the target's probabilities of each of the n drafted tokens and of the one behind them, bfloat16 or float32;
+    draft [b, n, vocab]: what the tokens were drawn from (None: they were looked up); tokens [b, n] int32; uniform [b, n + 1] float32:
+    random numbers from [0, 1); draft_lens [b]: tokens that each sequence has drafted (None: n).
+
+        n_accepted, tokens_out = buf.verify()   [b] and [b, n + 1] int32: accepted tokens, the one after them, and -1
+    """
+
+    def __init__(self, target, tokens, uniform, draft=None, draft_lens=None):
+        dev = target.device
+        if target.dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"unsupported dtype {target.dtype}")
+        if draft is not None and draft.dtype != target.dtype:
+            raise TypeError(f"drafts of {draft.dtype} with a target of {target.dtype}")
+        if target.dim() != 3 or target.shape[1] < 2:
+            raise ValueError("target [b, n + 1, vocab], n >= 1")
+        b, n, vocab = target.shape[0], target.shape[1] - 1, target.shape[2]
+        if draft is not None and draft.shape != (b, n, vocab):
+            raise ValueError("target [b, n + 1, vocab] and draft [b, n, vocab] share batch, tokens and vocabulary")
+        if any(t is not None and t.stride(2) != 1 and vocab > 1 for t in (target, draft)):
+            raise ValueError("probabilities of a token are contiguous")
+        if tokens.dtype != torch.int32 or tokens.shape != (b, n) or not tokens.is_contiguous():
+            raise ValueError("tokens [b, n] is a dense int32 tensor")
+        if uniform.dtype != torch.float32 or uniform.shape != (b, n + 1) or not uniform.is_contiguous():
+            raise ValueError("uniform [b, n + 1] is a dense float32 tensor")
+        if any(t is not None and t.device != dev for t in (draft, tokens, uniform)):
+            raise ValueError("probabilities, tokens and random numbers are on one device")
+        self.target, self.draft, self.tokens, self.uniform = target, draft, tokens, uniform
+        self.draft_lens = None if draft_lens is None else _ints(draft_lens, dev)
+        if self.draft_lens is not None and self.draft_lens.numel() != b:
+            raise ValueError("target and draft_lens are of one batch")
+        s = self.shape = QuokaDraftShape()
+        s.batch, s.n_draft, s.vocab = b, n, vocab
+        s.dtype = QUOKA_BF16 if target.dtype == torch.bfloat16 else QUOKA_F32
+        s.target_stride = (ctypes.c_int64 * 2)(target.stride(0), target.stride(1))
+        s.draft_stride = (ctypes.c_int64 * 2)(*(draft.stride()[:2] if draft is not None else (0, 0)))
+        self.n_accepted = torch.empty(b, dtype=torch.int32, device=dev)
+        self.tokens_out = torch.empty((b, n + 1), dtype=torch.int32, device=dev)
+        self.workspace = torch.empty(quoka_verify_workspace_bytes(s), dtype=torch.uint8, device=dev)
+
+    def verify(self):
+        quoka_verify_draft(self.shape, self.target, self.draft, self.tokens, self.uniform, self.draft_lens, self.n_accepted,
+                           self.tokens_out, self.workspace)
+        return self.n_accepted, self.tokens_out

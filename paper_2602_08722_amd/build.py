@@ -13,7 +13,8 @@ OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libquoka.so")
 
 SOURCES = ["api.hip", "select_queries.hip", "score_keys.hip", "topk_keys.hip", "select_keys.hip", "score_stream.hip", "attn_mfma.hip", "attn_decode.hip", "attn_f32.hip",
-           "pages.hip", "paged_attn.hip", "paged_decode.hip", "attn_mfma_paged.hip", "probes.hip"]
+           "pages.hip", "paged_attn.hip", "paged_decode.hip", "attn_mfma_paged.hip",
+           "attn_mfma_states.hip", "page_rows.hip", "page_owners.hip", "verify.hip", "probes.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -25,7 +26,7 @@ FLAGS = [
 ]
 
 # Where the attention kernel's loop begins in a 64-byte line of code moves its time by 1 % either way with every change before it.
-SOURCE_FLAGS = {src: ["-falign-loops=64"] for src in ("attn_mfma.hip", "attn_mfma_paged.hip")}
+SOURCE_FLAGS = {src: ["-falign-loops=64"] for src in ("attn_mfma.hip", "attn_mfma_paged.hip", "attn_mfma_states.hip")}
 
 
 def _compile(src: str, extra) -> str:

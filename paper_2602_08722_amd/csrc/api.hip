@@ -590,7 +590,8 @@ quoka_status quoka_topk_keys_noalloc(const quoka_shape* shape, const float* scor
 }
 
 // ---- caches in pages -----------------------------------------------------------------------------------------------
-static quoka_status check_pages(const quoka_shape& s, const quoka_pages* p, quoka::Pages* out) {
+// (`tokens`: positions of every sequence that the call may ask for)
+static quoka_status check_pages(const quoka_shape& s, const quoka_pages* p, quoka::Pages* out, long long tokens) {
   if (p == nullptr || p->k == nullptr || p->v == nullptr || p->page_table == nullptr) return QUOKA_EINVAL;
   if (p->n_pages < 1 || p->max_pages < 1 || p->page_len < 1 || (p->page_len & (p->page_len - 1)) != 0) return QUOKA_EINVAL;
   if (p->format != QUOKA_PAGES_RAW && p->format != QUOKA_PAGES_FP8) return QUOKA_EUNSUPPORTED;
@@ -600,7 +601,7 @@ static quoka_status check_pages(const quoka_shape& s, const quoka_pages* p, quok
   for (int i = 0; i < 3; ++i)
     if (p->stride[i] < 0 || p->stride[i] % 16 != 0) return QUOKA_EINVAL;
   if (p->stride[2] < s.head_dim) return QUOKA_EINVAL;
-  if ((long long)p->max_pages * p->page_len < s.max_kv_len) return QUOKA_EINVAL;
+  if ((long long)p->max_pages * p->page_len < tokens) return QUOKA_EINVAL;
   // kernels number the 16-byte pieces of a head's rows, to the end of its last one, and scales with 32 bits
   const unsigned __int128 rows_end =
       (unsigned __int128)(p->n_pages - 1) * (uint64_t)p->stride[0] + (unsigned __int128)(p->page_len - 1) * (uint64_t)p->stride[2] + s.head_dim;
@@ -619,6 +620,8 @@ static quoka_status check_pages(const quoka_shape& s, const quoka_pages* p, quok
   out->shift = __builtin_ctz((unsigned)p->page_len);
   return QUOKA_OK;
 }
+
+static quoka_status check_pages(const quoka_shape& s, const quoka_pages* p, quoka::Pages* out) { return check_pages(s, p, out, s.max_kv_len); }
 
 quoka_status quoka_cache_write(const quoka_shape* shape, const quoka_pages* pages, const void* k_chunk, const void* v_chunk,
                                const int32_t* kv_lens, const int32_t* chunk_lens, void* stream) {
@@ -657,9 +660,10 @@ quoka_status quoka_paged_workspace_bytes(const quoka_shape* shape, size_t* out_b
   return QUOKA_OK;
 }
 
-quoka_status quoka_paged_attn(const quoka_shape* shape, const quoka_pages* pages, const void* q, const int32_t* kv_lens,
-                              const int32_t* chunk_lens, const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse,
-                              void* workspace, size_t workspace_bytes, void* stream) {
+// (own: the chunk's own rows are attended too)
+static quoka_status paged_common(const quoka_shape* shape, const quoka_pages* pages, const void* q, const int32_t* kv_lens,
+                                 const int32_t* chunk_lens, const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse,
+                                 void* workspace, size_t workspace_bytes, void* stream, bool own) {
   Dims dm;
   quoka::PagedArgs a;
   quoka_status st = check_shape(shape, &dm);
@@ -684,7 +688,170 @@ quoka_status quoka_paged_attn(const quoka_shape* shape, const quoka_pages* pages
   a.out = out;
   a.lse = lse;
   return from_hip(quoka::launch_paged_attn(dm, shape->dtype, pages->format == QUOKA_PAGES_FP8, a, static_cast<float*>(workspace),
-                                           static_cast<hipStream_t>(stream)));
+                                           static_cast<hipStream_t>(stream), own));
+}
+
+quoka_status quoka_paged_attn(const quoka_shape* shape, const quoka_pages* pages, const void* q, const int32_t* kv_lens,
+                              const int32_t* chunk_lens, const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  return paged_common(shape, pages, q, kv_lens, chunk_lens, k_idx, k_cnt, out, lse, workspace, workspace_bytes, stream, true);
+}
+
+quoka_status quoka_cross_attn(const quoka_shape* shape, const quoka_pages* pages, const void* q, const int32_t* kv_lens,
+                              const int32_t* chunk_lens, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  return paged_common(shape, pages, q, kv_lens, chunk_lens, nullptr, nullptr, out, lse, workspace, workspace_bytes, stream, false);
+}
+
+// What the two calls that move rows have in common.
+static quoka_status move_common(const quoka_shape* shape, const quoka_pages* src, const quoka_pages* dst, long long src_tokens,
+                                long long dst_tokens, Dims* dm, quoka::MoveArgs* a, int* row_bytes) {
+  quoka_status st = check_shape(shape, dm);
+  if (st != QUOKA_OK) return st;
+  st = check_pages(*shape, src, &a->src, src_tokens);
+  if (st != QUOKA_OK) return st;
+  st = check_pages(*shape, dst, &a->dst, dst_tokens);
+  if (st != QUOKA_OK) return st;
+  if (src->format != dst->format || (src->page_table == dst->page_table && src->k == dst->k)) return QUOKA_EINVAL;
+  a->n_kv = shape->n_kv_heads;
+  a->es = src->format == QUOKA_PAGES_FP8 ? 1 : shape->dtype == QUOKA_BF16 ? 2 : 4;
+  *row_bytes = shape->head_dim * a->es;
+  return QUOKA_OK;
+}
+
+quoka_status quoka_cache_compact(const quoka_shape* shape, const quoka_pages* src, const quoka_pages* dst, const int32_t* k_idx,
+                                 const int32_t* k_cnt, void* stream) {
+  Dims dm;
+  quoka::MoveArgs a;
+  int row_bytes = 0;
+  const quoka_status st = move_common(shape, src, dst, shape != nullptr ? shape->max_kv_len : 0, shape != nullptr ? shape->max_budget : 0, &dm, &a, &row_bytes);
+  if (st != QUOKA_OK) return st;
+  if (k_cnt == nullptr || (k_idx == nullptr && dm.B_max > 0)) return QUOKA_EINVAL;
+  if (dm.B_max == 0) return QUOKA_OK;
+  a.list = k_idx;
+  a.cnt = k_cnt;
+  a.B_max = dm.B_max;
+  a.T_max = dm.T_max;
+  return from_hip(quoka::launch_move_rows(a, dm.b, row_bytes, src->format == QUOKA_PAGES_FP8, static_cast<hipStream_t>(stream)));
+}
+
+quoka_status quoka_cache_copy(const quoka_shape* shape, const quoka_pages* src, const quoka_pages* dst, const int32_t* parents,
+                              int32_t n_parents, const int32_t* first, const int32_t* lens, int32_t max_rows, void* stream) {
+  Dims dm;
+  quoka::MoveArgs a;
+  int row_bytes = 0;
+  const quoka_status st = move_common(shape, src, dst, 0, 0, &dm, &a, &row_bytes);
+  if (st != QUOKA_OK) return st;
+  if (lens == nullptr || n_parents < 1 || max_rows < 0 || (parents == nullptr && n_parents < dm.b)) return QUOKA_EINVAL;
+  if (max_rows >= kMaxKv) return QUOKA_EUNSUPPORTED;
+  if (max_rows == 0) return QUOKA_OK;
+  a.parents = parents;
+  a.n_parents = n_parents;
+  a.first = first;
+  a.lens = lens;
+  a.max_rows = max_rows;
+  return from_hip(quoka::launch_move_rows(a, dm.b, row_bytes, src->format == QUOKA_PAGES_FP8, static_cast<hipStream_t>(stream)));
+}
+
+// ---- who holds the pages -------------------------------------------------------------------------------------------
+static quoka_status check_owners(const quoka_page_owners* o, quoka::Owners* out) {
+  if (o == nullptr || o->ref == nullptr || o->page_table == nullptr || o->held == nullptr) return QUOKA_EINVAL;
+  if (o->n_pages < 1 || o->max_pages < 1 || o->batch < 1 || o->page_len < 1 || (o->page_len & (o->page_len - 1)) != 0) return QUOKA_EINVAL;
+  if (o->page_len > 65536 || o->batch > 65535 || o->n_pages > 1 << 30 || (long long)o->batch * o->max_pages >= 1ll << 31) return QUOKA_EUNSUPPORTED;
+  *out = {o->ref, o->page_table, o->held, o->n_pages, __builtin_ctz((unsigned)o->page_len), o->max_pages, o->batch};
+  return QUOKA_OK;
+}
+
+static quoka_status check_owners_ws(const quoka::Owners& o, const void* workspace, size_t bytes) {
+  if (workspace == nullptr) return QUOKA_EINVAL;
+  if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0 || bytes < round_up(quoka::owners_ws_bytes(o), kAlign)) return QUOKA_EWORKSPACE;
+  return QUOKA_OK;
+}
+
+quoka_status quoka_pages_workspace_bytes(const quoka_page_owners* owners, size_t* out_bytes) {
+  quoka::Owners o;
+  const quoka_status st = check_owners(owners, &o);
+  if (st != QUOKA_OK) return st;
+  if (out_bytes == nullptr) return QUOKA_EINVAL;
+  *out_bytes = round_up(quoka::owners_ws_bytes(o), kAlign);
+  return QUOKA_OK;
+}
+
+quoka_status quoka_pages_resize(const quoka_page_owners* owners, const int32_t* lens, int32_t* lacking, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  quoka::Owners o;
+  quoka_status st = check_owners(owners, &o);
+  if (st != QUOKA_OK) return st;
+  if (lens == nullptr || lacking == nullptr) return QUOKA_EINVAL;
+  st = check_owners_ws(o, workspace, workspace_bytes);
+  if (st != QUOKA_OK) return st;
+  return from_hip(quoka::launch_pages_resize(o, lens, lacking, workspace, static_cast<hipStream_t>(stream)));
+}
+
+quoka_status quoka_pages_fork(const quoka_page_owners* from, const quoka_page_owners* children, const int32_t* parents, const int32_t* lens,
+                              int32_t* first, int32_t* child_lens, int32_t* lacking, void* workspace, size_t workspace_bytes,
+                              void* stream) {
+  quoka::Owners p, o;
+  quoka_status st = check_owners(from, &p);
+  if (st != QUOKA_OK) return st;
+  st = check_owners(children, &o);
+  if (st != QUOKA_OK) return st;
+  if (p.ref != o.ref || p.n_pages != o.n_pages || p.shift != o.shift || p.table == o.table || p.held == o.held) return QUOKA_EINVAL;
+  if (parents == nullptr || lens == nullptr || first == nullptr || child_lens == nullptr || lacking == nullptr || child_lens == lens) return QUOKA_EINVAL;
+  st = check_owners_ws(o, workspace, workspace_bytes);
+  if (st != QUOKA_OK) return st;
+  quoka::ForkArgs f;
+  f.parents = parents;
+  f.lens = lens;
+  f.first = first;
+  f.child_lens = child_lens;
+  return from_hip(quoka::launch_pages_fork(p, o, f, lacking, workspace, static_cast<hipStream_t>(stream)));
+}
+
+// ---- verification of drafted tokens --------------------------------------------------------------------------------
+static quoka_status check_draft(const quoka_draft_shape* s) {
+  if (s == nullptr || s->batch < 1 || s->n_draft < 1 || s->vocab < 1) return QUOKA_EINVAL;
+  for (int i = 0; i < 2; ++i)
+    if (s->target_stride[i] < 0 || s->draft_stride[i] < 0) return QUOKA_EINVAL;
+  if (s->dtype != QUOKA_F32 && s->dtype != QUOKA_BF16) return QUOKA_EUNSUPPORTED;
+  if (s->batch > 65535 || s->n_draft > 65535 || s->vocab > 1 << 24) return QUOKA_EUNSUPPORTED;
+  return QUOKA_OK;
+}
+
+quoka_status quoka_verify_workspace_bytes(const quoka_draft_shape* shape, size_t* out_bytes) {
+  const quoka_status st = check_draft(shape);
+  if (st != QUOKA_OK) return st;
+  if (out_bytes == nullptr) return QUOKA_EINVAL;
+  *out_bytes = round_up(quoka::verify_ws_bytes(shape->batch, shape->vocab), kAlign);
+  return QUOKA_OK;
+}
+
+quoka_status quoka_verify_draft(const quoka_draft_shape* shape, const void* target, const void* draft, const int32_t* tokens,
+                                const float* uniform, const int32_t* draft_lens, int32_t* n_accepted, int32_t* tokens_out,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  const quoka_status st = quoka_verify_workspace_bytes(shape, &need);
+  if (st != QUOKA_OK) return st;
+  if (target == nullptr || tokens == nullptr || uniform == nullptr || n_accepted == nullptr || tokens_out == nullptr || workspace == nullptr)
+    return QUOKA_EINVAL;
+  const uintptr_t es = shape->dtype == QUOKA_BF16 ? 2 : 4;
+  if (reinterpret_cast<uintptr_t>(target) % es != 0 || reinterpret_cast<uintptr_t>(draft) % es != 0) return QUOKA_EINVAL;
+  if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0 || workspace_bytes < need) return QUOKA_EWORKSPACE;
+  quoka::VerifyArgs a;
+  a.target = target;
+  a.draft = draft;
+  a.tokens = tokens;
+  a.draft_lens = draft_lens;
+  a.uniform = uniform;
+  a.n_accepted = n_accepted;
+  a.tokens_out = tokens_out;
+  for (int i = 0; i < 2; ++i) {
+    a.ts[i] = shape->target_stride[i];
+    a.ds[i] = shape->draft_stride[i];
+  }
+  a.b = shape->batch;
+  a.n = shape->n_draft;
+  a.V = shape->vocab;
+  return from_hip(quoka::launch_verify(a, shape->dtype, workspace, static_cast<hipStream_t>(stream)));
 }
 
 quoka_status quoka_probe_mfma(int blocks, int iters, float* sink, void* stream) {

@@ -39,7 +39,7 @@ struct FaCfg {
   static constexpr int REC = D + 2;       // floats per row of a partial: O[D], m, l
   static constexpr size_t kLdsBytes =
       (size_t)32 * QLD * 4 + (size_t)kFaWaves * 32 * OLD * 4 + (size_t)kFaWaves * 32 * 2 * 4 +
-      (size_t)kFaWaves * 32 * 4 * (SRC == kFp8Pages ? 2 : 1);
+      (size_t)kFaWaves * 32 * 4 * (is_fp8(SRC) ? 2 : 1);
 };
 
 template <int DB>
@@ -69,7 +69,7 @@ __device__ __forceinline__ FaRow fa_row(int r, int g) { return {r / g, r % g}; }
 template <int D, bool STAGED, int SRC = kContiguous>
 __global__ __launch_bounds__(kFaThreads, 2) void attn_f32(Dims dm, attn_args<SRC> a, float* __restrict__ part, int n_splits) {
   using Cfg = FaCfg<D, SRC>;
-  constexpr bool PAGED = SRC != kContiguous, FP8 = SRC == kFp8Pages;
+  constexpr bool PAGED = SRC != kContiguous, FP8 = is_fp8(SRC), OWN = has_own_rows(SRC);
   static_assert(!(STAGED && FP8), "");
   constexpr int NI = Cfg::NI, DB = Cfg::DB, QLD = Cfg::QLD, OLD = Cfg::OLD, REC = Cfg::REC;
   static_assert(OLD >= D, "a unit's K rows in the place of a wave's output rows");
@@ -106,7 +106,7 @@ __global__ __launch_bounds__(kFaThreads, 2) void attn_f32(Dims dm, attn_args<SRC
   const bool sparse = a.k_idx != nullptr;
   int n_cache = sparse ? min(a.n_cache[b * dm.n_kv + kv], dm.B_max) : min(a.n_cache[b * dm.ls], dm.T_max);
   n_cache = max(n_cache, 0);
-  const int n_chunk = fa_row(min(row0 + 31, n_rows - 1), g).tok + 1;   // chunk keys any row of the block can see
+  const int n_chunk = !OWN ? 0 : fa_row(min(row0 + 31, n_rows - 1), g).tok + 1;   // chunk keys any row of the block can see
   const int cache_units = (n_cache + 31) / 32, units = cache_units + (n_chunk + 31) / 32;
   const int u_begin = (int)((long long)units * split / n_splits), u_end = (int)((long long)units * (split + 1) / n_splits);
 
@@ -414,7 +414,7 @@ __global__ __launch_bounds__(kFaThreads, 2) void attn_f32(Dims dm, attn_args<SRC
       const int h = kv * g + fr.head;
       float* orow = static_cast<float*>(a.out) + b * dm.os[0] + h * dm.os[1] + (size_t)fr.tok * dm.os[2];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] /= l;
+      for (int e = 0; e < 4; ++e) acc[e] = !OWN && l == 0.f ? 0.f : acc[e] / l;   // (a row that sees nothing)
       *reinterpret_cast<f32x4*>(orow + 4 * c4) = acc;
       if (c4 == 0 && a.lse != nullptr)
         a.lse[(size_t)(b * dm.n_q + h) * dm.C + fr.tok] = (m + log2f(l)) * 0.6931471805599453f;
@@ -470,10 +470,11 @@ __global__ __launch_bounds__(kFmThreads) void attn_f32_merge(Dims dm, attn_args<
   }
   float l = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  const float m_fin = !has_own_rows(SRC) && m == -INFINITY ? 0.f : m;
 #pragma unroll
   for (int i = 0; i < RUNS * kFmRun; ++i) {
     if (s0 + i < s1) {
-      const float wgt = __builtin_amdgcn_exp2f(ms[i] - m);   // (every row sees at least its own key: m is finite)
+      const float wgt = __builtin_amdgcn_exp2f(ms[i] - m_fin);   // (a row that has rows of its own sees its own key: m is finite)
       l += wgt * ls[i];
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] += wgt * x[i][e];
@@ -506,7 +507,7 @@ __global__ __launch_bounds__(kFmThreads) void attn_f32_merge(Dims dm, attn_args<
   const int h = kv * dm.g + fr.head;
   float* orow = static_cast<float*>(a.out) + b * dm.os[0] + h * dm.os[1] + (size_t)fr.tok * dm.os[2];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) acc[e] /= l;
+  for (int e = 0; e < 4; ++e) acc[e] = !has_own_rows(SRC) && l == 0.f ? 0.f : acc[e] / l;
   *reinterpret_cast<f32x4*>(orow + 4 * c4) = acc;
   if (c4 == 0 && a.lse != nullptr)
     a.lse[(size_t)(b * dm.n_q + h) * dm.C + fr.tok] = (m + log2f(l)) * 0.6931471805599453f;
@@ -522,22 +523,24 @@ inline bool attn_f32_is_short(const Dims& dm, bool sparse) {
 // Splits of the key list: as many as give every compute unit a block, but at least one unit of 32 keys for every wave
 // of a block (a split costs 16 KiB of partials and a share of the merge launch).
 inline long long f32_blocks(const Dims& dm) { return (long long)dm.b * dm.n_kv * ((dm.C * dm.g + 31) / 32); }
-inline long long f32_units(const Dims& dm, bool sparse) {   // of the longest key list
-  return ((long long)attended_cap(dm, sparse) + 31) / 32 + (dm.C + 31) / 32;
+inline long long f32_units(const Dims& dm, bool sparse, bool own = true) {   // of the longest key list
+  const long long units = ((long long)attended_cap(dm, sparse) + 31) / 32 + (own ? (dm.C + 31) / 32 : 0);
+  return units > 0 ? units : 1;   // (of states without length nothing is split)
 }
-inline int f32_most_splits(const Dims& dm, bool sparse) {
-  const long long n = (f32_units(dm, sparse) + kFaWaves - 1) / kFaWaves;
+inline int f32_most_splits(const Dims& dm, bool sparse, bool own = true) {
+  const long long n = (f32_units(dm, sparse, own) + kFaWaves - 1) / kFaWaves;
   return (int)(n > kFaMaxSplits ? kFaMaxSplits : n);
 }
-inline int f32_splits(const Dims& dm, bool sparse) {
+inline int f32_splits(const Dims& dm, bool sparse, bool own = true) {
   const long long blocks = f32_blocks(dm), n = (256 + blocks - 1) / blocks;
-  const int most = f32_most_splits(dm, sparse);
+  const int most = f32_most_splits(dm, sparse, own);
   return n < most ? (int)n : most;
 }
 
 template <int D, int SRC = kContiguous>
 static hipError_t launch_f32_units(const Dims& dm, const attn_args<SRC>& a, float* part, hipStream_t st) {
-  const int n_splits = f32_splits(dm, a.k_idx != nullptr), n_rb = (dm.C * dm.g + 31) / 32;
+  constexpr bool OWN = has_own_rows(SRC);
+  const int n_splits = f32_splits(dm, a.k_idx != nullptr, OWN), n_rb = (dm.C * dm.g + 31) / 32;
   auto launch = [&](auto staged) -> hipError_t {
     constexpr bool kStaged = decltype(staged)::value;
     constexpr size_t lds = FaCfg<D, SRC>::kLdsBytes;
@@ -549,9 +552,9 @@ static hipError_t launch_f32_units(const Dims& dm, const attn_args<SRC>& a, floa
     return hipSuccess;
   };
   hipError_t e;
-  if constexpr (D == 128 && SRC != kFp8Pages) {
+  if constexpr (D == 128 && !is_fp8(SRC)) {
     // at most four waves of the block have a unit (a list of so few is never split)
-    e = f32_units(dm, a.k_idx != nullptr) <= 4 ? launch(std::false_type{}) : launch(std::true_type{});
+    e = f32_units(dm, a.k_idx != nullptr, OWN) <= 4 ? launch(std::false_type{}) : launch(std::true_type{});
   } else {
     e = launch(std::false_type{});
   }

@@ -103,6 +103,7 @@ struct ListShares {   // of lane i's sequence
   uint32_t n_splits, first_block, blocks, first_record;
   PagedSeq seq;
 };
+template <bool OWN>
 __device__ __forceinline__ ListShares list_shares(const Dims& dm, const PagedAttnArgs& a, int kv) {
   const int lane = threadIdx.x & 63;
   uint32_t row_blocks = 0, groups = 0, tiles = 0;
@@ -111,7 +112,7 @@ __device__ __forceinline__ ListShares list_shares(const Dims& dm, const PagedAtt
   if (lane < dm.b) {
     row_blocks = (uint32_t)(dm.g * ((seq.C + 31) / 32));
     groups = of_two(row_blocks, a.block_shift);
-    tiles = seq.C == 0 ? 0u : of_two(seq.n, a.tile_shift) + of_two(seq.C, a.tile_shift);
+    tiles = seq.C == 0 ? 0u : of_two(seq.n, a.tile_shift) + (OWN ? of_two(seq.C, a.tile_shift) : 0u);
   }
   const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan_u32(groups), 63);
   const float work = wave64_sum((float)groups * (float)tiles);
@@ -131,6 +132,7 @@ __device__ __forceinline__ ListShares list_shares(const Dims& dm, const PagedAtt
   return {n, wave_incl_scan_u32(blocks) - blocks, blocks, wave_incl_scan_u32(records) - records, seq};
 }
 // The share of block `slot`.
+template <bool OWN>
 __device__ __forceinline__ ListShare list_share(const Dims& dm, const PagedAttnArgs& a, int kv, int slot) {
   if (dm.b > kWave) {
     const int each = a.slots / dm.b, groups = (dm.g * ((dm.C + 31) / 32) + (1 << a.block_shift) - 1) >> a.block_shift, n = each / groups;
@@ -138,7 +140,7 @@ __device__ __forceinline__ ListShare list_share(const Dims& dm, const PagedAttnA
     return {b < dm.b && slot % each < groups * n ? b : -1, n, (uint32_t)(slot % each), (uint32_t)(b * dm.g * ((dm.C + 31) / 32) * n),
             paged_seq(dm, a, kv, min(b, dm.b - 1))};
   }
-  const ListShares s = list_shares(dm, a, kv);
+  const ListShares s = list_shares<OWN>(dm, a, kv);
   const unsigned long long mine = __builtin_amdgcn_ballot_w64((uint32_t)slot >= s.first_block && (uint32_t)slot < s.first_block + s.blocks);
   if (mine == 0) return {-1, 1, 0u, 0u, {}};
   const int b = (int)__builtin_ctzll(mine);
@@ -163,7 +165,7 @@ template <int D, bool SPLIT, int SRC = kContiguous>
 struct AttnCfg {
   static constexpr int KT = SPLIT ? 2 * kSub : kSub;  // keys per staged tile
   static constexpr int KS = D / 16;                   // k-steps of the QK^T product
-  static constexpr bool FP8 = SRC == kFp8Pages;
+  static constexpr bool FP8 = is_fp8(SRC);
   static constexpr int CG = D / 8;                    // 16-byte chunks per row
   static constexpr int LPR = FP8 ? CG / 2 : CG;       // lanes that fetch a row, 16 bytes each
   static constexpr int RPI = kSetThreads / LPR;       // rows per set-wide load
@@ -215,7 +217,8 @@ struct AttnCfg {
 template <int D, bool SPLIT, bool XS, bool KSPLIT, bool WHOLE, int SRC = kContiguous>
 __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_args<SRC> a) {
   using Cfg = AttnCfg<D, SPLIT, SRC>;
-  constexpr bool PAGED = SRC != kContiguous, FP8 = SRC == kFp8Pages;
+  constexpr bool PAGED = SRC != kContiguous, FP8 = is_fp8(SRC), OWN = has_own_rows(SRC);
+  constexpr int kFirst = OWN ? -1 : 0;   // number of the first tile
   constexpr bool DMA = Cfg::DMA;
   constexpr int KT = Cfg::KT, KS = Cfg::KS, CG = Cfg::CG, LPR = Cfg::LPR, RPI = Cfg::RPI, NLD = Cfg::NLD,
                 DB = Cfg::DB, HW = Cfg::HW;
@@ -231,7 +234,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   [[maybe_unused]] ListShare share = {};
   [[maybe_unused]] PagedSeq seq = {};
   if constexpr (PAGED && KSPLIT) {
-    share = list_share(dm, a, kv, blockIdx.y);
+    share = list_share<OWN>(dm, a, kv, blockIdx.y);
     if (share.b < 0) return;   // block-uniform
     b = share.b;
     if (share.block == 0 && threadIdx.x == 0) a.shares[kv * dm.b + b] = u32x2{(uint32_t)share.n_splits, share.record};
@@ -418,7 +421,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
       dma16(p, area + slot * (32 * Cfg::ROW) + (uint32_t)((SPLIT ? set * N : 0) + i) * 1024u);
     }
   };
-  if constexpr (!KSPLIT) request_q(q_area(-1));
+  if constexpr (!KSPLIT) request_q(q_area(kFirst));
   const int n_cache = max(min(n_given, sparse ? dm.B_max : dm.T_max), 0);
   // Tile order: the chunk's first tile, the cache tiles, the chunk's other tiles.  What a wave can see is one run of tiles [w0, w1), whose
   // end is where its causal range ends; the first tile needs no index look-up, so its loads leave right at kernel start; and every row
@@ -426,22 +429,23 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   // as a tile has.  (With the chunk's tiles from the last to the first a row met the tile of its diagonal first, of which it may see
   // a single key; the largest probability is then less often 1, the only one that is not rounded: the outputs of a first chunk of 1024
   // tokens lay 0.27 % further from float64, of 2048 0.46 %, of 1024 over 100 keys 0.27 %.)
-  const int n_cht = (c_end_blk + KT - 1) / KT;
+  // (Not OWN: the cache tiles alone, which every row sees whole.)
+  const int n_cht = OWN ? (c_end_blk + KT - 1) / KT : 0;
   const int n_ct = (n_cache + KT - 1) / KT;
   const int n_tiles = n_cht + n_ct;
   // Tiles are numbered from -1, so that the cache tiles are 0 .. n_ct - 1.
-  const int t_begin = (KSPLIT ? (int)((uint32_t)n_tiles * (uint32_t)split / (uint32_t)n_splits) : 0) - 1;
-  const int t_end = (KSPLIT ? (int)((uint32_t)n_tiles * (uint32_t)(split + 1) / (uint32_t)n_splits) : n_tiles) - 1;
+  const int t_begin = (KSPLIT ? (int)((uint32_t)n_tiles * (uint32_t)split / (uint32_t)n_splits) : 0) + kFirst;
+  const int t_end = (KSPLIT ? (int)((uint32_t)n_tiles * (uint32_t)(split + 1) / (uint32_t)n_splits) : n_tiles) + kFirst;
   auto is_cache = [&](int t) __attribute__((always_inline)) { return (uint32_t)t < (uint32_t)n_ct; };
   // first key (cache slot or chunk position) of tile t
   auto tile_base = [&](int t) __attribute__((always_inline)) { return (is_cache(t) ? t : max(t - (n_ct - 1), 0)) * KT; };
-  const int seen = tok0 + 31 >= sub ? (tok0 + 31 - sub) / KT + 1 : 0;   // chunk tiles of whose share for this set the wave sees something
+  const int seen = !OWN ? 0 : tok0 + 31 >= sub ? (tok0 + 31 - sub) / KT + 1 : 0;   // chunk tiles of whose share for this set the wave sees something
   // Tiles whose unit u has keys that not every row sees: at the end of the cache list, and the last chunk tile (-2: none).
   int tail_tile[2], diag_tile[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     tail_tile[u] = n_ct > 0 && (n_ct - 1) * KT + sub + 32 * u + 32 > n_cache ? n_ct - 1 : -2;
-    diag_tile[u] = max(seen - 1, 0) * KT + sub + 32 * u + 31 > tok0 ? (seen <= 1 ? -1 : n_ct + seen - 2) : -2;
+    diag_tile[u] = OWN && max(seen - 1, 0) * KT + sub + 32 * u + 31 > tok0 ? (seen <= 1 ? -1 : n_ct + seen - 2) : -2;
   }
   int w0 = seen > 0 ? -1 : 0;
   int w1 = n_ct + max(seen - 1, 0);
@@ -958,7 +962,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   }
   if constexpr (!WHOLE) {
     if (wave_on && tok < C) {
-      const float inv = 1.0f / l_tot;
+      const float inv = inverse_sum<SRC>(l_tot);
       uint16_t* orow = static_cast<uint16_t*>(a.out) + b * dm.os[0] + h * dm.os[1] + (size_t)tok * dm.os[2];
 #pragma unroll
       for (int c = 0; c < DB; ++c)
@@ -983,7 +987,7 @@ __global__ __launch_bounds__(2 * kSetThreads, 2) void attn_bf16(Dims dm, attn_ar
   }
   uint16_t* ot = reinterpret_cast<uint16_t*>(smem) + (SPLIT ? (size_t)slot * 64 * (2 + DB * 16) * 2 : (size_t)slot * 32 * OLD);
   if (!wave_on) return;
-  const float inv = 1.0f / l_tot;
+  const float inv = inverse_sum<SRC>(l_tot);
 #pragma unroll
   for (int c = 0; c < DB; ++c)
 #pragma unroll
@@ -1123,7 +1127,7 @@ __global__ __launch_bounds__(64 * kMergeWaves) void attn_bf16_merge(Dims dm, att
   }
   const int tok = (x / dm.g) * 32 + li, h = kv * dm.g + x % dm.g;
   if (tok >= C) return;
-  const float inv = 1.0f / l;
+  const float inv = inverse_sum<SRC>(l);
   uint16_t* orow = static_cast<uint16_t*>(a.out) + b * dm.os[0] + h * dm.os[1] + (size_t)tok * dm.os[2];
 #pragma unroll
   for (int v4 = 0; v4 < 4; ++v4) {
@@ -1134,9 +1138,12 @@ __global__ __launch_bounds__(64 * kMergeWaves) void attn_bf16_merge(Dims dm, att
     a.lse[(size_t)(b * dm.n_q + h) * dm.C + tok] = (m + log2f(l)) * 0.6931471805599453f;
 }
 
-inline int key_splits_limit(const Dims& dm, bool sparse, int keys_per_tile) {
-  const long long tiles = ((long long)attended_cap(dm, sparse) + keys_per_tile - 1) / keys_per_tile +
-                          (dm.C + keys_per_tile - 1) / keys_per_tile;
+// `own`: the list ends with the chunk's rows.
+inline long long tiles_at_most(const Dims& dm, bool sparse, int keys_per_tile, bool own) {
+  return ((long long)attended_cap(dm, sparse) + keys_per_tile - 1) / keys_per_tile + (own ? (dm.C + keys_per_tile - 1) / keys_per_tile : 0);
+}
+inline int key_splits_limit(const Dims& dm, bool sparse, int keys_per_tile, bool own = true) {
+  const long long tiles = tiles_at_most(dm, sparse, keys_per_tile, own);
   return (int)(tiles < kMaxKeySplits ? tiles : kMaxKeySplits);
 }
 
@@ -1167,7 +1174,7 @@ static hipError_t launch_variant(const Dims& dm, const attn_args<SRC>& a, hipStr
                     room = kMaxRecords / (dm.n_kv * of_block);
     const long long slots = dm.b == 1 || dm.b > kWave || planned >= round ? planned : one_more < round ? one_more : round;
     aa.slots = (int)(slots < room ? slots : room);
-    if (dm.b <= kWave) most_splits = key_splits_limit(dm, a.k_idx != nullptr, Cfg::KT);
+    if (dm.b <= kWave) most_splits = key_splits_limit(dm, a.k_idx != nullptr, Cfg::KT, has_own_rows(SRC));
     aa.n_splits = most_splits;
     const long long of_lists = (long long)dm.b * nrb * most_splits;
     aa.records = (int)((long long)aa.slots * of_block < of_lists ? (long long)aa.slots * of_block : of_lists);
@@ -1236,11 +1243,11 @@ struct AttnPlan {
 // fill seven eighths of a round at most are shared by the blocks of a whole round.  (27 batches of 2 - 13 sequences, 130 - 224 blocks of
 // eight, 8400 - 31200 keys and chunk tokens together: 0.84 - 0.90 of the time of whole lists in blocks of four for equal lengths, 0.73 - 1.05 for
 // lengths and chunks up to eight times apart; fuller rounds and 2000 - 8000 keys 0.9 - 1.2, shorter lists 1.1 - 2.)
-inline AttnPlan attn_plan(const Dims& dm, bool sparse, bool paged = false) {
+inline AttnPlan attn_plan(const Dims& dm, bool sparse, bool paged = false, bool own = true) {
   const long long nrb = (long long)dm.g * ((dm.C + 31) / 32), heads = (long long)dm.n_kv * dm.b;
   const long long eights = heads * ((nrb + 7) / 8);
   if (paged && dm.b > 1 && dm.b <= kWave && heads * nrb * 2 > kMaxRecords && eights <= kComputeUnits * 7 / 8 &&
-      attended_cap(dm, sparse) + dm.C >= 8192 && dm.b * ((nrb + 7) / 8) <= kComputeUnits / dm.n_kv)
+      attended_cap(dm, sparse) + (own ? dm.C : 0) >= 8192 && dm.b * ((nrb + 7) / 8) <= kComputeUnits / dm.n_kv)
     return AttnPlan{false, 2};
   if (heads * nrb * 2 > kMaxRecords) return AttnPlan{!eight_row_blocks(dm, sparse, heads * ((nrb + 7) / 8)), 1};
   struct Fit {
@@ -1256,8 +1263,8 @@ inline AttnPlan attn_plan(const Dims& dm, bool sparse, bool paged = false) {
   for (int mode = 1; mode >= 0; --mode) {
     const int kt = mode == 0 ? kSub : 2 * kSub, per_block = mode == 0 ? 8 : 4;
     const long long blocks = heads * ((nrb + per_block - 1) / per_block);
-    const int limit = key_splits_limit(dm, sparse, kt);
-    const long long tiles = ((long long)attended_cap(dm, sparse) + kt - 1) / kt + (dm.C + kt - 1) / kt;
+    const int limit = key_splits_limit(dm, sparse, kt, own);
+    const long long tiles = tiles_at_most(dm, sparse, kt, own);
     const bool whole = mode == 1 || (heads * ((nrb + 3) / 4) > kComputeUnits && (dm.b == 1 || attended_cap(dm, sparse) <= kRaggedKeys));
     for (int n = whole ? 1 : 2; n == 1 || (n <= limit && heads * nrb * n <= kMaxRecords); ++n) {
       const Fit& f = n == 1 ? kWhole[wide][mode] : kSplit[wide][mode];

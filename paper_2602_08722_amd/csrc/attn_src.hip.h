@@ -9,7 +9,10 @@
 namespace quoka {
 
 // Where the rows of the cache and the chunk lie: in tensors of their own, or in pages, which hold both, as they are or in 8 bits.
-constexpr int kContiguous = 0, kRawPages = 1, kFp8Pages = 2;
+// kRawStates, kFp8States: in pages likewise, but none of the rows is the chunk's own: every query sees all cached rows (cross attention).
+constexpr int kContiguous = 0, kRawPages = 1, kFp8Pages = 2, kRawStates = 3, kFp8States = 4;
+constexpr bool is_fp8(int src) { return src == kFp8Pages || src == kFp8States; }
+constexpr bool has_own_rows(int src) { return src < kRawStates; }
 struct PagedAttnArgs : AttnArgs {   // (n_cache: as in AttnArgs)
   const int32_t *kv_lens = nullptr, *chunk_lens = nullptr;
   Pages pg = {};
@@ -38,6 +41,12 @@ using attn_args = std::conditional_t<SRC == kContiguous, AttnArgs, PagedAttnArgs
 __device__ __forceinline__ int chunk_of(const Dims& dm, const AttnArgs&, int b) { return dm.chunk(b); }
 __device__ __forceinline__ int chunk_of(const Dims& dm, const PagedAttnArgs& a, int b) {
   return a.chunk_lens == nullptr ? dm.C : max(min(a.chunk_lens[b], dm.C), 0);
+}
+// (1 / 0 for a row that sees nothing, of which only cross attention has any: its sums are zero, and so is what they are multiplied with)
+template <int SRC>
+__device__ __forceinline__ float inverse_sum(float l) {
+  if constexpr (has_own_rows(SRC)) return 1.0f / l;
+  return l > 0.f ? 1.0f / l : 0.f;
 }
 // its cached tokens (in pages; elsewhere nothing asks)
 __device__ __forceinline__ int paged_len(const Dims&, const AttnArgs&, int) { return 0; }

@@ -148,11 +148,46 @@ struct PagedArgs {
 };
 size_t paged_attn_bf16_ws_floats(const Dims& dm);
 hipError_t launch_paged_attn_bf16(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st);
-// up to 32 query rows per KV head
+hipError_t launch_cross_attn_bf16(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st);
+// up to 32 query rows per KV head.  `own`: the chunk's own rows are attended, causally (else the cached ones alone)
 size_t paged_decode_ws_floats(const Dims& dm);
-hipError_t launch_paged_decode(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st);
+hipError_t launch_paged_decode(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st, bool own = true);
 size_t paged_attn_ws_floats(const Dims& dm, int dtype);
-hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float* part, hipStream_t st);
+hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float* part, hipStream_t st, bool own = true);
+
+// rows of pages into other pages (page_rows.hip): the listed ones of every KV head (list), or first .. lens - 1 of the parents
+struct MoveArgs {
+  Pages src, dst;
+  const int32_t *list = nullptr, *cnt = nullptr;
+  const int32_t *parents = nullptr, *first = nullptr, *lens = nullptr;   // parents, first: may be nullptr
+  int n_kv = 0, es = 0, B_max = 0, T_max = 0, n_parents = 0, max_rows = 0;
+};
+hipError_t launch_move_rows(MoveArgs a, int batch, int row_bytes, bool fp8, hipStream_t st);
+
+// --- who holds the pages (page_owners.hip) ------------------------------------------------------------
+struct Owners {
+  int32_t *ref, *table, *held;
+  int n_pages, shift, max_pages, b;   // page_len == 1 << shift
+};
+struct ForkArgs {
+  const int32_t *parents = nullptr, *lens = nullptr;
+  int32_t *first = nullptr, *child_lens = nullptr;
+};
+size_t owners_ws_bytes(const Owners& o);
+hipError_t launch_pages_resize(const Owners& o, const int32_t* lens, int32_t* lacking, void* ws, hipStream_t st);
+hipError_t launch_pages_fork(const Owners& from, const Owners& o, const ForkArgs& f, int32_t* lacking, void* ws, hipStream_t st);
+
+// --- verification of drafted tokens (verify.hip) ----------------------------------------------------------
+struct VerifyArgs {
+  const void *target, *draft;   // draft: nullptr where the drafts come without probabilities
+  const int32_t *tokens, *draft_lens;
+  const float* uniform;
+  int32_t *n_accepted, *tokens_out;
+  long long ts[2], ds[2];   // sequence and token strides
+  int b, n, V;
+};
+size_t verify_ws_bytes(int batch, int vocab);
+hipError_t launch_verify(const VerifyArgs& a, int dtype, void* ws, hipStream_t st);
 
 // --- measurement aids (probes.hip) ------------------------------------------------------------------
 hipError_t launch_probe_mfma(int blocks, int iters, float* sink, hipStream_t st);

@@ -10,7 +10,7 @@ namespace quoka {
 // 6.6 -> 6.0; 8-bit pages 10.1 -> 5.6, 10.8 -> 7.9, 7.3 -> 5.8.
 constexpr int kPsThreads = 256;
 
-template <bool FP8, int D>
+template <bool FP8, int D, bool OWN>
 __global__ __launch_bounds__(kPsThreads) void paged_f32_short(Dims dm, PagedArgs a) {
   constexpr int EPL = D / 64;
   __shared__ float qs[kPsThreads / 64][D];
@@ -39,7 +39,7 @@ __global__ __launch_bounds__(kPsThreads) void paged_f32_short(Dims dm, PagedArgs
   const int n_list = a.k_idx == nullptr ? n_before : min(max(a.k_cnt[b * dm.n_kv + kv], 0), dm.B_max);
   const int32_t* list = a.k_idx == nullptr ? nullptr : a.k_idx + (long long)(b * dm.n_kv + kv) * dm.B_max;
   const int32_t* table = pg.table + (long long)b * pg.max_pages;
-  const int total = n_list + i + 1;
+  const int total = OWN ? n_list + i + 1 : n_list;
   const float scale = 1.0f / sqrtf((float)D);
   float m_run = -INFINITY, l_run = 0.f, acc[EPL];
 #pragma unroll
@@ -88,18 +88,19 @@ __global__ __launch_bounds__(kPsThreads) void paged_f32_short(Dims dm, PagedArgs
   }
   float* out = static_cast<float*>(a.out) + b * dm.os[0] + h * dm.os[1] + i * dm.os[2];
 #pragma unroll
-  for (int e = 0; e < EPL; ++e) out[lane + 64 * e] = acc[e] / l_run;
+  for (int e = 0; e < EPL; ++e) out[lane + 64 * e] = !OWN && total == 0 ? 0.f : acc[e] / l_run;   // (nothing to see)
   if (a.lse != nullptr && lane == 0) a.lse[(long long)(b * dm.n_q + h) * dm.C + i] = m_run + logf(l_run);
 }
 
-template <bool FP8, int D>
+template <bool FP8, int D, bool OWN>
 static hipError_t launch_paged_f32(const Dims& dm, const PagedArgs& a, float* part, hipStream_t st) {
   if (attn_f32_is_short(dm, a.k_idx != nullptr)) {
     const dim3 grid((dm.C + kPsThreads / 64 - 1) / (kPsThreads / 64), dm.n_q, dm.b);
-    hipLaunchKernelGGL((paged_f32_short<FP8, D>), grid, dim3(kPsThreads), 0, st, dm, a);
+    hipLaunchKernelGGL((paged_f32_short<FP8, D, OWN>), grid, dim3(kPsThreads), 0, st, dm, a);
     return hipGetLastError();
   }
-  return launch_f32_units<D, FP8 ? kFp8Pages : kRawPages>(dm, paged_attn_args(a, part), part, st);
+  constexpr int SRC = OWN ? FP8 ? kFp8Pages : kRawPages : FP8 ? kFp8States : kRawStates;
+  return launch_f32_units<D, SRC>(dm, paged_attn_args(a, part), part, st);
 }
 
 size_t paged_attn_ws_floats(const Dims& dm, int dtype) {
@@ -107,11 +108,17 @@ size_t paged_attn_ws_floats(const Dims& dm, int dtype) {
   return attn_decode_applies(dm) ? paged_decode_ws_floats(dm) : paged_attn_bf16_ws_floats(dm);
 }
 
-hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float* part, hipStream_t st) {
-  if (dtype == QUOKA_BF16)
-    return attn_decode_applies(dm) ? launch_paged_decode(dm, fp8, a, part, st) : launch_paged_attn_bf16(dm, fp8, a, part, st);
-  if (dm.d == 64) return fp8 ? launch_paged_f32<true, 64>(dm, a, part, st) : launch_paged_f32<false, 64>(dm, a, part, st);
-  return fp8 ? launch_paged_f32<true, 128>(dm, a, part, st) : launch_paged_f32<false, 128>(dm, a, part, st);
+hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float* part, hipStream_t st, bool own) {
+  if (dtype == QUOKA_BF16) {
+    if (attn_decode_applies(dm)) return launch_paged_decode(dm, fp8, a, part, st, own);
+    return own ? launch_paged_attn_bf16(dm, fp8, a, part, st) : launch_cross_attn_bf16(dm, fp8, a, part, st);
+  }
+  auto launch = [&](auto own_rows) {
+    constexpr bool OWN = decltype(own_rows)::value;
+    if (dm.d == 64) return fp8 ? launch_paged_f32<true, 64, OWN>(dm, a, part, st) : launch_paged_f32<false, 64, OWN>(dm, a, part, st);
+    return fp8 ? launch_paged_f32<true, 128, OWN>(dm, a, part, st) : launch_paged_f32<false, 128, OWN>(dm, a, part, st);
+  };
+  return own ? launch(std::true_type{}) : launch(std::false_type{});
 }
 
 }  // namespace quoka

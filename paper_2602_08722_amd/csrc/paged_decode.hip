@@ -83,14 +83,18 @@ __device__ __forceinline__ PdSeq pd_seq(const Dims& dm, const PagedArgs& a, int 
 }
 
 // 64 sequences from b0 on, one a lane, and their tiles (a sequence without a token in this chunk has none).
+template <bool OWN>
 struct PdLine {
   PdSeq seq;
   uint32_t end;   // and where their room in the line of tiles ends (pd_place)
   int b0;
-  __device__ __forceinline__ uint32_t tiles() const { return seq.C > 0 ? (uint32_t)(seq.n_list + seq.C + kPdTile - 1) / kPdTile : 0u; }
+  __device__ __forceinline__ uint32_t tiles() const {
+    return seq.C > 0 ? (uint32_t)(seq.n_list + (OWN ? seq.C : 0) + kPdTile - 1) / kPdTile : 0u;
+  }
 };
-__device__ __forceinline__ PdLine pd_line(const Dims& dm, const PagedArgs& a, int kv, int b0, bool sparse) {
-  PdLine line;
+template <bool OWN>
+__device__ __forceinline__ PdLine<OWN> pd_line(const Dims& dm, const PagedArgs& a, int kv, int b0, bool sparse) {
+  PdLine<OWN> line;
   line.b0 = b0;
   const int b = b0 + (threadIdx.x & 63);
   line.seq = dm.b == 1 ? pd_seq(dm, a, 0, kv, sparse) : pd_seq(dm, a, min(b, dm.b - 1), kv, sparse);   // (one sequence: scalar fetches)
@@ -109,9 +113,10 @@ struct PdPlan {
   uint32_t quota, total;
   bool whole;
 };
-__device__ __forceinline__ PdPlan pd_plan(const Dims& dm, const PagedArgs& a, int kv, const PdLine& start, int n_slots, bool sparse) {   // start: b0 = 0
+template <bool OWN>
+__device__ __forceinline__ PdPlan pd_plan(const Dims& dm, const PagedArgs& a, int kv, const PdLine<OWN>& start, int n_slots, bool sparse) {   // start: b0 = 0
   uint32_t total = dm.b == 1 ? (uint32_t)__builtin_amdgcn_readfirstlane((int)start.tiles()) : last_lane(wave_incl_scan_u32(start.tiles()));
-  for (int b0 = kWave; b0 < dm.b; b0 += kWave) total += last_lane(wave_incl_scan_u32(pd_line(dm, a, kv, b0, sparse).tiles()));
+  for (int b0 = kWave; b0 < dm.b; b0 += kWave) total += last_lane(wave_incl_scan_u32(pd_line<OWN>(dm, a, kv, b0, sparse).tiles()));
   const uint32_t even = max((total + (uint32_t)n_slots - 1) / (uint32_t)n_slots, 1u);
   if (dm.b > 1 && dm.b <= kWave && 2 * dm.b <= n_slots) {   // (with more sequences it is rarely so, and the question costs 2 - 3 %)
     const uint32_t quota = (even + kPdWaves - 1) / kPdWaves * kPdWaves, blocks = last_lane(wave_incl_scan_u32(blocks_of(start.tiles(), quota)));
@@ -123,14 +128,16 @@ __device__ __forceinline__ PdPlan pd_plan(const Dims& dm, const PagedArgs& a, in
 __device__ __forceinline__ uint32_t pd_room(const PdPlan& plan, uint32_t tiles) {
   return plan.whole ? blocks_of(tiles, plan.quota) * plan.quota : tiles;
 }
-__device__ __forceinline__ void pd_place(const Dims& dm, const PdPlan& plan, PdLine& line, uint32_t before) {
+template <bool OWN>
+__device__ __forceinline__ void pd_place(const Dims& dm, const PdPlan& plan, PdLine<OWN>& line, uint32_t before) {
   const uint32_t room = pd_room(plan, line.tiles());
   line.end = before + (dm.b == 1 ? (uint32_t)__builtin_amdgcn_readfirstlane((int)room) : wave_incl_scan_u32(room));
 }
 
 // part: [n_kv, n_slots + batch, kRec] float32.  The partial of sequence b from block s is s + b: along the line of tiles either grows with every
 // part of a sequence.  parts: [n_kv, batch], the block of a sequence's first part and how many there are, for the merge.
-template <int D, bool FP8, bool LIST>
+// OWN: the chunk's own rows come behind the list, and token c sees those up to its own; otherwise every token sees the list and no more.
+template <int D, bool FP8, bool LIST, bool OWN>
 __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs a, float* __restrict__ part, u32x2* __restrict__ parts,
                                                               int n_slots) {
   using Cfg = PdCfg<D, FP8>;
@@ -142,7 +149,7 @@ __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 31, hf = lane >> 5;
   const int g = dm.g;
-  PdLine line = pd_line(dm, a, kv, 0, LIST);
+  PdLine<OWN> line = pd_line<OWN>(dm, a, kv, 0, LIST);
   const PdPlan plan = pd_plan(dm, a, kv, line, n_slots, LIST);
   pd_place(dm, plan, line, 0u);
   uint32_t at = blockIdx.x * plan.quota;   // (blocks x quota < total + a block's share: 32 bits)
@@ -151,7 +158,7 @@ __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs
     unsigned long long hit;
     while ((hit = __builtin_amdgcn_ballot_w64(at < line.end)) == 0) {   // (at < total: some sequence has it)
       const uint32_t before = last_lane(line.end);
-      line = pd_line(dm, a, kv, line.b0 + kWave, LIST);
+      line = pd_line<OWN>(dm, a, kv, line.b0 + kWave, LIST);
       pd_place(dm, {0u, 0u, false}, line, before);   // (more than 64 sequences: not by whole blocks)
     }
     const int of = (int)__builtin_ctzll(hit), b = line.b0 + of;
@@ -161,7 +168,7 @@ __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs
     seq.C = __builtin_amdgcn_readlane(line.seq.C, of);
     const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)(line.end - pd_room(plan, line.tiles())), of),
                    end = first + (uint32_t)__builtin_amdgcn_readlane((int)line.tiles(), of);
-    const int n_list = seq.n_list, n_keys = n_list + seq.C, n_rows = seq.C * g;   // n_rows <= 32, checked by the launcher
+    const int n_list = seq.n_list, n_keys = n_list + (OWN ? seq.C : 0), n_rows = seq.C * g;   // n_rows <= 32, checked by the launcher
     const int t_end = (int)(min(at_end, end) - first);
     if (at == first && tid == 0) parts[kv * dm.b + b] = u32x2{blockIdx.x, (end - 1) / plan.quota - blockIdx.x + 1};
     int t = (int)(at - first) + w;   // this wave's tiles: every fourth
@@ -279,7 +286,7 @@ __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs
       for (int ks = 0; ks < KS; ++ks)
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kp + ks * 16), qreg[ks], s, 0, 0, 0);
       if (slot0 + kPdTile > n_list) {   // wave-uniform: the tile touches the chunk's rows or the end
-        const int limit = n_list + tok + 1 - slot0;   // keys kk < limit of the tile are visible
+        const int limit = n_list + (OWN ? tok + 1 : 0) - slot0;   // keys kk < limit of the tile are visible
 #pragma unroll
         for (int v = 0; v < 16; ++v)
           if (8 * (v / 4) + 4 * hf + v % 4 >= limit) s[v] = -INFINITY;
@@ -384,9 +391,17 @@ __global__ __launch_bounds__(kPdThreads, 2) void paged_decode(Dims dm, PagedArgs
   }
 }
 
+// Tokens of sequence b's chunk that see any row (not OWN: none where nothing is cached, and then there are no partials).
+template <bool OWN>
+__device__ __forceinline__ int pd_live(const Dims& dm, const PagedArgs& a, int b) {
+  const int C = a.chunk_lens == nullptr ? dm.C : max(min(a.chunk_lens[b], dm.C), 0);
+  if constexpr (OWN) return C;
+  return a.kv_lens[b] > 0 && dm.T_max > 0 ? C : 0;
+}
+
 // Many partials: a block merges row r of sequence b.  Threads weigh a partial each, or two; thread (four dims c4, group sg) adds up the outputs of
 // every NG-th split, four of them on the way at a time, and the groups' sums meet in LDS, in a fixed order.
-template <int D>
+template <int D, bool OWN>
 __device__ __forceinline__ void merge_row(const Dims& dm, const PagedArgs& a, const float* __restrict__ part, const u32x2* __restrict__ parts,
                                           int n_slots, int r, int kv, int b) {
   constexpr int TPR = D / 4, NG = kPdThreads / TPR, RUN = 4;
@@ -396,8 +411,8 @@ __device__ __forceinline__ void merge_row(const Dims& dm, const PagedArgs& a, co
   __shared__ float4 red[NG][TPR];
   __shared__ float wm[kPdWaves], wl[kPdWaves];
   const int tid = threadIdx.x;
-  const int C = a.chunk_lens == nullptr ? dm.C : max(min(a.chunk_lens[b], dm.C), 0);
-  if (r >= C * dm.g) {   // block-uniform: a row past the sequence's chunk
+  const int C = pd_live<OWN>(dm, a, b);
+  if (r >= C * dm.g) {   // block-uniform: a row past the sequence's chunk, or without a row to see
     const int tok = r / dm.g, h = kv * dm.g + r % dm.g;
     uint16_t* orow = static_cast<uint16_t*>(a.out) + b * dm.os[0] + h * dm.os[1] + (size_t)tok * dm.os[2];
     if (tid < TPR) *reinterpret_cast<u32x2*>(orow + 4 * tid) = u32x2{0u, 0u};
@@ -493,6 +508,7 @@ __device__ __forceinline__ void merge_row(const Dims& dm, const PagedArgs& a, co
 
 // The sequence of a KV head that is number `rank` of those with more than kPdFew partials, or -1.  Every wave finds it for itself, 256
 // sequences at a time.
+template <bool OWN>
 __device__ __forceinline__ int long_sequence(const Dims& dm, const PagedArgs& a, const u32x2* __restrict__ parts, int kv, int rank) {
   constexpr int RUN = 4;
   const int lane = threadIdx.x & 63;
@@ -501,7 +517,7 @@ __device__ __forceinline__ int long_sequence(const Dims& dm, const PagedArgs& a,
 #pragma unroll
     for (int u = 0; u < RUN; ++u) {
       const int b = b0 + u * kWave + lane, at = min(b, dm.b - 1);
-      const int C = a.chunk_lens == nullptr ? dm.C : a.chunk_lens[at];   // (without a token the parts are not this call's)
+      const int C = OWN ? a.chunk_lens == nullptr ? dm.C : a.chunk_lens[at] : pd_live<OWN>(dm, a, at);   // (without a token the parts are not this call's)
       is_long[u] = b < dm.b && C > 0 && (int)parts[kv * dm.b + at][1] > kPdFew;
     }
 #pragma unroll
@@ -519,10 +535,10 @@ __device__ __forceinline__ int long_sequence(const Dims& dm, const PagedArgs& a,
 }
 
 // Many partials a sequence: one block per (row, KV head, sequence).
-template <int D>
+template <int D, bool OWN>
 __global__ __launch_bounds__(kPdThreads) void paged_decode_merge(Dims dm, PagedArgs a, const float* __restrict__ part,
                                                                const u32x2* __restrict__ parts, int n_slots) {
-  merge_row<D>(dm, a, part, parts, n_slots, blockIdx.x, blockIdx.y, blockIdx.z);
+  merge_row<D, OWN>(dm, a, part, parts, n_slots, blockIdx.x, blockIdx.y, blockIdx.z);
 }
 
 // Few partials a sequence: a thread adds up four dims of a row over all of them, eight on the way at a time, and D / 4 threads are a row, so that
@@ -532,7 +548,7 @@ __global__ __launch_bounds__(kPdThreads) void paged_decode_merge(Dims dm, PagedA
 // Few on the mean, that is: a sequence far longer than the others has nearly all blocks' partials.  Those of more than kPdFew are left to the
 // launch's first `n_long` layers, where a block is a row as above (one sequence of 100000 keys among 73 of 100, whole calls, 16/1 heads of 128
 // 70.9 -> 24.9 us, 16/2 49.0 -> 26.8, 32/4 of 64 41.8 -> 29.4, 32/8 68.8 -> 63.8; 32 - 128 of 500 the same within 1 %, and so with kPdFew 8 or 32).
-template <int D>
+template <int D, bool OWN>
 __global__ __launch_bounds__(kPdThreads) void paged_decode_merge_few(Dims dm, PagedArgs a, const float* __restrict__ part,
                                                                    const u32x2* __restrict__ parts, int n_slots, int n_long) {
   constexpr int TPR = D / 4, RUN = 8;
@@ -540,13 +556,13 @@ __global__ __launch_bounds__(kPdThreads) void paged_decode_merge_few(Dims dm, Pa
   const int kv = blockIdx.y, rows = dm.C * dm.g;
   if ((int)blockIdx.z < n_long) {
     const int unit = (int)blockIdx.z * (int)gridDim.x + (int)blockIdx.x, rank = unit / rows;
-    const int b = long_sequence(dm, a, parts, kv, rank);
-    if (b >= 0) merge_row<D>(dm, a, part, parts, n_slots, unit - rank * rows, kv, b);   // block-uniform
+    const int b = long_sequence<OWN>(dm, a, parts, kv, rank);
+    if (b >= 0) merge_row<D, OWN>(dm, a, part, parts, n_slots, unit - rank * rows, kv, b);   // block-uniform
     return;
   }
   const int r = (int)blockIdx.x * (kPdThreads / TPR) + (int)threadIdx.x / TPR, c4 = threadIdx.x % TPR, b = (int)blockIdx.z - n_long;
   if (r >= rows) return;
-  const int C = a.chunk_lens == nullptr ? dm.C : max(min(a.chunk_lens[b], dm.C), 0);
+  const int C = pd_live<OWN>(dm, a, b);
   const u32x2 of = parts[kv * dm.b + b];   // (a sequence without a token in this chunk has none, and uses none)
   if (n_long > 0 && C > 0 && (int)of[1] > kPdFew) return;
   const int tok = r / dm.g, h = kv * dm.g + r % dm.g;
@@ -604,21 +620,22 @@ static int pd_slots(const Dims& dm) { return (kPdMaxSlots + dm.n_kv - 1) / dm.n_
 static size_t pd_part_floats(const Dims& dm) { return (size_t)dm.n_kv * (pd_slots(dm) + dm.b) * 32 * (dm.d + 2); }
 size_t paged_decode_ws_floats(const Dims& dm) { return pd_part_floats(dm) + (size_t)2 * dm.n_kv * dm.b; }
 
-hipError_t launch_paged_decode(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st) {
+hipError_t launch_paged_decode(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st, bool own) {
   const int n_slots = pd_slots(dm);
   u32x2* parts = reinterpret_cast<u32x2*>(part + pd_part_floats(dm));
-  const long long tiles = ((long long)attended_cap(dm, a.k_idx != nullptr) + dm.C + kPdTile - 1) / kPdTile;
+  const long long tiles = ((long long)attended_cap(dm, a.k_idx != nullptr) + (own ? dm.C : 0) + kPdTile - 1) / kPdTile;
   if (dm.b * tiles >= 1ll << 31) return hipErrorInvalidValue;   // (refused by the entry point)
   const long long most = dm.b * ((tiles + kPdWaves - 1) / kPdWaves);   // (blocks that short lists leave without work)
-  auto launch = [&](auto d, auto eight_bit, auto is_list) -> hipError_t {
+  auto launch = [&](auto d, auto eight_bit, auto is_list, auto own_rows) -> hipError_t {
     constexpr int D = decltype(d)::value;
-    constexpr bool FP8 = decltype(eight_bit)::value, LIST = decltype(is_list)::value;
+    constexpr bool FP8 = decltype(eight_bit)::value, LIST = decltype(is_list)::value, OWN = decltype(own_rows)::value;
     constexpr size_t lds = PdCfg<D, FP8>::kLdsBytes;
     static std::atomic<uint64_t> lds_done{0};
-    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&paged_decode<D, FP8, LIST>), lds, lds_done);
+    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&paged_decode<D, FP8, LIST, OWN>), lds, lds_done);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((paged_decode<D, FP8, LIST>), dim3(n_slots < most ? n_slots : (int)most, dm.n_kv), dim3(kPdThreads), lds, st, dm, a,
-                       part, parts, n_slots);
+    if (most > 0)   // (states of no length at all leave the merge alone, which writes the rows that see nothing)
+      hipLaunchKernelGGL((paged_decode<D, FP8, LIST, OWN>), dim3(n_slots < most ? n_slots : (int)most, dm.n_kv), dim3(kPdThreads), lds, st,
+                         dm, a, part, parts, n_slots);
     const int rows = dm.C * dm.g, of_block = kPdThreads / (D / 4);
     // partials of a sequence: at most those of the longest list there can be; on the mean one more than its share of the blocks
     const long long of_list = (tiles + kPdWaves - 1) / kPdWaves, of_batch = n_slots / dm.b + 1;
@@ -628,10 +645,10 @@ hipError_t launch_paged_decode(const Dims& dm, bool fp8, const PagedArgs& a, flo
       const int blocks = (rows + of_block - 1) / of_block, most_long = of_list < kPdFew || n_slots <= kPdFew ? 0 : n_slots / (kPdFew - 1);
       int n_long = ((most_long < dm.b ? most_long : dm.b) * rows + blocks - 1) / blocks;
       if (n_long + dm.b > 65535) n_long = 0;   // (layers of a grid)
-      hipLaunchKernelGGL((paged_decode_merge_few<D>), dim3(blocks, dm.n_kv, n_long + dm.b), dim3(kPdThreads), 0, st, dm, a, part, parts,
+      hipLaunchKernelGGL((paged_decode_merge_few<D, OWN>), dim3(blocks, dm.n_kv, n_long + dm.b), dim3(kPdThreads), 0, st, dm, a, part, parts,
                          n_slots, n_long);
     } else {
-      hipLaunchKernelGGL((paged_decode_merge<D>), dim3(rows, dm.n_kv, dm.b), dim3(kPdThreads), 0, st, dm, a, part, parts, n_slots);
+      hipLaunchKernelGGL((paged_decode_merge<D, OWN>), dim3(rows, dm.n_kv, dm.b), dim3(kPdThreads), 0, st, dm, a, part, parts, n_slots);
     }
     return hipGetLastError();
   };
@@ -640,7 +657,8 @@ hipError_t launch_paged_decode(const Dims& dm, bool fp8, const PagedArgs& a, flo
   using d64 = std::integral_constant<int, 64>;
   using d128 = std::integral_constant<int, 128>;
   auto with_list = [&](auto d, auto eight_bit) {
-    return a.k_idx != nullptr ? launch(d, eight_bit, true_type{}) : launch(d, eight_bit, false_type{});
+    if (!own) return launch(d, eight_bit, false_type{}, false_type{});   // (cross attention takes no lists)
+    return a.k_idx != nullptr ? launch(d, eight_bit, true_type{}, true_type{}) : launch(d, eight_bit, false_type{}, true_type{});
   };
   if (dm.d == 64) return fp8 ? with_list(d64{}, true_type{}) : with_list(d64{}, false_type{});
   return fp8 ? with_list(d128{}, true_type{}) : with_list(d128{}, false_type{});
