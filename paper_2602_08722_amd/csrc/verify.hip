@@ -5,8 +5,9 @@
 // (p_a, should nothing be left of it), else p_a.  Sums are in 64 bits: a token's part of that line is as narrow as its probability.
 //
 // Bound by memory where there are many sequences (two rows of the vocabulary each), by a chain of fetches where there are few (tokens, their
-// probabilities, the rows).  Every block works out `a` for itself.  verify_parts leaves the sums of tiles of kVfTile entries,
-// verify_pick finds the tile and the token in it.
+// probabilities, the rows).  Lanes take neighbouring pieces of 16 bytes, wherever a row starts (an odd vocabulary's rows are aligned to an
+// element), and a wave a run of neighbouring entries: the sums of whole waves say which one the random number points into, and that one
+// alone adds up its entries in order.
 #include <type_traits>
 
 #include "common.hip.h"
@@ -14,38 +15,47 @@
 
 namespace quoka {
 
-constexpr int kVfThreads = 256, kVfRun = 16, kVfTile = kVfThreads * kVfRun;   // entries of a thread, of a tile
-
-__device__ __forceinline__ double wave64_sum(double x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, kWave);
-  return x;
+// Sums over the wave's lanes, by moves between neighbouring lanes as in common.hip.h (through LDS, a step takes several times as long).
+__device__ __forceinline__ double lane_of(double x, int lane) {
+  const unsigned long long u = __double_as_longlong(x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)u, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), lane);
+  return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
+}
+template <int CTRL, int ROW_MASK = 0xF>
+__device__ __forceinline__ double plus_lane(double x) {
+  const unsigned long long u = __double_as_longlong(x);
+  const uint32_t lo = dpp_take<CTRL, ROW_MASK>(0u, (uint32_t)u), hi = dpp_take<CTRL, ROW_MASK>(0u, (uint32_t)(u >> 32));
+  return x + __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
 }
 __device__ __forceinline__ double wave_incl_scan(double x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const double y = __shfl_up(x, o, kWave);
-    if (lane >= o) x += y;
-  }
-  return x;
+  x = plus_lane<0x111>(x);
+  x = plus_lane<0x112>(x);
+  x = plus_lane<0x114>(x);
+  x = plus_lane<0x118>(x);
+  x = plus_lane<0x142, 0xA>(x);
+  return plus_lane<0x143, 0xC>(x);
 }
+__device__ __forceinline__ double last_lane(double x) { return lane_of(x, 63); }
+__device__ __forceinline__ double wave64_sum(double x) { return last_lane(wave_incl_scan(x)); }
 
 // What an entry weighs: nothing unless it is a positive number.
 __device__ __forceinline__ double weight_of(double x) { return x > 0.0 && x < (double)INFINITY ? x : 0.0; }
 
-// Accepted tokens of sequence b.  Every wave works it out for itself, 64 tokens at a time.
+__device__ __forceinline__ int drafted(const VerifyArgs& a, int b) {
+  return a.draft_lens == nullptr ? a.n : min(max(a.draft_lens[b], 0), a.n);
+}
+
+// Accepted tokens of sequence b, n of which are drafted.  Every wave works it out for itself, 64 tokens at a time.
 template <typename T>
-__device__ __forceinline__ int accepted(const VerifyArgs& a, int b) {
+__device__ __forceinline__ int accepted(const VerifyArgs& a, int b, int n) {
   const int lane = threadIdx.x & 63;
-  const int n = a.draft_lens == nullptr ? a.n : min(max(a.draft_lens[b], 0), a.n);
   for (int i0 = 0; i0 < n; i0 += kWave) {
     const int i = i0 + lane;
     bool good = false;
     if (i < n) {
       const int x = a.tokens[(long long)b * a.n + i];
+      const double u = a.uniform[(long long)b * (a.n + 1) + i];
       if (x >= 0 && x < a.V) {
-        const double u = a.uniform[(long long)b * (a.n + 1) + i];
         const double p = Elem<T>::load1(static_cast<const T*>(a.target) + b * a.ts[0] + i * a.ts[1] + x);
         const double q = a.draft == nullptr ? 1.0 : Elem<T>::load1(static_cast<const T*>(a.draft) + b * a.ds[0] + i * a.ds[1] + x);
         good = u * q < p;
@@ -64,8 +74,7 @@ struct VfRows {
   int x;            // the refused token, whose weight loses 1 (-1: none)
 };
 template <typename T>
-__device__ __forceinline__ VfRows<T> rows_of(const VerifyArgs& a, int b, int acc) {
-  const int n = a.draft_lens == nullptr ? a.n : min(max(a.draft_lens[b], 0), a.n);
+__device__ __forceinline__ VfRows<T> rows_of(const VerifyArgs& a, int b, int n, int acc) {
   VfRows<T> r;
   r.p = static_cast<const T*>(a.target) + b * a.ts[0] + acc * a.ts[1];
   r.q = nullptr;
@@ -77,134 +86,216 @@ __device__ __forceinline__ VfRows<T> rows_of(const VerifyArgs& a, int b, int acc
   return r;
 }
 
-// Entries v0 .. v0 + kVfRun - 1: `left` what remains of p, `all` p itself.
+// 16 bytes of a row, at an element's alignment.
 template <typename T>
-__device__ __forceinline__ void weights(const VfRows<T>& r, int V, int v0, double (&left)[kVfRun], double (&all)[kVfRun]) {
-  float p[kVfRun], q[kVfRun];
-#pragma unroll
-  for (int e = 0; e < kVfRun; ++e) {
-    p[e] = v0 + e < V ? Elem<T>::load1(r.p + v0 + e) : 0.f;
-    q[e] = r.q != nullptr && v0 + e < V ? Elem<T>::load1(r.q + v0 + e) : v0 + e == r.x ? 1.f : 0.f;
-  }
-#pragma unroll
-  for (int e = 0; e < kVfRun; ++e) {
-    all[e] = weight_of((double)p[e]);
-    left[e] = weight_of((double)p[e] - (double)q[e]);
-  }
-}
-
-// parts: [b, tiles] sums of what is left and of p.
-template <typename T>
-__global__ __launch_bounds__(kVfThreads) void verify_parts(VerifyArgs a, double2* __restrict__ parts) {
-  __shared__ double2 of_wave[kVfThreads / kWave];
-  const int b = blockIdx.y, tid = threadIdx.x;
-  const VfRows<T> r = rows_of<T>(a, b, accepted<T>(a, b));
-  double left[kVfRun], all[kVfRun], sl = 0.0, sa = 0.0;
-  weights<T>(r, a.V, (int)blockIdx.x * kVfTile + tid * kVfRun, left, all);
-#pragma unroll
-  for (int e = 0; e < kVfRun; ++e) {
-    sl += left[e];
-    sa += all[e];
-  }
-  sl = wave64_sum(sl);
-  sa = wave64_sum(sa);
-  if ((tid & 63) == 0) of_wave[tid >> 6] = make_double2(sl, sa);
-  __syncthreads();
-  if (tid != 0) return;
-#pragma unroll
-  for (int w = 1; w < kVfThreads / kWave; ++w) {
-    sl += of_wave[w].x;
-    sa += of_wave[w].y;
-  }
-  parts[(size_t)b * gridDim.x + blockIdx.x] = make_double2(sl, sa);
-}
-
-template <typename T>
-__global__ __launch_bounds__(kVfThreads) void verify_pick(VerifyArgs a, const double2* __restrict__ parts, int tiles) {
-  __shared__ double of_wave[kVfThreads / kWave];
-  __shared__ int first_of[kVfThreads / kWave], last_of[kVfThreads / kWave];
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int acc = accepted<T>(a, b);
-  const VfRows<T> r = rows_of<T>(a, b, acc);
-  // every wave: the sums of the whole row, then the tile that the random number points into
-  const double2* mine = parts + (size_t)b * tiles;
-  double sl = 0.0, sa = 0.0;
-  for (int t = lane; t < tiles; t += kWave) {
-    sl += mine[t].x;
-    sa += mine[t].y;
-  }
-  const bool use_left = wave64_sum(sl) > 0.0;
-  (void)sa;
-  auto part_of = [&](int t) { return t < tiles ? use_left ? mine[t].x : mine[t].y : 0.0; };
-  double total = 0.0;
-  for (int t0 = 0; t0 < tiles; t0 += kWave) total += __shfl(wave_incl_scan(part_of(t0 + lane)), 63, kWave);
-  const float u = fminf(fmaxf(a.uniform[(long long)b * (a.n + 1) + a.n], 0.f), 1.f - 0x1p-24f);
-  const double point = (double)u * total;
-  double before = 0.0;
-  int tile = -1;
-  for (int t0 = 0; t0 < tiles && tile < 0; t0 += kWave) {
-    const double incl = wave_incl_scan(part_of(t0 + lane));
-    const unsigned long long hit = __builtin_amdgcn_ballot_w64(before + incl > point);
-    if (hit != 0) {
-      const int at = (int)__builtin_ctzll(hit);
-      tile = t0 + at;
-      before += __shfl(incl, at, kWave) - __shfl(part_of(t0 + lane), at, kWave);
+struct Piece {
+  static constexpr int N = 16 / sizeof(T);
+  typedef T vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+  vec x;
+  __device__ __forceinline__ void load(const T* row, int v0, int V) {   // entries past V are zeros
+    if (v0 + N <= V) {
+      x = *reinterpret_cast<const vec*>(row + v0);
     } else {
-      before += __shfl(incl, 63, kWave);
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = v0 + e < V ? row[v0 + e] : T(0);
     }
   }
-  int y = -1;
-  if (tile >= 0) {   // block-uniform (-1: nothing has any weight)
-    double left[kVfRun], all[kVfRun], s = 0.0;
-    const int v0 = tile * kVfTile + tid * kVfRun;
-    weights<T>(r, a.V, v0, left, all);
+  __device__ __forceinline__ double at(int e) const {
+    if constexpr (sizeof(T) == 4) return (double)x[e];
+    else return (double)bf16_bits_to_f32(x[e]);
+  }
+};
+
+// J pieces of a lane, 64 lanes' pieces one behind the other: N * 64 * J neighbouring entries of a wave, from v0 on (the lane's own start in it).
+template <typename T, int J>
+struct Run {
+  static constexpr int N = Piece<T>::N, kEntries = N * kWave * J;
+  Piece<T> p[J], q[J];
+  int x;   // place of the refused token among the wave's entries, as seen from this lane (negative or large: elsewhere)
+  bool has_q;
+  __device__ __forceinline__ void load(const VfRows<T>& r, int first, int V) {
+    const int v0 = first + (int)(threadIdx.x & 63) * N;
+    has_q = r.q != nullptr;
+    x = r.x < 0 ? -1 : r.x - v0;
 #pragma unroll
-    for (int e = 0; e < kVfRun; ++e) {
-      if (!use_left) left[e] = all[e];
-      s += left[e];
+    for (int j = 0; j < J; ++j) p[j].load(r.p, v0 + j * N * kWave, V);
+    if (has_q) {   // (the same for all lanes)
+#pragma unroll
+      for (int j = 0; j < J; ++j) q[j].load(r.q, v0 + j * N * kWave, V);
     }
-    const double incl = wave_incl_scan(s);
-    if (lane == 63) of_wave[w] = incl;
-    __syncthreads();
-    double run = before + (incl - s);
-    for (int i = 0; i < w; ++i) run += of_wave[i];
-    int first = INT32_MAX, last = -1;
+  }
+  __device__ __forceinline__ double all(int j, int e) const { return weight_of(p[j].at(e)); }
+  __device__ __forceinline__ double left(int j, int e) const {   // what remains of p
+    return weight_of(p[j].at(e) - (has_q ? q[j].at(e) : x == j * N * kWave + e ? 1.0 : 0.0));
+  }
+  __device__ __forceinline__ double weight(bool use_left, int j, int e) const { return use_left ? left(j, e) : all(j, e); }
+
+  // The lowest entry of positive weight behind which `before` and the entries up to it are more than `point`; should there be none, the last
+  // one of positive weight (sums of two orders may leave the point a rounding past the end); as a place in the row, -1: nothing weighs.
+  __device__ __forceinline__ int find(bool use_left, double before, double point, int first) const {
+    const int lane = threadIdx.x & 63;
+    double w[J][N], s[J], incl[J];
 #pragma unroll
-    for (int e = 0; e < kVfRun; ++e) {
-      run += left[e];
-      if (left[e] > 0.0) {
-        last = v0 + e;
-        if (run > point && first == INT32_MAX) first = v0 + e;
+    for (int j = 0; j < J; ++j) {
+      s[j] = 0.0;
+#pragma unroll
+      for (int e = 0; e < N; ++e) s[j] += w[j][e] = weight(use_left, j, e);
+      incl[j] = wave_incl_scan(s[j]);
+    }
+    int last = -1;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      double run = before + (incl[j] - s[j]);
+      int hit = -1, mine = -1;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        run += w[j][e];
+        if (w[j][e] > 0.0) {
+          mine = e;
+          if (run > point && hit < 0) hit = e;
+        }
       }
+      const int at = first + j * N * kWave + lane * N;
+      const unsigned long long hits = __builtin_amdgcn_ballot_w64(hit >= 0);
+      if (hits != 0) return __builtin_amdgcn_readlane(at + hit, (int)__builtin_ctzll(hits));
+      const unsigned long long some = __builtin_amdgcn_ballot_w64(mine >= 0);
+      if (some != 0) last = __builtin_amdgcn_readlane(at + mine, 63 - (int)__builtin_clzll(some));
+      before += last_lane(incl[j]);
     }
-    first = (int)wave_min_u32((uint32_t)first);
-    last = (int)wave_max_u32((uint32_t)(last + 1)) - 1;
-    if (lane == 0) {
-      first_of[w] = first;
-      last_of[w] = last;
-    }
-    __syncthreads();
-    for (int i = 0; i < kVfThreads / kWave; ++i) {
-      first = min(first, first_of[i]);
-      last = max(last, last_of[i]);
-    }
-    y = first != INT32_MAX ? first : last;   // (sums of two orders may leave the point a rounding past the tile's end)
+    return last;
   }
-  if (tid == 0) a.n_accepted[b] = acc;
-  for (int i = tid; i <= a.n; i += kVfThreads)
+};
+
+// The random number, cut to [0, 1).
+__device__ __forceinline__ double draw_of(const VerifyArgs& a, int b) {
+  return (double)fminf(fmaxf(a.uniform[(long long)b * (a.n + 1) + a.n], 0.f), 1.f - 0x1p-24f);
+}
+__device__ __forceinline__ void put_tokens(const VerifyArgs& a, int b, int acc, int y, int lane) {   // one wave
+  for (int i = lane; i <= a.n; i += kWave)
     a.tokens_out[(long long)b * (a.n + 1) + i] = i < acc ? a.tokens[(long long)b * a.n + i] : i == acc ? y : -1;
 }
 
-static int vf_tiles(int vocab) { return (vocab + kVfTile - 1) / kVfTile; }
+// Two launches: the sums of parts of kVfPart entries, a wave each; then the part that the random number points into, and the token in it.
+constexpr int kVfThreads = 256, kVfPart = 1024;
 
-size_t verify_ws_bytes(int batch, int vocab) { return (size_t)batch * vf_tiles(vocab) * sizeof(double2); }
+// sums: [b, parts] of what is left and of p
+template <typename T>
+__global__ __launch_bounds__(kVfThreads) void verify_parts(VerifyArgs a, double2* __restrict__ sums, int parts) {
+  constexpr int J = kVfPart / (Piece<T>::N * kWave);
+  const int b = blockIdx.y, part = (int)blockIdx.x * (kVfThreads / kWave) + (int)(threadIdx.x >> 6);
+  if (part >= parts) return;
+  const int n = drafted(a, b), acc = accepted<T>(a, b, n);
+  if (part == 0 && (threadIdx.x & 63) == 0) a.n_accepted[b] = acc;   // (what the next launch goes by, too)
+  Run<T, J> run;
+  run.load(rows_of<T>(a, b, n, acc), part * kVfPart, a.V);
+  double left = 0.0, all = 0.0;
+#pragma unroll
+  for (int j = 0; j < J; ++j)
+#pragma unroll
+    for (int e = 0; e < Piece<T>::N; ++e) {
+      left += run.left(j, e);
+      all += run.all(j, e);
+    }
+  left = wave64_sum(left);
+  all = wave64_sum(all);
+  if ((threadIdx.x & 63) == 0) sums[(size_t)b * parts + part] = make_double2(left, all);
+}
+
+// A wave a sequence; a lane has K neighbouring sums at a time.
+template <typename T>
+__global__ __launch_bounds__(kWave) void verify_pick(VerifyArgs a, const double2* __restrict__ sums, int parts) {
+  constexpr int J = kVfPart / (Piece<T>::N * kWave), K = 4;
+  const int b = blockIdx.x, lane = threadIdx.x;
+  const double2* mine = sums + (size_t)b * parts;
+  double2 s[K];
+  auto load = [&](int t0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int t = t0 + lane * K + k;
+      s[k] = t < parts ? mine[t] : make_double2(0.0, 0.0);
+    }
+  };
+  load(0);
+  const double u = draw_of(a, b);
+  const int n = drafted(a, b), acc = min(max(a.n_accepted[b], 0), n);
+  const VfRows<T> r = rows_of<T>(a, b, n, acc);
+  double left = 0.0, all = 0.0;
+  for (int t0 = 0; t0 < parts; t0 += K * kWave) {
+    if (t0 > 0) load(t0);
+    double l = 0.0, p = 0.0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      l += s[k].x;
+      p += s[k].y;
+    }
+    left += last_lane(wave_incl_scan(l));   // (in the order of the search below: the line's end is its last sum)
+    all += last_lane(wave_incl_scan(p));
+  }
+  const bool use_left = left > 0.0;
+  const double point = u * (use_left ? left : all);
+  double before = 0.0;
+  int y = -1;
+  if (left > 0.0 || all > 0.0) {   // (the same for all lanes)
+    int part = -1, last = -1;
+    double before_last = 0.0;
+    for (int t0 = 0; t0 < parts && part < 0; t0 += K * kWave) {
+      if (parts > K * kWave) load(t0);
+      double w[K], sum = 0.0;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        w[k] = use_left ? s[k].x : s[k].y;
+        sum += w[k];
+      }
+      const double incl = wave_incl_scan(sum);
+      double run = before + (incl - sum), at = run, at_some = run;
+      int hit = -1, some = -1;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        if (w[k] > 0.0) {
+          some = k;
+          at_some = run;
+          if (hit < 0 && run + w[k] > point) {
+            hit = k;
+            at = run;
+          }
+        }
+        run += w[k];
+      }
+      const unsigned long long hits = __builtin_amdgcn_ballot_w64(hit >= 0), any = __builtin_amdgcn_ballot_w64(some >= 0);
+      if (hits != 0) {
+        const int of = (int)__builtin_ctzll(hits);
+        part = t0 + of * K + __builtin_amdgcn_readlane(hit, of);
+        before = lane_of(at, of);
+      } else {
+        if (any != 0) {
+          const int of = 63 - (int)__builtin_clzll(any);
+          last = t0 + of * K + __builtin_amdgcn_readlane(some, of);
+          before_last = lane_of(at_some, of);
+        }
+        before += last_lane(incl);
+      }
+    }
+    if (part < 0) {
+      part = last;
+      before = before_last;
+    }
+    Run<T, J> run;
+    run.load(r, part * kVfPart, a.V);
+    y = run.find(use_left, before, point, part * kVfPart);
+  }
+  put_tokens(a, b, acc, y, lane);
+}
+
+static int vf_parts(int vocab) { return (vocab + kVfPart - 1) / kVfPart; }
+
+size_t verify_ws_bytes(int batch, int vocab) { return (size_t)batch * vf_parts(vocab) * sizeof(double2); }
 
 hipError_t launch_verify(const VerifyArgs& a, int dtype, void* ws, hipStream_t st) {
   auto launch = [&](auto one) {
     using T = decltype(one);
-    const int tiles = vf_tiles(a.V);
-    hipLaunchKernelGGL((verify_parts<T>), dim3(tiles, a.b), dim3(kVfThreads), 0, st, a, static_cast<double2*>(ws));
-    hipLaunchKernelGGL((verify_pick<T>), dim3(a.b), dim3(kVfThreads), 0, st, a, static_cast<const double2*>(ws), tiles);
+    const int parts = vf_parts(a.V), waves = kVfThreads / kWave;
+    hipLaunchKernelGGL((verify_parts<T>), dim3((parts + waves - 1) / waves, a.b), dim3(kVfThreads), 0, st, a, static_cast<double2*>(ws), parts);
+    hipLaunchKernelGGL((verify_pick<T>), dim3(a.b), dim3(kWave), 0, st, a, static_cast<const double2*>(ws), parts);
     return hipGetLastError();
   };
   return dtype == QUOKA_BF16 ? launch(uint16_t{}) : launch(float{});

@@ -4,6 +4,7 @@
     python3 profile_summary.py trace <workload> <rocprofv3 output dir> <bench.py stdout file>
     python3 profile_summary.py cases <dir holding one rocprofv3 output dir per case, named like it>
     python3 profile_summary.py operators <the same, of perf/operators.py's cases>
+    python3 profile_summary.py more_operators <the same, of perf/more_operators.py's cases>
     python3 profile_summary.py traffic <workload> <dir holding one rocprofv3 output dir per pass>
     python3 profile_summary.py counters <title> <kernel substring> <rocprofv3 output dir> [<dir> ...]
 
@@ -86,9 +87,9 @@ def trace(workload, out_dir, bench_log):
 
 
 def cases(base, module="cases"):
-    """Kernel traces of perf/cases.py's (perf/operators.py's) cases: every pass launches the same kernels, the first tenth is left out."""
-    own = "c.own = True; " if module == "operators" else ""
-    passes = 1000 if module == "operators" else 40   # (the clock settles over the first 10 - 20 ms of a busy card)
+    """Kernel traces of perf/cases.py's (perf/operators.py's, perf/more_operators.py's) cases: every pass launches the same kernels, the first tenth is left out."""
+    own = "c.own = True; " if module != "cases" else ""
+    passes = 1000 if module != "cases" else 40   # (the clock settles over the first 10 - 20 ms of a busy card)
     out = [f"# rocprofv3 kernel traces of the timed cases (perf/{module}.py), one pass after another", "",
            "Commands (run from /tmp with TMPDIR=/tmp, repository root = $R, one run per case):",
            "    rocprofv3 --kernel-trace --stats --output-format csv -d <base>/<case> -o kt -- python3 -c \"import sys, torch; "
@@ -226,7 +227,7 @@ def main():
     mode = sys.argv[1]
     if mode == "trace" and len(sys.argv) == 5:
         trace(sys.argv[2], sys.argv[3], sys.argv[4])
-    elif mode in ("cases", "operators") and len(sys.argv) == 3:
+    elif mode in ("cases", "operators", "more_operators") and len(sys.argv) == 3:
         cases(sys.argv[2], mode)
     elif mode == "traffic" and len(sys.argv) == 4:
         traffic(sys.argv[2], sys.argv[3])
