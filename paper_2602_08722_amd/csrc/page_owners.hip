@@ -3,14 +3,16 @@
 //
 // Pages are handed out lowest first, in the order of the sequences and of their entries, so that a call's result depends on nothing but its
 // arguments: counts are changed by integer atomics, whose order does not matter, and the rank of a free page among the free ones names the
-// entry that gets it.  Three launches, each of which uses what the one before has completed: entries that go or are shared (a wave a
-// sequence), free pages counted (a tile of pages a block) beside the sum of what the sequences lack, free pages to entries.
+// entry that gets it.  Three steps, each of which uses what the one before has completed: entries that go or are shared, free pages counted
+// beside the sum of what the sequences lack, free pages to entries.  Small pools and batches take them in one launch of one block, others in
+// three launches (a block a sequence, a tile of pages a block).
 #include "common.hip.h"
 #include "kernels.h"
 
 namespace quoka {
 
 constexpr int kOwThreads = 256, kOwRun = 16, kOwTile = kOwThreads * kOwRun;   // pages of a thread, of a tile
+constexpr int kOwBatch = 4096;   // sequences whose sums a block keeps in LDS
 
 // What a call leaves for its later launches.
 struct OwWs {
@@ -31,51 +33,100 @@ __device__ __forceinline__ void add_holder(const Owners& o, int32_t page, int by
 }
 __device__ __forceinline__ int held_by(const Owners& o, int b) { return min(max(o.held[b], 0), o.max_pages); }
 
-__global__ __launch_bounds__(kOwThreads) void owners_cut(Owners o, const int32_t* __restrict__ lens, OwWs ws) {
-  const int b = (int)blockIdx.x * (kOwThreads / kWave) + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (b >= o.b) return;
+// What sequence b holds after a cut, and lacks; `lane` of `width` threads that share its entries.
+__device__ __forceinline__ void cut_sequence(const Owners& o, const int32_t* __restrict__ lens, int b, int lane, int width, int& start, int& need) {
   const int len = lens[b], had = held_by(o, b);
-  const int n = len <= 0 ? 0 : min(((len - 1) >> o.shift) + 1, o.max_pages), stay = min(had, n);
+  const int n = len <= 0 ? 0 : min(((len - 1) >> o.shift) + 1, o.max_pages);
   int32_t* row = o.table + (long long)b * o.max_pages;
-  for (int e = n + lane; e < had; e += kWave) {
+  start = min(had, n);
+  need = n - start;
+  for (int e = n + lane; e < had; e += width) {
     add_holder(o, row[e], -1);
     row[e] = -1;
   }
-  if (lane == 0) {
-    ws.start[b] = stay;
-    ws.need[b] = n - stay;
-  }
 }
 
-__global__ __launch_bounds__(kOwThreads) void owners_share(Owners from, Owners o, ForkArgs f, OwWs ws) {
-  const int b = (int)blockIdx.x * (kOwThreads / kWave) + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (b >= o.b) return;
+// Likewise for a child that goes on from its parent.
+__device__ __forceinline__ void share_sequence(const Owners& from, const Owners& o, const ForkArgs& f, int b, int lane, int width, int& start,
+                                               int& need) {
   const int had = held_by(o, b), parent = f.parents[b];
   const bool has_parent = (uint32_t)parent < (uint32_t)from.b;
   // (at most what the parent holds and the child has room for: 64 bits)
   long long len = 0;
   if (has_parent) len = min((long long)max(f.lens[parent], 0), (long long)min(held_by(from, parent), o.max_pages) << o.shift);
-  const int whole = (int)(len >> o.shift), need = (len & ((1 << o.shift) - 1)) != 0 ? 1 : 0;
+  const int whole = (int)(len >> o.shift);
+  start = whole;
+  need = (len & ((1 << o.shift) - 1)) != 0 ? 1 : 0;
   int32_t* row = o.table + (long long)b * o.max_pages;
   const int32_t* theirs = from.table + (long long)(has_parent ? parent : 0) * from.max_pages;
-  for (int e = lane; e < max(whole, had); e += kWave) {
-    if (e < had) add_holder(o, row[e], -1);
-    int32_t page = -1;
-    if (e < whole) {
-      page = theirs[e];
-      add_holder(o, page, 1);
-    }
+  for (int e = lane; e < max(whole, had); e += width) {
+    const int32_t old = e < had ? row[e] : -1, page = e < whole ? theirs[e] : -1;
+    if (e < had && old == page) continue;   // (shared as it was: beams that swap between two tables keep most of their pages)
+    add_holder(o, old, -1);
+    add_holder(o, page, 1);
     row[e] = page;
   }
   if (lane == 0) {
-    ws.start[b] = whole;
-    ws.need[b] = need;
     f.first[b] = whole << o.shift;
     f.child_lens[b] = (int)len;
   }
 }
 
-__device__ __forceinline__ bool is_free(const Owners& o, int page) { return page < o.n_pages && o.ref[page] <= 0; }
+__global__ __launch_bounds__(kOwThreads) void owners_cut(Owners o, const int32_t* __restrict__ lens, OwWs ws) {
+  const int b = blockIdx.x;
+  int start, need;
+  cut_sequence(o, lens, b, threadIdx.x, kOwThreads, start, need);
+  if (threadIdx.x == 0) {
+    ws.start[b] = start;
+    ws.need[b] = need;
+  }
+}
+
+__global__ __launch_bounds__(kOwThreads) void owners_share(Owners from, Owners o, ForkArgs f, OwWs ws) {
+  const int b = blockIdx.x;
+  int start, need;
+  share_sequence(from, o, f, b, threadIdx.x, kOwThreads, start, need);
+  if (threadIdx.x == 0) {
+    ws.start[b] = start;
+    ws.need[b] = need;
+  }
+}
+
+// Which of the pages page0 .. page0 + kOwRun - 1 are free.
+__device__ __forceinline__ uint32_t free_pages(const Owners& o, int page0) {
+  typedef int32_t four __attribute__((ext_vector_type(4), aligned(4)));
+  uint32_t is = 0;
+  if (page0 + kOwRun <= o.n_pages) {
+    four r[kOwRun / 4];
+#pragma unroll
+    for (int i = 0; i < kOwRun / 4; ++i) r[i] = *reinterpret_cast<const four*>(o.ref + page0 + 4 * i);
+#pragma unroll
+    for (int i = 0; i < kOwRun; ++i) is |= r[i / 4][i % 4] <= 0 ? 1u << i : 0u;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kOwRun; ++i) is |= page0 + i < o.n_pages && o.ref[min(page0 + i, o.n_pages - 1)] <= 0 ? 1u << i : 0u;
+  }
+  return is;
+}
+
+// Free pages `is` of page0 .. page0 + kOwRun - 1, the first of which is number `rank` of all free ones, to the entries that want them.
+// prefix [b + 1], start [b]: what the sequences before each one lack, and its entries in use.
+template <typename P, typename S>
+__device__ __forceinline__ void give_pages(const Owners& o, int page0, uint32_t is, uint32_t rank, uint32_t wanted, const P* prefix, const S* start) {
+  if (is == 0 || rank >= wanted) return;
+  int lo = 0, hi = o.b - 1;   // the last sequence whose first rank is not above `rank` (one that wants none has the next one's)
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if ((uint32_t)prefix[mid] <= rank) lo = mid;
+    else hi = mid - 1;
+  }
+  for (; is != 0 && rank < wanted; is &= is - 1, ++rank) {
+    while ((uint32_t)prefix[lo + 1] <= rank) ++lo;   // (rank < wanted, the last of them)
+    const int page = page0 + __builtin_ctz(is);
+    o.ref[page] = 1;
+    o.table[(long long)lo * o.max_pages + (int)start[lo] + (int)(rank - (uint32_t)prefix[lo])] = page;
+  }
+}
 
 // The last block: the sums of what the sequences before each one lack.
 __global__ __launch_bounds__(kOwThreads) void owners_count(Owners o, OwWs ws) {
@@ -93,10 +144,7 @@ __global__ __launch_bounds__(kOwThreads) void owners_count(Owners o, OwWs ws) {
     if (tid == 0) ws.prefix[o.b] = (int32_t)before;
     return;
   }
-  uint32_t n = 0;
-#pragma unroll
-  for (int i = 0; i < kOwRun; ++i) n += is_free(o, (int)blockIdx.x * kOwTile + i * kOwThreads + tid) ? 1u : 0u;
-  block_excl_scan<kOwThreads>(n, scan, &total);
+  block_excl_scan<kOwThreads>((uint32_t)__popc(free_pages(o, (int)blockIdx.x * kOwTile + tid * kOwRun)), scan, &total);
   if (tid == 0) ws.counts[blockIdx.x] = (int32_t)total;
 }
 
@@ -119,25 +167,101 @@ __global__ __launch_bounds__(kOwThreads) void owners_take(Owners o, ForkArgs f, 
     return;
   }
   if (before >= wanted) return;   // block-uniform
-  uint32_t is = 0, total;
+  uint32_t total;
   const int page0 = (int)blockIdx.x * kOwTile + tid * kOwRun;
-#pragma unroll
-  for (int i = 0; i < kOwRun; ++i) is |= is_free(o, page0 + i) ? 1u << i : 0u;
-  uint32_t rank = before + block_excl_scan<kOwThreads>((uint32_t)__popc(is), scan, &total);
-  for (; is != 0 && rank < wanted; is &= is - 1, ++rank) {
-    const int page = page0 + __builtin_ctz(is);
-    int lo = 0, hi = o.b - 1;   // the last sequence whose first rank is not above `rank` (one that wants none has the next one's)
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) / 2;
-      if ((uint32_t)ws.prefix[mid] <= rank) lo = mid;
-      else hi = mid - 1;
+  const uint32_t is = free_pages(o, page0);
+  const uint32_t rank = before + block_excl_scan<kOwThreads>((uint32_t)__popc(is), scan, &total);
+  if (o.b <= kOwBatch) {   // (a search is some ten look-ups one after the other)
+    __shared__ int32_t prefix[kOwBatch + 1], start[kOwBatch];
+    for (int b = tid; b <= o.b; b += kOwThreads) {
+      prefix[b] = ws.prefix[b];
+      if (b < o.b) start[b] = ws.start[b];
     }
-    o.ref[page] = 1;
-    o.table[(long long)lo * o.max_pages + ws.start[lo] + (int)(rank - (uint32_t)ws.prefix[lo])] = page;
+    __syncthreads();
+    give_pages(o, page0, is, rank, wanted, prefix, start);
+  } else {
+    give_pages(o, page0, is, rank, wanted, ws.prefix, ws.start);
   }
 }
 
-static hipError_t launch_take(const Owners& o, const ForkArgs& f, const OwWs& w, int32_t* lacking, hipStream_t st) {
+// Free pages counted and handed out by one block.  A thread has the sequence of its number: `need` entries that want a page behind the
+// `start_of` ones in use.
+constexpr int kOsThreads = 1024;
+template <bool FORK>
+__device__ __forceinline__ void hand_out(const Owners& o, const ForkArgs& f, int start_of, int need, int32_t* lacking) {
+  __shared__ uint32_t scan[kOsThreads / kWave + 1];
+  __shared__ int32_t prefix[kOsThreads + 1], start[kOsThreads];
+  const int tid = threadIdx.x;
+  uint32_t wanted, total;
+  const uint32_t mine = block_excl_scan<kOsThreads>((uint32_t)need, scan, &wanted);
+  prefix[tid] = (int32_t)mine;   // (past the batch: `wanted`)
+  start[tid] = start_of;
+  if (tid == kOsThreads - 1) prefix[kOsThreads] = (int32_t)wanted;
+  __syncthreads();
+  uint32_t before = 0;
+  for (int page0 = tid * kOwRun; before < wanted && page0 - tid * kOwRun < o.n_pages; page0 += kOsThreads * kOwRun) {   // block-uniform
+    const uint32_t is = free_pages(o, page0);
+    const uint32_t rank = before + block_excl_scan<kOsThreads>((uint32_t)__popc(is), scan, &total);
+    give_pages(o, page0, is, rank, wanted, prefix, start);
+    before += total;
+  }
+  if (tid < o.b) {
+    const int got = min(max((int)(before - mine), 0), need);
+    o.held[tid] = start_of + got;
+    if (FORK && got < need) f.child_lens[tid] = f.first[tid];
+  }
+  if (tid == 0) *lacking = (int32_t)(wanted > before ? wanted - before : 0u);
+}
+
+// All of it in one block.  (Counts are first fetched when the atomics of the first step have reached them: no line of theirs can be in the
+// first-level cache before.)
+template <bool FORK>
+__global__ __launch_bounds__(kOsThreads) void owners_one(Owners from, Owners o, ForkArgs f, const int32_t* __restrict__ lens,
+                                                         int32_t* __restrict__ lacking) {
+  __shared__ int32_t starts[kOsThreads], needs[kOsThreads];
+  const int tid = threadIdx.x, lane = tid & 63;
+  for (int b = tid >> 6; b < o.b; b += kOsThreads / kWave) {   // a wave a sequence
+    int start, need;
+    if constexpr (FORK) share_sequence(from, o, f, b, lane, kWave, start, need);
+    else cut_sequence(o, lens, b, lane, kWave, start, need);
+    if (lane == 0) {
+      starts[b] = start;
+      needs[b] = need;
+    }
+  }
+  wait_vmcnt<0>();
+  __syncthreads();
+  hand_out<FORK>(o, f, tid < o.b ? starts[tid] : 0, tid < o.b ? needs[tid] : 0, lacking);
+}
+
+// The second and third step.
+template <bool FORK>
+__global__ __launch_bounds__(kOsThreads) void owners_rest(Owners o, ForkArgs f, OwWs ws, int32_t* __restrict__ lacking) {
+  const int b = min((int)threadIdx.x, o.b - 1);
+  const int start = ws.start[b], need = ws.need[b];
+  hand_out<FORK>(o, f, start, (int)threadIdx.x < o.b ? need : 0, lacking);
+}
+
+// Which launches: one block for all, its last two steps, or many blocks throughout.  Us a call over pools below and above 32768 pages; a resize by 40 tokens, one
+// that gives back or takes every page, a fork: 16 sequences of 260 pages 3.3 / 6.8, 5.5 / 8.5, 8.8 / 11.0; of 1004 pages 3.4 / 6.9, 12.8 / 9.1,
+// 10.4 / 11.8 (two steps in one block; all three 14.7); 64 of 254 4.7 / 7.6, 13.7 / 9.0, 9.4 / 11.0 (all three 16.1); 256 of 67 6.5 / 7.5, 14.5 /
+// 9.2, 11.4 / 11.2.  The step that a generated token takes is what counts, so a resize goes by it; the block's time grows by 0.7 us for
+// every 16384 pages that are looked through, that of the many not.
+struct OwPlan {
+  bool one, rest;
+};
+static OwPlan ow_plan(const Owners& o, bool fork) {
+  const bool small_pool = o.n_pages <= 32768;
+  const long long entries = (long long)o.b * o.max_pages;
+  return {small_pool && (fork ? o.b <= 64 && entries <= 8192 : o.b <= 128 && entries <= 16384), small_pool && o.b <= kOsThreads};
+}
+
+static hipError_t launch_take(const Owners& o, const ForkArgs& f, const OwWs& w, int32_t* lacking, bool fork, hipStream_t st) {
+  if (ow_plan(o, fork).rest) {
+    if (fork) hipLaunchKernelGGL((owners_rest<true>), dim3(1), dim3(kOsThreads), 0, st, o, f, w, lacking);
+    else hipLaunchKernelGGL((owners_rest<false>), dim3(1), dim3(kOsThreads), 0, st, o, f, w, lacking);
+    return hipGetLastError();
+  }
   const int tiles = ow_tiles(o.n_pages);
   hipLaunchKernelGGL(owners_count, dim3(tiles + 1), dim3(kOwThreads), 0, st, o, w);
   hipLaunchKernelGGL(owners_take, dim3(tiles + 1), dim3(kOwThreads), 0, st, o, f, w, lacking);
@@ -145,17 +269,23 @@ static hipError_t launch_take(const Owners& o, const ForkArgs& f, const OwWs& w,
 }
 
 hipError_t launch_pages_resize(const Owners& o, const int32_t* lens, int32_t* lacking, void* ws, hipStream_t st) {
+  if (ow_plan(o, false).one) {
+    hipLaunchKernelGGL((owners_one<false>), dim3(1), dim3(kOsThreads), 0, st, o, o, ForkArgs{}, lens, lacking);
+    return hipGetLastError();
+  }
   const OwWs w = ow_ws(o, ws);
-  constexpr int per_block = kOwThreads / kWave;
-  hipLaunchKernelGGL(owners_cut, dim3((o.b + per_block - 1) / per_block), dim3(kOwThreads), 0, st, o, lens, w);
-  return launch_take(o, ForkArgs{}, w, lacking, st);
+  hipLaunchKernelGGL(owners_cut, dim3(o.b), dim3(kOwThreads), 0, st, o, lens, w);
+  return launch_take(o, ForkArgs{}, w, lacking, false, st);
 }
 
 hipError_t launch_pages_fork(const Owners& from, const Owners& o, const ForkArgs& f, int32_t* lacking, void* ws, hipStream_t st) {
+  if (ow_plan(o, true).one) {
+    hipLaunchKernelGGL((owners_one<true>), dim3(1), dim3(kOsThreads), 0, st, from, o, f, nullptr, lacking);
+    return hipGetLastError();
+  }
   const OwWs w = ow_ws(o, ws);
-  constexpr int per_block = kOwThreads / kWave;
-  hipLaunchKernelGGL(owners_share, dim3((o.b + per_block - 1) / per_block), dim3(kOwThreads), 0, st, from, o, f, w);
-  return launch_take(o, f, w, lacking, st);
+  hipLaunchKernelGGL(owners_share, dim3(o.b), dim3(kOwThreads), 0, st, from, o, f, w);
+  return launch_take(o, f, w, lacking, true, st);
 }
 
 }  // namespace quoka
