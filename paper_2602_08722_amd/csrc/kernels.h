@@ -152,6 +152,9 @@ hipError_t launch_cross_attn_bf16(const Dims& dm, bool fp8, const PagedArgs& a, 
 // up to 32 query rows per KV head.  `own`: the chunk's own rows are attended, causally (else the cached ones alone)
 size_t paged_decode_ws_floats(const Dims& dm);
 hipError_t launch_paged_decode(const Dims& dm, bool fp8, const PagedArgs& a, float* part, hipStream_t st, bool own = true);
+// cross attention of as many, where a sequence's states are few enough for one block
+bool cross_few_applies(const Dims& dm);
+hipError_t launch_cross_few(const Dims& dm, bool fp8, const PagedArgs& a, hipStream_t st);
 size_t paged_attn_ws_floats(const Dims& dm, int dtype);
 hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float* part, hipStream_t st, bool own = true);
 

@@ -110,7 +110,8 @@ size_t paged_attn_ws_floats(const Dims& dm, int dtype) {
 
 hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float* part, hipStream_t st, bool own) {
   if (dtype == QUOKA_BF16) {
-    if (attn_decode_applies(dm)) return launch_paged_decode(dm, fp8, a, part, st, own);
+    if (attn_decode_applies(dm))
+      return !own && cross_few_applies(dm) ? launch_cross_few(dm, fp8, a, st) : launch_paged_decode(dm, fp8, a, part, st, own);
     return own ? launch_paged_attn_bf16(dm, fp8, a, part, st) : launch_cross_attn_bf16(dm, fp8, a, part, st);
   }
   auto launch = [&](auto own_rows) {
