@@ -66,6 +66,33 @@ __device__ __forceinline__ FaRow fa_row(int r, int g) { return {r / g, r % g}; }
 // SRC = kRawPages, kFp8Pages: every row is found through the page table, an entry of a list two units ahead of its page and the page a unit
 // ahead of the rows; offsets are numbers of 16 bytes.  8-bit rows are widened in registers, exactly, and never staged: a row is one line.
 // (8/2 heads, d 128, 512 tokens over 4096 keys: 89 us from tensors, 94 from pages, 92 from 8-bit ones.)
+// Cross attention: a list of so many units has shares of `per` units.  Row blocks and shares that there are lie one behind the other, sequence
+// after sequence, and the grid's blocks take one each: blocks that had nothing to do among the others would be dealt to the same shader
+// engines time and again, whose other blocks then wait (3 sequences of 1999, 764 and no states, 3 KV heads of 3, d 64, 333 tokens at most 43 -> 31 us).
+__device__ __forceinline__ int state_parts(int units, int per) { return max((units + per - 1) / per, 1); }
+struct StateShare {
+  int b, kv, rb, split, C;   // b < 0: none
+};
+__device__ __forceinline__ StateShare state_share(const Dims& dm, const PagedAttnArgs& a, uint32_t at) {
+  uint32_t before = 0;
+  for (int b0 = 0; b0 < dm.b; b0 += kWave) {   // every wave for itself, a sequence a lane
+    const int lane = threadIdx.x & 63, b = min(b0 + lane, dm.b - 1);
+    const int len = paged_len(dm, a, b), C = chunk_of(dm, a, b);
+    const uint32_t rows = b0 + lane < dm.b && len > 0 ? (uint32_t)(C * dm.g + 31) / 32 : 0u;
+    const uint32_t parts = (uint32_t)state_parts((len + 31) / 32, a.slots), mine = rows * parts * (uint32_t)dm.n_kv;
+    const uint32_t incl = before + wave_incl_scan_u32(mine);
+    const unsigned long long hit = __builtin_amdgcn_ballot_w64(at < incl);
+    if (hit != 0) {
+      const int of = (int)__builtin_ctzll(hit);
+      const uint32_t n = (uint32_t)__builtin_amdgcn_readlane((int)rows, of), p = (uint32_t)__builtin_amdgcn_readlane((int)parts, of);
+      const uint32_t i = at - (uint32_t)__builtin_amdgcn_readlane((int)(incl - mine), of);
+      return {b0 + of, (int)(i / (n * p)), (int)(i % n), (int)(i / n % p), __builtin_amdgcn_readlane(C, of)};
+    }
+    before = (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
+  }
+  return {-1, 0, 0, 0, 0};
+}
+
 template <int D, bool STAGED, int SRC = kContiguous>
 __global__ __launch_bounds__(kFaThreads, 2) void attn_f32(Dims dm, attn_args<SRC> a, float* __restrict__ part, int n_splits) {
   using Cfg = FaCfg<D, SRC>;
@@ -84,21 +111,33 @@ __global__ __launch_bounds__(kFaThreads, 2) void attn_f32(Dims dm, attn_args<SRC
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 31, hf = lane >> 5;
-  const int rb = gridDim.x - 1 - blockIdx.x;   // longest causal ranges first
-  const int split = blockIdx.y;
-  const int kv = blockIdx.z % dm.n_kv, b = blockIdx.z / dm.n_kv;
-  const int g = dm.g, n_rows = (PAGED ? chunk_of(dm, a, b) : dm.C) * g, row0 = rb * 32;
+  int rb = gridDim.x - 1 - blockIdx.x;   // longest causal ranges first
+  int split = blockIdx.y;
+  int kv = blockIdx.z % dm.n_kv, b = blockIdx.z / dm.n_kv;
+  const int g = dm.g;
+  int n_rows = (PAGED ? chunk_of(dm, a, b) : dm.C) * g, row0 = rb * 32;
   if constexpr (PAGED) {
-    if (split == 0 && n_rows < dm.C * g) {   // rows past the sequence's chunk: zeros, and no weight
+    const int live = OWN || paged_len(dm, a, b) > 0 ? n_rows : 0;   // (not OWN: without a state no row sees anything)
+    if (split == 0 && live < dm.C * g) {   // rows past the sequence's chunk: zeros, and no weight
       for (int i = tid; i < 32 * (D / 4); i += kFaThreads) {
         const int r = row0 + i / (D / 4);
-        if (r < n_rows || r >= dm.C * g) continue;
+        if (r < live || r >= dm.C * g) continue;
         const FaRow fr = fa_row(r, g);
         const int h = kv * g + fr.head;
         *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + b * dm.os[0] + h * dm.os[1] + (size_t)fr.tok * dm.os[2] + 4 * (i % (D / 4))) =
             f32x4{0.f, 0.f, 0.f, 0.f};
         if (a.lse != nullptr && i % (D / 4) == 0) a.lse[(size_t)(b * dm.n_q + h) * dm.C + fr.tok] = -INFINITY;
       }
+    }
+    if constexpr (!OWN) {
+      const StateShare share = state_share(dm, a, (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x);
+      if (share.b < 0) return;   // block-uniform
+      b = share.b;
+      kv = share.kv;
+      rb = share.rb;
+      split = share.split;
+      n_rows = share.C * g;
+      row0 = rb * 32;
     }
     if (row0 >= n_rows) return;   // block-uniform: a short chunk has no rows here
   }
@@ -108,7 +147,13 @@ __global__ __launch_bounds__(kFaThreads, 2) void attn_f32(Dims dm, attn_args<SRC
   n_cache = max(n_cache, 0);
   const int n_chunk = !OWN ? 0 : fa_row(min(row0 + 31, n_rows - 1), g).tok + 1;   // chunk keys any row of the block can see
   const int cache_units = (n_cache + 31) / 32, units = cache_units + (n_chunk + 31) / 32;
-  const int u_begin = (int)((long long)units * split / n_splits), u_end = (int)((long long)units * (split + 1) / n_splits);
+  int u_begin = (int)((long long)units * split / n_splits), u_end = (int)((long long)units * (split + 1) / n_splits);
+  int n_parts = n_splits;   // of this list
+  if constexpr (!OWN) {   // (shares of so many units: as many as the list has)
+    u_begin = split * a.slots;
+    u_end = min(units, u_begin + a.slots);
+    n_parts = state_parts(units, a.slots);
+  }
 
   // Q rows of the block to LDS (rows past the end repeat the last one and are never stored)
   for (int i = tid; i < 32 * (D / 4); i += kFaThreads) {
@@ -386,7 +431,7 @@ __global__ __launch_bounds__(kFaThreads, 2) void attn_f32(Dims dm, attn_args<SRC
     *reinterpret_cast<vrow*>(my_os + DB * m) = t;   // dims DB*m .. +DB
   }
   __syncthreads();
-  float* my_part = part + ((size_t)(blockIdx.z * gridDim.x + rb) * n_splits + split) * 32 * REC;
+  float* my_part = part + ((size_t)((OWN ? blockIdx.z : b * dm.n_kv + kv) * gridDim.x + rb) * n_splits + split) * 32 * REC;
   for (int i = tid; i < 32 * (D / 4); i += kFaThreads) {
     const int r = i / (D / 4), c4 = i % (D / 4);
     float m = -INFINITY;
@@ -403,7 +448,7 @@ __global__ __launch_bounds__(kFaThreads, 2) void attn_f32(Dims dm, attn_args<SRC
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] += wgt * x[e];
     }
-    if (n_splits > 1) {   // block-uniform
+    if (n_parts > 1) {   // block-uniform
       *reinterpret_cast<f32x4*>(my_part + r * D + 4 * c4) = acc;
       if (c4 == 0) {
         my_part[32 * D + r] = m;
@@ -444,6 +489,10 @@ __global__ __launch_bounds__(kFmThreads) void attn_f32_merge(Dims dm, attn_args<
   const bool row_on = row < (SRC == kContiguous ? dm.C : chunk_of(dm, a, b)) * dm.g;
   const int r = row % 32, rb = row_on ? row / 32 : 0;
   const float* rec = part + ((size_t)blockIdx.y * n_rb + rb) * n_splits * 32 * REC;
+  if constexpr (!has_own_rows(SRC)) {
+    n_splits = state_parts((paged_len(dm, a, b) + 31) / 32, a.slots);
+    if (n_splits == 1) return;   // block-uniform: written by the block that had all of it
+  }
   const int s0 = n_splits * grp / G, s1 = n_splits * (grp + 1) / G;
   float ms[RUNS * kFmRun], ls[RUNS * kFmRun];
   f32x4 x[RUNS * kFmRun];
@@ -531,16 +580,45 @@ inline int f32_most_splits(const Dims& dm, bool sparse, bool own = true) {
   const long long n = (f32_units(dm, sparse, own) + kFaWaves - 1) / kFaWaves;
   return (int)(n > kFaMaxSplits ? kFaMaxSplits : n);
 }
-inline int f32_splits(const Dims& dm, bool sparse, bool own = true) {
+inline int f32_splits(const Dims& dm, bool sparse) {
   const long long blocks = f32_blocks(dm), n = (256 + blocks - 1) / blocks;
-  const int most = f32_most_splits(dm, sparse, own);
+  const int most = f32_most_splits(dm, sparse);
   return n < most ? (int)n : most;
+}
+
+// Cross attention: units of a share, in eights (one for every wave).  A block is alone on its compute unit and takes 5.5 us and, at d 64, 5.7 for
+// every unit of a wave (d 128 9.6; 3.4 and 6.8 are the matrix instructions', which the vector unit's work is not hidden behind: twelve
+// waves a block take as long, and so do two blocks of four a SIMD with K by way of LDS), the partials' launch 6.  Of shares that take equally
+// long in a batch whose lists are all of `units`, the fewest: shorter lists have fewer, and their other blocks end at once.
+constexpr long long kMostStateParts = 2048;   // partials of 32 rows
+inline int f32_state_units(const Dims& dm) {
+  const long long blocks = f32_blocks(dm), units = f32_units(dm, false, false), rounds_of_waves = (units + kFaWaves - 1) / kFaWaves;
+  long long best = rounds_of_waves;
+  float best_us = 1e30f;
+  for (long long waves = rounds_of_waves; waves >= 1; --waves) {
+    const long long n = (rounds_of_waves + waves - 1) / waves;
+    if (n > 1 && (n > kFaMaxSplits || blocks * n > kMostStateParts)) break;
+    const float us = (float)((blocks * n + 255) / 256) * (5.5f + (dm.d == 64 ? 5.7f : 9.6f) * (float)waves) + (n > 1 ? 6.0f : 0.0f);
+    if (us < 0.98f * best_us) {
+      best_us = us;
+      best = waves;
+    }
+  }
+  return (int)best * kFaWaves;
+}
+inline int f32_state_shares(const Dims& dm, int per) { return (int)((f32_units(dm, false, false) + per - 1) / per); }
+inline size_t cross_f32_ws_floats(const Dims& dm) {
+  const long long most = f32_blocks(dm) * f32_most_splits(dm, false, false);
+  return (size_t)(most < kMostStateParts ? most : kMostStateParts) * 32 * (dm.d + 2);
 }
 
 template <int D, int SRC = kContiguous>
 static hipError_t launch_f32_units(const Dims& dm, const attn_args<SRC>& a, float* part, hipStream_t st) {
   constexpr bool OWN = has_own_rows(SRC);
-  const int n_splits = f32_splits(dm, a.k_idx != nullptr, OWN), n_rb = (dm.C * dm.g + 31) / 32;
+  const int n_rb = (dm.C * dm.g + 31) / 32;
+  int n_splits;
+  if constexpr (OWN) n_splits = f32_splits(dm, a.k_idx != nullptr);
+  else n_splits = f32_state_shares(dm, a.slots);
   auto launch = [&](auto staged) -> hipError_t {
     constexpr bool kStaged = decltype(staged)::value;
     constexpr size_t lds = FaCfg<D, SRC>::kLdsBytes;

@@ -16,6 +16,7 @@ constexpr bool has_own_rows(int src) { return src < kRawStates; }
 struct PagedAttnArgs : AttnArgs {   // (n_cache: as in AttnArgs)
   const int32_t *kv_lens = nullptr, *chunk_lens = nullptr;
   Pages pg = {};
+  // float32, cross attention: units of 32 states of a share (slots)
   // set by the launcher of the bf16 kernel where lists are shared: blocks of a KV head and their records; row blocks of a block and keys of a
   // tile, as powers of two; number of shares and first record of every KV head's and sequence's list
   u32x2* shares = nullptr;

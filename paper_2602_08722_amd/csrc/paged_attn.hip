@@ -100,11 +100,13 @@ static hipError_t launch_paged_f32(const Dims& dm, const PagedArgs& a, float* pa
     return hipGetLastError();
   }
   constexpr int SRC = OWN ? FP8 ? kFp8Pages : kRawPages : FP8 ? kFp8States : kRawStates;
-  return launch_f32_units<D, SRC>(dm, paged_attn_args(a, part), part, st);
+  PagedAttnArgs aa = paged_attn_args(a, part);
+  if constexpr (!OWN) aa.slots = f32_state_units(dm);
+  return launch_f32_units<D, SRC>(dm, aa, part, st);
 }
 
 size_t paged_attn_ws_floats(const Dims& dm, int dtype) {
-  if (dtype != QUOKA_BF16) return attn_f32_ws_floats(dm);
+  if (dtype != QUOKA_BF16) return attn_f32_ws_floats(dm) > cross_f32_ws_floats(dm) ? attn_f32_ws_floats(dm) : cross_f32_ws_floats(dm);
   return attn_decode_applies(dm) ? paged_decode_ws_floats(dm) : paged_attn_bf16_ws_floats(dm);
 }
 
