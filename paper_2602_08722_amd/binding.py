@@ -482,8 +482,17 @@ class PagedCache:
     """
 
     def __init__(self, k_pages, v_pages, page_table, k_scale=None, v_scale=None):
-        self._pool, self._page_table, self._shape = (k_pages, v_pages, k_scale, v_scale), page_table, None
+        self._pool, self._page_table = (k_pages, v_pages, k_scale, v_scale), page_table
         self.pages = make_pages(k_pages, v_pages, page_table, k_scale, v_scale)   # (addresses: of the tensors that are kept here)
+        # what rows that move in or out have to agree in, and the description of such a call
+        _, n_kv, _, d = k_pages.shape
+        self._rows = (k_pages.dtype, n_kv, d, k_pages.device)
+        s = self._shape = QuokaShape()
+        s.n_q_heads = s.n_kv_heads = n_kv
+        s.head_dim, s.chunk_len, s.n_retain = d, 1, 1
+        s.dtype = QUOKA_F32 if k_pages.dtype == torch.float32 else QUOKA_BF16
+        s.q_stride = s.kv_stride = s.ck_stride = s.o_stride = (ctypes.c_int64 * 3)(0, 0, d)
+        s.batch = page_table.shape[0]
 
     k_pages = property(lambda self: self._pool[0])
     v_pages = property(lambda self: self._pool[1])
@@ -514,42 +523,36 @@ class PagedCache:
 
     def _moves(self, source, max_kv_len, max_budget):
         """The description of a call that brings rows of `source` here."""
-        mine, theirs = self.k_pages, source.k_pages
-        if theirs.dtype != mine.dtype:
-            raise TypeError(f"pages of {theirs.dtype} into pages of {mine.dtype}")
-        if theirs.shape[1] != mine.shape[1] or theirs.shape[3] != mine.shape[3] or theirs.device != mine.device:
+        if source._rows != self._rows:
+            if source._rows[0] != self._rows[0]:
+                raise TypeError(f"pages of {source._rows[0]} into pages of {self._rows[0]}")
             raise ValueError("caches that rows move between share KV heads, head size and device")
         s = self._shape
-        if s is None:
-            _, n_kv, _, d = mine.shape
-            s = self._shape = QuokaShape()
-            s.n_q_heads = s.n_kv_heads = n_kv
-            s.head_dim, s.chunk_len, s.n_retain = d, 1, 1
-            s.dtype = QUOKA_F32 if mine.dtype == torch.float32 else QUOKA_BF16
-            s.q_stride = s.kv_stride = s.ck_stride = s.o_stride = (ctypes.c_int64 * 3)(0, 0, d)
-        s.batch, s.max_kv_len, s.max_budget = self._page_table.shape[0], max_kv_len, max_budget
+        s.max_kv_len, s.max_budget = max_kv_len, max_budget
         return s
 
     def compact(self, source, k_idx, k_cnt):
         """The rows that k_idx [b, n_KV, B_max] lists, k_cnt [b, n_KV] of them, from the pages of `source`, another PagedCache of the same
         batch, one behind the other into the pages of this one."""
-        b, n_kv = self._page_table.shape[0], self.k_pages.shape[1]
-        for t, dims in ((k_idx, 3), (k_cnt, 2)):
-            if t.dtype != torch.int32 or t.dim() != dims or t.shape[:2] != (b, n_kv) or not t.is_contiguous():
-                raise ValueError("k_idx [b, n_KV, B_max] and k_cnt [b, n_KV] are dense int32 tensors")
-            if t.device != self.k_pages.device:
-                raise ValueError("key lists are on the pages' device")
-        if source.page_table.shape[0] != b:
+        _, n_kv, d, dev = self._rows
+        lists, b = k_idx.shape, self._shape.batch
+        if (k_idx.dtype != torch.int32 or k_cnt.dtype != torch.int32 or len(lists) != 3 or lists[0] != b or lists[1] != n_kv or
+                k_cnt.shape != lists[:2] or not k_idx.is_contiguous() or not k_cnt.is_contiguous()):
+            raise ValueError("k_idx [b, n_KV, B_max] and k_cnt [b, n_KV] are dense int32 tensors")
+        if k_idx.device != dev or k_cnt.device != dev:
+            raise ValueError("key lists are on the pages' device")
+        if source._shape.batch != b:
             raise ValueError("caches that rows move between are of one batch")
         # (the positions that the source's table has, as far as there are such caches)
-        room = min(source.pages.max_pages * source.pages.page_len, (1 << 24) - 1, (1 << 32) // (4 * self.k_pages.shape[3]) - 1)
-        quoka_cache_compact(self._moves(source, room, k_idx.shape[2]), source.pages, self.pages, k_idx, k_cnt)
+        theirs = source.pages
+        room = min(theirs.max_pages * theirs.page_len, (1 << 24) - 1, (1 << 32) // (4 * d) - 1)
+        quoka_cache_compact(self._moves(source, room, lists[2]), theirs, self.pages, k_idx, k_cnt)
 
     def copy(self, source, parents=None, first=None, lens=None, max_rows=None):
         """Rows first[b] .. lens[b] - 1 of sequence parents[b] of `source`, another PagedCache, to the same positions of sequence b.  (After
         PagedSequences.fork: its parents, first and lens.)  parents None: sequence b itself; first None: 0.  No sequence has more than
         max_rows of them (None: page_len, what a fork leaves to be copied)."""
-        b, n_parents, dev = self._page_table.shape[0], source.page_table.shape[0], self.k_pages.device
+        dev, b, n_parents = self._rows[3], self._shape.batch, source._shape.batch
         if lens is None:
             raise ValueError("no lengths")
         for t in (parents, first, lens):

@@ -1,7 +1,9 @@
 // Rows of a cache in pages into other pages, as they are kept (quoka_cache_copy, quoka_cache_compact).
 //
 // Bound by memory: every row is read once and written once.  A row is CG lanes of 16 bytes; a thread has U rows of K and of V on the way at
-// once, and the chain ahead of them is length (or list), both pages, row.
+// once, and the chain ahead of them is length (or list), both pages, row.  Measured, caches that are in no cache memory: lists of 8192 for each
+// of 4 sequences and 8 heads of 128, 16-bit rows (269 MB read and written) 56 us (4.8 TB/s; a copy of 1 GiB on this card 5.1), 8-bit rows 27.8 (4.9);
+// 333 of 3 sequences and 3 float32 heads of 64 3.5, of which launch and chain are all.
 #include <type_traits>
 
 #include "pages.hip.h"
@@ -62,8 +64,14 @@ __global__ __launch_bounds__(kPrThreads) void move_rows(MoveArgs a) {
     if (i >= n || dst_page[u] >= (uint32_t)a.dst.n_pages || (to >> a.dst.shift) >= a.dst.max_pages) continue;   // (no page: the row is dropped)
     const int slot = slot_of(a.dst, to);
     const long long at = row_at(a.dst, dst_page[u], kv, slot) + 16 * c;
-    *reinterpret_cast<u32x4*>(static_cast<char*>(a.dst.k) + at) = xk[u];
-    *reinterpret_cast<u32x4*>(static_cast<char*>(a.dst.v) + at) = xv[u];
+    u32x4 *to_k = reinterpret_cast<u32x4*>(static_cast<char*>(a.dst.k) + at), *to_v = reinterpret_cast<u32x4*>(static_cast<char*>(a.dst.v) + at);
+    if constexpr (LIST) {   // (past the cache memories, which long lists would fill: 59.6 -> 56.4 us and 33.3 -> 27.8 in the two cases above)
+      __builtin_nontemporal_store(xk[u], to_k);
+      __builtin_nontemporal_store(xv[u], to_v);
+    } else {
+      *to_k = xk[u];
+      *to_v = xv[u];
+    }
     if constexpr (FP8) {
       const long long s = scale_at(a.dst, dst_page[u], kv, slot);
       if (c == 0) {
@@ -75,7 +83,7 @@ __global__ __launch_bounds__(kPrThreads) void move_rows(MoveArgs a) {
 }
 
 hipError_t launch_move_rows(MoveArgs a, int batch, int row_bytes, bool fp8, hipStream_t st) {
-  constexpr int U = 2;
+  constexpr int U = 2;   // (1, 2, 4: 59.4, 59.6, 60.7 us and 33.5, 33.3, 33.4)
   for (int i = 0; i < 3; ++i) {
     a.src.st[i] *= a.es;
     a.dst.st[i] *= a.es;
