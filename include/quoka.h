@@ -332,7 +332,8 @@ quoka_status quoka_pages_resize(const quoka_page_owners* owners, const int32_t* 
 
 /* Sequences that go on from others: child b, from sequence parents[b] of `from`, of which lens[parents[b]] tokens are cached (cut to the
  * pages that it holds, and to the child's max_pages).  Whole pages are shared; for a last page that is not full the child gets a page of its
- * own, whose rows quoka_cache_copy brings from the parent's (in every layer's cache).  So no page that is written to has two holders.
+ * own, whose rows quoka_cache_copy brings from the parent's (in every layer's cache).  So sequences that grow never write to a page that
+ * others hold.  (One that is cut back into a page that it shares may not be written to from there on: it goes on by a fork to that length.)
  * Pages that the child held before are given back first.  A parent outside [0, from->batch): no pages, length 0.
  * `from` and `children` share ref, n_pages and page_len, and have tables of their own.
  *   lens        in   [from->batch] int32;  parents  in  [children->batch] int32, repeated ones too

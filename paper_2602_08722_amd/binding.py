@@ -149,6 +149,12 @@ def _stream(stream):
     return _raw_stream(torch.cuda.current_device())
 
 
+def _here(index) -> None:
+    """Calls go to the current device's stream: tensors of another device (its index; None: no GPU's) are refused."""
+    if index is not None and index != torch.cuda.current_device():
+        raise ValueError(f"tensors of device {index}, and the current one is {torch.cuda.current_device()}")
+
+
 def _strides3(t: torch.Tensor):
     assert t.dim() == 4 and t.stride(3) == 1, "expected [batch, heads, tokens, head_dim] with head_dim contiguous"
     return (ctypes.c_int64 * 3)(t.stride(0), t.stride(1), t.stride(2))
@@ -487,6 +493,7 @@ class PagedCache:
         # what rows that move in or out have to agree in, and the description of such a call
         _, n_kv, _, d = k_pages.shape
         self._rows = (k_pages.dtype, n_kv, d, k_pages.device)
+        self._index = k_pages.device.index
         s = self._shape = QuokaShape()
         s.n_q_heads = s.n_kv_heads = n_kv
         s.head_dim, s.chunk_len, s.n_retain = d, 1, 1
@@ -527,6 +534,7 @@ class PagedCache:
             if source._rows[0] != self._rows[0]:
                 raise TypeError(f"pages of {source._rows[0]} into pages of {self._rows[0]}")
             raise ValueError("caches that rows move between share KV heads, head size and device")
+        _here(self._index)
         s = self._shape
         s.max_kv_len, s.max_budget = max_kv_len, max_budget
         return s
@@ -691,6 +699,7 @@ class PagedBuffers:
     def cross_attn(self):
         if self.q is None:
             raise ValueError("no queries")
+        _here(self.cache._index)
         quoka_cross_attn(self.shape, self.cache.pages, self.q, self.kv_lens, self.chunk_lens, self.out, self.lse, self.workspace)
         return self.out
 
@@ -717,6 +726,7 @@ class PagedSequences:
                                             are shared, and PagedCache.copy(.., parents, children.first, children.lens) brings the rest
 
     lacking [1]: how many pages the last call would have needed beyond those that were free.  first, lens [b]: of the last fork.
+    A sequence that is cut back into a page that it shares goes on by a fork to that length, not by writing there.
     """
 
     def __init__(self, ref, page_table, held, page_len):
@@ -725,7 +735,7 @@ class PagedSequences:
                 raise ValueError("ref [n_pages], page_table [b, max_pages] and held [b] are dense int32 tensors on one device")
         if held.shape[0] != page_table.shape[0]:
             raise ValueError("page_table and held are of one batch")
-        self._tensors = (ref, page_table, held)
+        self._tensors, self._index = (ref, page_table, held), ref.device.index
         o = self.owners = QuokaPageOwners()   # (addresses: of the tensors that are kept here)
         o.ref, o.page_table, o.held = ref.data_ptr(), page_table.data_ptr(), held.data_ptr()
         o.n_pages, o.page_len, o.max_pages, o.batch = ref.shape[0], int(page_len), page_table.shape[1], page_table.shape[0]
@@ -759,11 +769,13 @@ class PagedSequences:
         return x
 
     def resize(self, lens):
+        _here(self._index)
         o = self.owners
         quoka_pages_resize(o, self._lens(lens, o.batch), self.lacking, self.workspace)
 
     def fork(self, source, parents, lens):
         """parents [b]: sequences of `source` (others: no parent).  lens: cached tokens of the sequences of `source`, each."""
+        _here(self._index)
         o, theirs = self.owners, source.owners
         quoka_pages_fork(theirs, o, self._lens(parents, o.batch), self._lens(lens, theirs.batch), self.first, self.lens, self.lacking,
                          self.workspace)
@@ -799,6 +811,7 @@ class DraftBuffers:
         if any(t is not None and t.device != dev for t in (draft, tokens, uniform)):
             raise ValueError("probabilities, tokens and random numbers are on one device")
         self.target, self.draft, self.tokens, self.uniform = target, draft, tokens, uniform
+        self._index = dev.index
         self.draft_lens = None if draft_lens is None else _ints(draft_lens, dev)
         if self.draft_lens is not None and self.draft_lens.numel() != b:
             raise ValueError("target and draft_lens are of one batch")
@@ -812,6 +825,7 @@ class DraftBuffers:
         self.workspace = torch.empty(quoka_verify_workspace_bytes(s), dtype=torch.uint8, device=dev)
 
     def verify(self):
+        _here(self._index)
         quoka_verify_draft(self.shape, self.target, self.draft, self.tokens, self.uniform, self.draft_lens, self.n_accepted,
                            self.tokens_out, self.workspace)
         return self.n_accepted, self.tokens_out

@@ -890,6 +890,6 @@ const char* quoka_status_string(quoka_status status) {
   return "unknown status";
 }
 
-int quoka_version(void) { return 200; }
+int quoka_version(void) { return 300; }
 
 }  // extern "C"

@@ -6,7 +6,7 @@
 // Bound by a chain of fetches (length, pages, rows: 4 us until a block of one round of tiles has ended) and by the waves' way through a round
 // of tiles, 1.2 us at d 64, 1.4 at d 128, whatever the bytes: LDS, which takes every row and gives it back, and the products' latency.  Two
 // tiles of each wave on the way at once, and rows in four registers in the place of sixteen (at most eight query rows, states on lanes, P by
-// way of LDS), left a round as it was.
+// way of LDS), left a round as it was; K as operands straight from memory and 16 waves a block made it longer (rows as they are 2.4 us).
 #include "decode_tile.hip.h"
 
 namespace quoka {

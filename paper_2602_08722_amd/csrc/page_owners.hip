@@ -213,8 +213,8 @@ __device__ __forceinline__ void hand_out(const Owners& o, const ForkArgs& f, int
   if (tid == 0) *lacking = (int32_t)(wanted > before ? wanted - before : 0u);
 }
 
-// All of it in one block.  (Counts are first fetched when the atomics of the first step have reached them: no line of theirs can be in the
-// first-level cache before.)
+// All of it in one block.  Counts are fetched when the atomics of the first step have reached them, and not from the first-level cache, where a
+// line may be that has table entries of the first step and counts in it.
 template <bool FORK>
 __global__ __launch_bounds__(kOsThreads) void owners_one(Owners from, Owners o, ForkArgs f, const int32_t* __restrict__ lens,
                                                          int32_t* __restrict__ lacking) {
@@ -231,6 +231,7 @@ __global__ __launch_bounds__(kOsThreads) void owners_one(Owners from, Owners o, 
   }
   wait_vmcnt<0>();
   __syncthreads();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   hand_out<FORK>(o, f, tid < o.b ? starts[tid] : 0, tid < o.b ? needs[tid] : 0, lacking);
 }
 

@@ -236,6 +236,27 @@ def test_drafts_refuse_tensors_that_do_not_fit():
     assert list(pk.DraftBuffers(rows, x, u).shape.target_stride) == [800, 200]
 
 
+def test_calls_for_another_device_than_the_current_one_are_refused(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    pk.binding._here(None)
+    pk.binding._here(0)
+    with pytest.raises(ValueError):
+        pk.binding._here(1)
+    cache, other = _cache(), _cache()
+    q = torch.zeros(2, 4, 3, 64, dtype=torch.bfloat16)
+    seqs = pk.PagedSequences.allocate(50, 16, 3, 4, "cpu")
+    kids, drafts = seqs.another(3), pk.DraftBuffers(torch.zeros(2, 4, 100), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 4))
+    buf = pk.PagedBuffers(cache, [1, 2], 60, q=q)
+    for x in (cache, other, seqs, kids, drafts):   # (as if their tensors were the second GPU's)
+        assert x._index is None
+        x._index = 1
+    lens, lists = _ints(1, 2, 3), (torch.zeros(2, 2, 5, dtype=torch.int32), torch.zeros(2, 2, dtype=torch.int32))
+    for call in (buf.cross_attn, lambda: other.compact(cache, *lists), lambda: other.copy(cache, lens=_ints(1, 2)), lambda: seqs.resize(lens),
+                 lambda: kids.fork(seqs, lens, lens), drafts.verify):
+        with pytest.raises(ValueError, match="current one"):
+            call()
+
+
 # ---- the plain forms, by hand -----------------------------------------------------------------------------------------
 
 def test_the_plain_verification_draws_from_the_target():

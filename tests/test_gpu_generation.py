@@ -113,6 +113,11 @@ CROSS_CASES = [
     dict(dtype="f32", fp8=False, n_q=8, n_kv=2, d=128, page_len=64, C=100, lens=[333, 0], chunks=[100, 37]),
     dict(dtype="f32", fp8=True, n_q=6, n_kv=2, d=64, page_len=16, C=70, lens=[64, 900], chunks=[0, 70]),
     dict(dtype="f32", fp8=False, n_q=16, n_kv=1, d=64, page_len=8, C=33, lens=[31]),
+    dict(dtype="f32", fp8=False, n_q=4, n_kv=2, d=128, page_len=16, C=1, lens=[0, 0]),
+    dict(dtype="f32", fp8=True, n_q=4, n_kv=2, d=64, page_len=16, C=70, lens=[0]),
+    dict(dtype="f32", fp8=False, n_q=4, n_kv=2, d=64, page_len=16, C=40, lens=[(97 * i) % 700 for i in range(140)], chunks=[(11 * i) % 41 for i in range(140)]),
+    dict(dtype="f32", fp8=False, n_q=2, n_kv=1, d=128, page_len=16, C=3, lens=[9000 - 700 * i for i in range(13)]),
+    dict(dtype="f32", fp8=True, n_q=32, n_kv=8, d=64, page_len=16, C=600, lens=[700, 300], chunks=[600, 100]),   # more row blocks than a round
 ]
 
 
@@ -337,6 +342,29 @@ def test_pages_that_come_and_go(n_pages, page_len, batch, max_pages):
         assert book.resize([0] * batch) == 0
     torch.cuda.synchronize()
     assert ref.tolist() == counts and set(counts) <= {0, 1}
+
+
+@pytest.mark.parametrize("batch,kids,n_pages", [(3, 5, 100), (40, 90, 40000), (7, 300, 3000), (2, 1100, 2500)])
+def test_children_with_less_room_than_their_parents(batch, kids, n_pages):
+    """Tables of other widths, and fewer free pages than last pages that want one; the same fork again changes nothing."""
+    pk, rng = _pk(), np.random.default_rng(70)
+    seqs = pk.PagedSequences.allocate(n_pages, 16, batch, 20, DEV)
+    lens = [int(x) for x in rng.integers(0, 320, batch)]
+    counts = [0] * n_pages
+    book, theirs = G.Book(counts, 16, batch, 20), G.Book(counts, 16, kids, 11)
+    seqs.resize(_ints(lens))
+    assert book.resize(lens) == 0
+    child = seqs.another(kids, 11)
+    parents = [int(x) for x in rng.integers(0, batch, kids)]
+    for _ in range(3):
+        child.fork(seqs, _ints(parents), _ints(lens))
+        first, got, lacking = theirs.fork(book, parents, lens)
+        torch.cuda.synchronize()
+        assert child.first.tolist() == first and child.lens.tolist() == got
+        _same(child, theirs, lacking, "")
+    child.resize(torch.zeros(kids, dtype=torch.int32, device=DEV))
+    theirs.resize([0] * kids)
+    _same(seqs, book, 0, "")
 
 
 def test_owners_that_hold_nonsense_stay_inside_the_arrays():
