@@ -1239,6 +1239,20 @@ struct AttnPlan {
   int n_splits;
 };
 
+// Whole lists of cross attention: eight row blocks or four by the rounds of 256 blocks that either takes (all rows of a block see the whole list, so
+// a round is as long as its tiles), where shorter lists of a batch are the smaller loss with four.  Us, eight and four: d 64, 4 x 4 heads of 3,
+// 1717 tokens over 1691 states (336 groups of eight) 75 / 60, 13 x 12 heads, 404 over 3284 (312) 122 / 98, 13 x 4 heads of 8, 247 over 68 (416)
+// 18.7 / 20.8; d 128, 2 x 4 heads of 8, 1251 over 7115 (320) 359 / 307, 3 x 4 heads of 3, 1469 over 1750 (216) 54 / 61, 4 x 4 heads of 8,
+// 1858 over 883 (944) 123 / 140; lists that differ: d 64, 4 x 12 heads, 1049 over 360 - 1441 (240) 34 / 27.
+// (The terms are as attn_plan's fits below, from 26 calls; by them the choice is 1.5 % behind the better of the two on the mean, before 8 %.)
+inline bool eight_of_states(const Dims& dm, long long eights, long long fours) {
+  const float tiles = (float)(dm.T_cap + kSub - 1) / kSub, halves = (float)(dm.T_cap + 2 * kSub - 1) / (2 * kSub);
+  const float r8 = (float)((eights + kComputeUnits - 1) / kComputeUnits), r4 = (float)((fours + kComputeUnits - 1) / kComputeUnits);
+  const float us8 = dm.d == 64 ? 6.6f + 1.2f * r8 * tiles + 3.4f * (r8 - 1.f) : 6.9f + 1.6f * r8 * tiles + 2.0f * (r8 - 1.f);
+  const float us4 = dm.d == 64 ? 4.7f + 1.05f * r4 * halves + 6.1f * (r4 - 1.f) : 7.2f + 1.74f * r4 * halves + 6.7f * (r4 - 1.f);
+  return us8 < (dm.b > 1 ? 0.9f : 1.f) * us4;
+}
+
 // Over pages, where a list's shares go by each sequence's length (list_shares): lists of 8192 keys and more of a batch whose blocks of eight
 // fill seven eighths of a round at most are shared by the blocks of a whole round.  (27 batches of 2 - 13 sequences, 130 - 224 blocks of
 // eight, 8400 - 31200 keys and chunk tokens together: 0.84 - 0.90 of the time of whole lists in blocks of four for equal lengths, 0.73 - 1.05 for
@@ -1249,6 +1263,7 @@ inline AttnPlan attn_plan(const Dims& dm, bool sparse, bool paged = false, bool 
   if (paged && dm.b > 1 && dm.b <= kWave && heads * nrb * 2 > kMaxRecords && eights <= kComputeUnits * 7 / 8 &&
       attended_cap(dm, sparse) + (own ? dm.C : 0) >= 8192 && dm.b * ((nrb + 7) / 8) <= kComputeUnits / dm.n_kv)
     return AttnPlan{false, 2};
+  if (heads * nrb * 2 > kMaxRecords && !own) return AttnPlan{!eight_of_states(dm, eights, heads * ((nrb + 3) / 4)), 1};
   if (heads * nrb * 2 > kMaxRecords) return AttnPlan{!eight_row_blocks(dm, sparse, heads * ((nrb + 7) / 8)), 1};
   struct Fit {
     float fixed, step, round, per_mb, per_split, beyond_four;   // a step is 8 row blocks x 64 keys or 4 x 128

@@ -92,9 +92,18 @@ __global__ __launch_bounds__(kPsThreads) void paged_f32_short(Dims dm, PagedArgs
   if (a.lse != nullptr && lane == 0) a.lse[(long long)(b * dm.n_q + h) * dm.C + i] = m_run + logf(l_run);
 }
 
+// Cross attention: a wave a row or units of 32 states, by what either takes; us, units / a wave a row: 12 heads, d 64, 16 tokens over 1 state
+// 7.6 / 5.2, over 16 7.5 / 6.6, over 32 7.5 / 8.7, 1000 over 1 13.6 / 11.5, over 8 13.4 / 16.6; d 128, 40 tokens over 16 10.4 / 7.4, over 32
+// 10.5 / 10.2; 8 x 4 heads of 8, d 128, 40 over 4 19.8 / 17.7, over 16 19.4 / 26.5.
+static bool states_are_few(const Dims& dm) {
+  const float rows = (float)dm.b * (float)dm.n_q * (float)dm.C * 1e-3f, n = (float)dm.T_cap;
+  if (dm.d == 64) return 4.6f + 0.11f * n + rows * (0.55f + 0.05f * n) < 7.5f + 0.7f * rows;
+  return 4.8f + 0.13f * n + rows * (0.92f + 0.075f * n) < 9.8f + 1.06f * rows;
+}
+
 template <bool FP8, int D, bool OWN>
 static hipError_t launch_paged_f32(const Dims& dm, const PagedArgs& a, float* part, hipStream_t st) {
-  if (attn_f32_is_short(dm, a.k_idx != nullptr)) {
+  if (OWN ? attn_f32_is_short(dm, a.k_idx != nullptr) : states_are_few(dm)) {
     const dim3 grid((dm.C + kPsThreads / 64 - 1) / (kPsThreads / 64), dm.n_q, dm.b);
     hipLaunchKernelGGL((paged_f32_short<FP8, D, OWN>), grid, dim3(kPsThreads), 0, st, dm, a);
     return hipGetLastError();
