@@ -289,7 +289,7 @@ quoka_status quoka_cross_attn(const quoka_shape* shape, const quoka_pages* pages
 
 /* Rows of one cache into the pages of another, or into other pages of the same pool, exactly as they are kept (scales included).  `src` and
  * `dst` share format, shape.dtype, n_KV and d; page_len, strides and pool may differ.  No row that is written may be one that is read, and
- * no two of them the same row of the pool; rows without a page are dropped, as by a write.  No workspace.
+ * no two of them the same row of the pool; rows without a page in src or in dst are dropped, as by a write.  No workspace.
  *
  * quoka_cache_compact: the listed rows of every KV head, one behind the other (a cache that keeps what quoka_topk_keys chose).
  *   k_idx, k_cnt  in  [b, n_KV, B_max], [b, n_KV]: the row at position k_idx[b,kv,j] of src goes to position j of dst, j < k_cnt[b,kv].
@@ -335,7 +335,7 @@ quoka_status quoka_pages_resize(const quoka_page_owners* owners, const int32_t* 
  * own, whose rows quoka_cache_copy brings from the parent's (in every layer's cache).  So sequences that grow never write to a page that
  * others hold.  (One that is cut back into a page that it shares may not be written to from there on: it goes on by a fork to that length.)
  * Pages that the child held before are given back first.  A parent outside [0, from->batch): no pages, length 0.
- * `from` and `children` share ref, n_pages and page_len, and have tables of their own.
+ * `from` and `children` share ref, n_pages and page_len, and have tables of their own, no part of which is the other's.
  *   lens        in   [from->batch] int32;  parents  in  [children->batch] int32, repeated ones too
  *   first       out  [children->batch]: the first position of a row that is to be copied (the whole pages' end)
  *   child_lens  out  [children->batch]: cached tokens; where the last page is lacking, those of the whole pages
@@ -351,8 +351,9 @@ quoka_status quoka_pages_fork(const quoka_page_owners* from, const quoka_page_ow
  * and a of them are until the first that is not.  The token after them, y, is drawn with uniform[b,n_draft] (cut to [0, 1)): the lowest v
  * of positive weight w_v with w_0 + .. + w_v > uniform[b,n_draft] * (w_0 + w_1 + ..), where
  *   w_v = max(p_a(v) - q_a(v), 0) for a < n, or p_a(v) should all of these be 0;   w_v = p_n(v) for a == n.
- * So the tokens are distributed as the target's, whatever drafted them.  Distributions need not add up to 1; entries that are no positive
- * number (NaN, infinities) weigh nothing and are not accepted, nor is a token outside [0, vocab).  All of it is in float64.
+ * So the tokens are distributed as the target's, whatever drafted them.  Distributions need not add up to 1.  A w_v that is no positive
+ * number (NaN, an infinity) weighs nothing; a token whose p_i(x_i) is none, whose q_i(x_i) is NaN or an infinity, or that is outside
+ * [0, vocab) is not accepted.  All of it is in float64.  No output is an input.
  *   target      in   [b, n_draft + 1, vocab] (dtype), the last axis contiguous, others by strides (elements, may be 0)
  *   draft       in   [b, n_draft, vocab] (dtype); NULL: q_i is 1 at x_i (tokens that were looked up)
  *   tokens      in   [b, n_draft] int32;  uniform  in  [b, n_draft + 1] float32

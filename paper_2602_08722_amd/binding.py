@@ -150,8 +150,11 @@ def _stream(stream):
 
 
 def _here(index) -> None:
-    """Calls go to the current device's stream: tensors of another device (its index; None: no GPU's) are refused."""
-    if index is not None and index != torch.cuda.current_device():
+    """Calls go to the current device's stream: tensors of another device (its index; None: the host's) are refused."""
+    if index is None:
+        if torch.cuda.is_available():
+            raise ValueError("tensors of no GPU")
+    elif index != torch.cuda.current_device():
         raise ValueError(f"tensors of device {index}, and the current one is {torch.cuda.current_device()}")
 
 
@@ -535,7 +538,7 @@ class PagedCache:
                 raise TypeError(f"pages of {source._rows[0]} into pages of {self._rows[0]}")
             raise ValueError("caches that rows move between share KV heads, head size and device")
         _here(self._index)
-        s = self._shape
+        s = QuokaShape.from_buffer_copy(self._shape)   # (one for each call: other threads may be in one)
         s.max_kv_len, s.max_budget = max_kv_len, max_budget
         return s
 

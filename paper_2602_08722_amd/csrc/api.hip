@@ -795,8 +795,11 @@ quoka_status quoka_pages_fork(const quoka_page_owners* from, const quoka_page_ow
   if (st != QUOKA_OK) return st;
   st = check_owners(children, &o);
   if (st != QUOKA_OK) return st;
-  if (p.ref != o.ref || p.n_pages != o.n_pages || p.shift != o.shift || p.table == o.table || p.held == o.held) return QUOKA_EINVAL;
-  if (parents == nullptr || lens == nullptr || first == nullptr || child_lens == nullptr || lacking == nullptr || child_lens == lens) return QUOKA_EINVAL;
+  if (p.ref != o.ref || p.n_pages != o.n_pages || p.shift != o.shift) return QUOKA_EINVAL;
+  auto overlap = [](const int32_t* x, long long n, const int32_t* y, long long m) { return x < y + m && y < x + n; };
+  if (overlap(p.table, (long long)p.b * p.max_pages, o.table, (long long)o.b * o.max_pages) || overlap(p.held, p.b, o.held, o.b)) return QUOKA_EINVAL;
+  if (parents == nullptr || lens == nullptr || first == nullptr || child_lens == nullptr || lacking == nullptr) return QUOKA_EINVAL;
+  if (overlap(child_lens, o.b, lens, p.b) || overlap(first, o.b, lens, p.b)) return QUOKA_EINVAL;   // (children of one parent read what another wrote)
   st = check_owners_ws(o, workspace, workspace_bytes);
   if (st != QUOKA_OK) return st;
   quoka::ForkArgs f;
@@ -833,6 +836,7 @@ quoka_status quoka_verify_draft(const quoka_draft_shape* shape, const void* targ
   if (st != QUOKA_OK) return st;
   if (target == nullptr || tokens == nullptr || uniform == nullptr || n_accepted == nullptr || tokens_out == nullptr || workspace == nullptr)
     return QUOKA_EINVAL;
+  if (n_accepted == draft_lens) return QUOKA_EINVAL;   // (waves read the one after others wrote the other)
   const uintptr_t es = shape->dtype == QUOKA_BF16 ? 2 : 4;
   if (reinterpret_cast<uintptr_t>(target) % es != 0 || reinterpret_cast<uintptr_t>(draft) % es != 0) return QUOKA_EINVAL;
   if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0 || workspace_bytes < need) return QUOKA_EWORKSPACE;

@@ -43,7 +43,12 @@ __global__ __launch_bounds__(kPrThreads) void move_rows(MoveArgs a) {
     dst_page[u] = (uint32_t)dst_table[min((LIST ? i : first + i) >> a.dst.shift, a.dst.max_pages - 1)];
   }
 #pragma unroll
-  for (int u = 0; u < U; ++u) src_page[u] = page_of(a.src, src_table, (int)pos[u]);
+  for (int u = 0; u < U; ++u) {
+    const uint32_t at = pos[u] >> a.src.shift;
+    src_page[u] = (uint32_t)src_table[min(at, (uint32_t)a.src.max_pages - 1)];
+    // (no page in either: the row is dropped; what is fetched in its place is inside the pool)
+    if (src_page[u] >= (uint32_t)a.src.n_pages || at >= (uint32_t)a.src.max_pages) dst_page[u] = ~0u, src_page[u] = 0;
+  }
   u32x4 xk[U], xv[U];
   uint8_t ek[FP8 ? U : 1], ev[FP8 ? U : 1];
 #pragma unroll
@@ -61,7 +66,7 @@ __global__ __launch_bounds__(kPrThreads) void move_rows(MoveArgs a) {
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int i = i0 + u * RPB + r0, to = LIST ? i : first + i;
-    if (i >= n || dst_page[u] >= (uint32_t)a.dst.n_pages || (to >> a.dst.shift) >= a.dst.max_pages) continue;   // (no page: the row is dropped)
+    if (i >= n || dst_page[u] >= (uint32_t)a.dst.n_pages || (to >> a.dst.shift) >= a.dst.max_pages) continue;
     const int slot = slot_of(a.dst, to);
     const long long at = row_at(a.dst, dst_page[u], kv, slot) + 16 * c;
     u32x4 *to_k = reinterpret_cast<u32x4*>(static_cast<char*>(a.dst.k) + at), *to_v = reinterpret_cast<u32x4*>(static_cast<char*>(a.dst.v) + at);

@@ -123,7 +123,12 @@ def test_owners_that_do_not_belong_together_and_bad_pointers_are_refused():
     for kw in (dict(), dict(page_table=0x7000), dict(held=0x8000), dict(page_table=0x7000, held=0x8000, ref=0x9000),
                dict(page_table=0x7000, held=0x8000, page_len=32), dict(page_table=0x7000, held=0x8000, n_pages=99)):
         assert lib.quoka_pages_fork(at, ctypes.byref(_owners(**kw)), AT, AT, OTHER, OTHER, AT, WS, BIG, None) == 1
+    for kw in (dict(page_table=o.page_table + 4 * (o.batch * o.max_pages - 1), held=0x8000), dict(page_table=0x70000, held=o.held + 4)):
+        assert lib.quoka_pages_fork(at, ctypes.byref(_owners(**kw)), AT, AT, OTHER, OTHER, AT, WS, BIG, None) == 1   # in part
     child = ctypes.byref(_owners(page_table=0x7000, held=0x8000))
+    later = ctypes.c_void_p(AT.value + 4)
+    for args in ((AT, AT, later, OTHER, AT), (AT, AT, OTHER, later, AT)):   # outputs over the lengths
+        assert lib.quoka_pages_fork(at, child, *args, WS, BIG, None) == 1
     for args in ((NULL, AT, OTHER, OTHER, AT), (AT, NULL, OTHER, OTHER, AT), (AT, AT, NULL, OTHER, AT), (AT, AT, OTHER, NULL, AT),
                  (AT, AT, OTHER, OTHER, NULL), (AT, AT, OTHER, AT, AT)):   # (the last: lengths in and out in one place)
         assert lib.quoka_pages_fork(at, child, *args, WS, BIG, None) == 1
@@ -151,6 +156,7 @@ def test_bad_pointers_of_a_verification_are_refused():
         args = [AT, AT, AT, AT, None, AT, AT]
         args[i] = NULL
         assert lib.quoka_verify_draft(s, *args, WS, BIG, None) == 1
+    assert lib.quoka_verify_draft(s, AT, AT, AT, AT, OTHER, OTHER, AT, WS, BIG, None) == 1   # lengths in, accepted tokens out
     assert lib.quoka_verify_draft(s, ODD, AT, AT, AT, None, AT, AT, WS, BIG, None) == 1
     assert lib.quoka_verify_draft(s, AT, ODD, AT, AT, None, AT, AT, WS, BIG, None) == 1
     for ws, size, code in ((NULL, BIG, 1), (ctypes.c_void_p(0x10010), BIG, 3), (WS, ctypes.c_size_t(n.value - 1), 3)):

@@ -518,6 +518,44 @@ def test_copied_rows_keep_their_positions(case, layout):
         _moved(before, _pool_bits(pool), src, dst)
 
 
+def test_rows_that_the_source_has_no_page_for_are_dropped():
+    """Entries that name no page of the pool, and positions past the source's table: what is in their place stays as it was."""
+    pk, rng = _pk(), np.random.default_rng(56)
+    pool = P.Pool(rng, [_rows(rng, 64, 2, 64, "bf16")], [_rows(rng, 64, 2, 64, "bf16")], 2, 64, 16, "bf16", False)
+    source = pool.cache()
+    pool.dev_table[0, 1] = -1
+    pool.dev_table[0, 3] = pool.k_pages.shape[0]
+    there = [torch.full((8, 2, 16, 64), 7.0, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    target = pk.PagedCache(*there, _ints([list(range(8))]))
+    shape = bytes(target._shape)
+    target.copy(source, lens=_ints([128]), max_rows=128)   # (the source's table has four pages)
+    for page in range(8):
+        for x, y in zip(there, (pool.k_pages, pool.v_pages)):
+            assert torch.equal(x[page], y[int(pool.table[0, page])]) if page in (0, 2) else bool((x[page] == 7.0).all())
+    for x in there:
+        x.fill_(7.0)
+    idx = torch.arange(60, 0, -1, dtype=torch.int32, device=DEV).expand(1, 2, 60).contiguous()
+    target.compact(source, idx, _ints([[60, 60]]))
+    for j in range(60):
+        t = 60 - j
+        for x, y in zip(there, (pool.k_pages, pool.v_pages)):
+            got = x[j // 16, :, j % 16]
+            assert torch.equal(got, y[int(pool.table[0, t // 16]), :, t % 16]) if t // 16 in (0, 2) else bool((got == 7.0).all())
+    assert bytes(target._shape) == shape   # (calls share nothing that they change)
+
+
+def test_tensors_of_the_host_are_refused():
+    pk = _pk()
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32)  # noqa: E731
+    cache, other = (pk.PagedCache(torch.zeros(4, 2, 16, 64), torch.zeros(4, 2, 16, 64), ints([0, 1])) for _ in range(2))
+    seqs = pk.PagedSequences.allocate(4, 16, 1, 4, "cpu")
+    drafts = pk.DraftBuffers(torch.zeros(1, 3, 9), ints([0, 1]), torch.zeros(1, 3))
+    for call in (lambda: other.copy(cache, lens=ints(3)), lambda: other.compact(cache, torch.zeros(1, 2, 3, dtype=torch.int32), torch.ones(1, 2, dtype=torch.int32)),
+                 lambda: seqs.resize(ints(3)), lambda: seqs.another(1).fork(seqs, ints(0), ints(3)), drafts.verify):
+        with pytest.raises(ValueError, match="no GPU"):
+            call()
+
+
 def test_a_cache_is_copied_into_another_pool():
     """No parents and one page table for both: the same sequences in a pool of other strides."""
     pk, rng = _pk(), np.random.default_rng(54)
