@@ -243,7 +243,7 @@ def test_drafts_refuse_tensors_that_do_not_fit():
 
 
 def test_calls_for_another_device_than_the_current_one_are_refused(monkeypatch):
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(pk.binding, "_device", lambda: 0)
     pk.binding._here(None)
     pk.binding._here(0)
     with pytest.raises(ValueError):

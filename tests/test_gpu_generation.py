@@ -527,7 +527,7 @@ def test_rows_that_the_source_has_no_page_for_are_dropped():
     pool.dev_table[0, 3] = pool.k_pages.shape[0]
     there = [torch.full((8, 2, 16, 64), 7.0, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
     target = pk.PagedCache(*there, _ints([list(range(8))]))
-    shape = bytes(target._shape)
+    one, shape = target._moves(source, 64, 3), bytes(target._moves(source, 64, 3))
     target.copy(source, lens=_ints([128]), max_rows=128)   # (the source's table has four pages)
     for page in range(8):
         for x, y in zip(there, (pool.k_pages, pool.v_pages)):
@@ -541,7 +541,7 @@ def test_rows_that_the_source_has_no_page_for_are_dropped():
         for x, y in zip(there, (pool.k_pages, pool.v_pages)):
             got = x[j // 16, :, j % 16]
             assert torch.equal(got, y[int(pool.table[0, t // 16]), :, t % 16]) if t // 16 in (0, 2) else bool((got == 7.0).all())
-    assert bytes(target._shape) == shape   # (calls share nothing that they change)
+    assert bytes(one) == shape   # (calls share nothing that they change)
 
 
 def test_tensors_of_the_host_are_refused():
