@@ -240,13 +240,21 @@ __global__ __launch_bounds__(64 * WAVES) void cross_few(Dims dm, PagedArgs a) {
 template <int D>
 constexpr int kFewWaves = D == 64 ? 12 : 8;   // as many as LDS has room for
 
-// Three rounds of tiles (two at d 128): us of this kernel and of the two launches that share lists (paged_decode), 12 heads, d 64, one or eight
-// sequences of 64 states 5.0 / 7.4, 500 6.3 / 7.8, 1000 7.7 / 8.0, 2000 11.0 / 8.2; 8 heads of 4, d 128, 64 states 5.0 / 7.5, 500 8.0 / 8.5, 1000
-// 10.8 / 8.6.  (Batches that fill the chip gain beyond that where all are equally long, 32 of 4000 92.6 / 102, and lose where they are not,
-// which the host does not know.)
+// Which lists are few, by rounds of tiles and blocks (a compute unit has one at a time); us of this kernel and of the two launches that share
+// lists (paged_decode), all lists equal, and of lists between an eighth of it and the longest.
+//   Few blocks: three rounds (two at d 128).  12 heads, d 64, one or eight sequences of 64 states 5.0 / 7.4, 500 6.3 / 7.8, 1000 7.7 / 8.0,
+//   2000 11.0 / 8.2; 8 heads of 4, d 128, 64 5.0 / 7.5, 500 8.0 / 8.5, 1000 10.8 / 8.6.
+//   96 blocks: four; 128 to 256, half of the compute units and all of them: eight.  32 sequences, d 64, 8 heads of 4, 1500 states 19.0 / 22.4 and
+//   14.6 / 17.4 (200 at least); of up to 3000 0.83 - 0.97 of the time, of 6000 0.85 - 1.15; d 128, 1500 31.8 / 35.8 and 24.7 / 26.5, of up to 2000
+//   0.85 - 1.03, of 4000 0.8 - 1.08.  The most that such a batch may lose are lists that differ at 100 blocks, 1.04 (four rounds; eight 1.14).
+//   More than 256: three (two) again, up to 768.  12 heads, d 64, 500 states, 300 blocks 0.8 - 0.92 of the time, 700 1.0 - 1.02, 1030 1.11 - 1.23,
+//   2000 1.23 - 1.27, since blocks with 129 or 152 KB of LDS leave a compute unit to one sequence after another.
 bool cross_few_applies(const Dims& dm) {
-  const int tiles = (dm.T_max + kPdTile - 1) / kPdTile;
-  return dm.d == 64 ? tiles <= 3 * kFewWaves<64> : tiles <= 2 * kFewWaves<128>;
+  const int tiles = (dm.T_max + kPdTile - 1) / kPdTile, waves = dm.d == 64 ? kFewWaves<64> : kFewWaves<128>;
+  const long long blocks = (long long)dm.b * dm.n_kv;
+  if (blocks > 768) return false;
+  const int rounds = blocks > 256 || blocks < 96 ? (dm.d == 64 ? 3 : 2) : blocks < 128 ? 4 : 8;
+  return tiles <= rounds * waves;
 }
 
 hipError_t launch_cross_few(const Dims& dm, bool fp8, const PagedArgs& a, hipStream_t st) {
