@@ -1,6 +1,8 @@
 // The bf16 attention kernel (attn_mfma.hip.h) over states in pages (quoka_cross_attn): every query sees all of its sequence's cached rows.
 //
 // Without a mask all row blocks of a launch take equally long, and the tiles are those of the list alone.
+// Bound by matrix and vector instructions together (matrix units 60 % busy at the clock it runs at).  Measured: 2048 tokens over 16384 states, 32/8 heads
+// of 128, 474 - 486 us on four cards (1.13 - 1.16 PFLOP/s; a large matrix product reaches 1.36).
 #include "attn_mfma.hip.h"
 
 namespace quoka {

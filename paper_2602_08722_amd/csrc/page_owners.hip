@@ -6,6 +6,9 @@
 // entry that gets it.  Three steps, each of which uses what the one before has completed: entries that go or are shared, free pages counted
 // beside the sum of what the sequences lack, free pages to entries.  Small pools and batches take them in one launch of one block, others in
 // three launches (a block a sequence, a tile of pages a block).
+// Bound by the chain: lengths, table, counts' atomics, counts, table.  Measured: a step of 16 sequences over 8192 pages 3 - 4 us, of 256 over 262144
+// 2.7 + 2.5 + 4.3; forks of 16 sequences 6.2, of 256 with 130816 entries 3.4 + 5.3.  (Counts fetched ahead of the scans, whether pages are wanted or not:
+// 0.6 us more for a step that wants none, which most are, otherwise the same.)
 #include "common.hip.h"
 #include "kernels.h"
 

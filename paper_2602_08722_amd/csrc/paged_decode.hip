@@ -12,6 +12,7 @@
 // Measured: one token for 32 sequences of 1024 - 32768, 8-bit rows of 8 heads of 128 (1.15 GB), 204 us (5.6 TB/s); for 8 of 4096 - 65536,
 // 16-bit rows (1.32 GB), 231 (5.7 TB/s).  One sequence of 8192 in 8 bits 12.8: 7 until the last partial has left (1.6 arguments and length,
 // 0.5 pages, 1 the first rows, then one or two tiles and the merge of the block's waves), the rest the second launch.
+// Over states (quoka_cross_attn; the chunk's own rows are not among the keys): the 32 above 196 us (1.09 GB, 5.6 TB/s).
 //
 // The tiles of all sequences lie one behind the other, and every block of a KV head takes as many of them: the end of one
 // sequence, whole ones, the beginning of another, or, where that costs nothing, a part of one (PdPlan).  A part of a sequence leaves a
