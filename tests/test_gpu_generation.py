@@ -88,7 +88,18 @@ CROSS_CASES = [
     dict(dtype="bf16", fp8=False, n_q=16, n_kv=1, d=128, page_len=32, C=1, lens=[0] * 30 + [20000] + [0, 40] * 15),   # a long one among many
     dict(dtype="bf16", fp8=False, n_q=8, n_kv=2, d=128, page_len=16, C=1, lens=[0, 0]),
     dict(dtype="bf16", fp8=False, n_q=4, n_kv=1, d=64, page_len=64, C=1, lens=[30000]),
+    # blocks for each sequence and KV head that fill half of the chip, all of it, and more than that
+    dict(dtype="bf16", fp8=False, n_q=16, n_kv=4, d=64, page_len=64, C=1, lens=[2900 - 89 * i for i in range(32)]),
+    dict(dtype="bf16", fp8=True, n_q=12, n_kv=4, d=128, page_len=32, C=2, lens=[65 * i for i in range(25)], chunks=[1 + i % 2 for i in range(25)]),
+    dict(dtype="bf16", fp8=False, n_q=12, n_kv=12, d=128, page_len=16, C=1, lens=[2047 - 90 * i for i in range(20)]),
+    dict(dtype="bf16", fp8=True, n_q=12, n_kv=12, d=64, page_len=64, C=1, lens=[(53 * i) % 997 for i in range(30)]),
+    dict(dtype="bf16", fp8=False, n_q=12, n_kv=12, d=64, page_len=16, C=1, lens=[(17 * i) % 131 for i in range(70)]),
+    dict(dtype="bf16", fp8=True, n_q=40, n_kv=40, d=128, page_len=16, C=1, lens=[33 * i for i in range(24)]),
+    dict(dtype="bf16", fp8=False, n_q=520, n_kv=520, d=64, page_len=16, C=1, lens=[2000, 0, 31]),
     # chunks: row blocks of four and eight, shared lists, whole ones
+    dict(dtype="bf16", fp8=False, n_q=10, n_kv=10, d=64, page_len=64, C=270, lens=[300 - 23 * i for i in range(13)]),       # four (260 groups of eight)
+    dict(dtype="bf16", fp8=True, n_q=10, n_kv=10, d=128, page_len=16, C=270, lens=[20 * i for i in range(13)], chunks=[270 - 20 * i for i in range(13)]),
+    dict(dtype="bf16", fp8=True, n_q=9, n_kv=3, d=64, page_len=16, C=300, lens=[9 * i for i in range(20)]),                 # eight
     dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=64, C=200, lens=[700]),
     dict(dtype="bf16", fp8=False, n_q=8, n_kv=2, d=64, page_len=16, C=77, lens=[0, 130]),
     dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=32, C=129, lens=[1, 511, 64, 65, 128, 129]),
@@ -118,6 +129,9 @@ CROSS_CASES = [
     dict(dtype="f32", fp8=False, n_q=4, n_kv=2, d=64, page_len=16, C=40, lens=[(97 * i) % 700 for i in range(140)], chunks=[(11 * i) % 41 for i in range(140)]),
     dict(dtype="f32", fp8=False, n_q=2, n_kv=1, d=128, page_len=16, C=3, lens=[9000 - 700 * i for i in range(13)]),
     dict(dtype="f32", fp8=True, n_q=32, n_kv=8, d=64, page_len=16, C=600, lens=[700, 300], chunks=[600, 100]),   # more row blocks than a round
+    dict(dtype="f32", fp8=False, n_q=12, n_kv=12, d=128, page_len=16, C=40, lens=[16]),
+    dict(dtype="f32", fp8=True, n_q=6, n_kv=2, d=64, page_len=8, C=90, lens=[12, 0, 1, 7], chunks=[90, 5, 0, 61]),
+    dict(dtype="f32", fp8=False, n_q=8, n_kv=2, d=128, page_len=16, C=1000, lens=[2, 3], chunks=[1000, 999]),
 ]
 
 
@@ -142,6 +156,64 @@ def test_cross_attention_over_other_strides_and_entries(case):
     buf.cross_attn()
     torch.cuda.synchronize()
     _check_cross(case, buf, pool, q, chunks)
+
+
+@pytest.mark.parametrize("case", [
+    dict(dtype="bf16", fp8=False, n_q=8, n_kv=2, d=128, page_len=16, C=1, lens=[500, 77]),
+    dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=64, page_len=16, C=2, lens=[5000, 900]),
+    dict(dtype="bf16", fp8=False, n_q=8, n_kv=2, d=64, page_len=16, C=150, lens=[700, 77]),
+    dict(dtype="bf16", fp8=True, n_q=32, n_kv=8, d=128, page_len=64, C=280, lens=[600]),
+], ids=_ids)
+@pytest.mark.parametrize("rising", [False, True])
+def test_cross_attention_of_wide_logits(case, rising):
+    """Logits of a standard deviation of 8, and such that grow along the states, so that a row's maximum moves on in every tile."""
+    pool, q, chunks = _cross_problem(case, 44, scale=8.0)
+    if rising:   # (the rows as they are kept, in the other order: the ones that the first query likes least come first; no input of other cases)
+        for i, n in enumerate(case["lens"]):
+            k, v = pool.k[i], pool.v[i]
+            order = np.argsort(k[:, 0] @ q[i, 0, 0].astype(np.float64))
+            at = torch.tensor(np.arange(n), device=DEV)
+            pages, slots = torch.tensor(pool.table[i], device=DEV)[at // case["page_len"]], at % case["page_len"]
+            o = torch.tensor(order, device=DEV)
+            for x in (pool.k_pages, pool.v_pages):
+                bits = x.view(torch.uint8) if x.element_size() == 1 else x
+                bits[pages, :, slots] = bits[pages[o], :, slots[o]]
+            if case["fp8"]:
+                for s in (pool.k_scale, pool.v_scale):
+                    s[pages, :, slots] = s[pages[o], :, slots[o]]
+            pool.k[i], pool.v[i] = k[order], v[order]
+    buf = _cross_buffers(case, pool, q)
+    buf.cross_attn()
+    torch.cuda.synchronize()
+    _check_cross(case, buf, pool, q, chunks)
+
+
+def test_calls_on_two_streams_at_once():
+    """Two buffers over one cache, and two pools of pages, each on a stream of its own."""
+    pk = _pk()
+    cases = [dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=16, C=C, lens=[4000, 90]) for C in (1, 70)]
+    pool, q, chunks = _cross_problem(cases[0], 45)
+    many = P.store(np.random.default_rng(46).standard_normal((2, 8, 70, 128)), "bf16")
+    bufs = [_cross_buffers(case, pool, x) for case, x in zip(cases, (q, many))]
+    seqs = [pk.PagedSequences.allocate(4000, 16, 5, 400) for _ in range(2)]
+    lens = [_ints([100, 0, 4000, 33, 17]), _ints([7, 6000, 1, 0, 800])]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(20):
+        for s, buf, seq, n in zip(streams, bufs, seqs, lens):
+            with torch.cuda.stream(s):
+                seq.resize(n)
+                buf.cross_attn()
+                seq.resize(torch.zeros_like(n))
+                seq.resize(n)
+    torch.cuda.synchronize()
+    for case, buf, x in zip(cases, bufs, (q, many)):
+        _check_cross(case, buf, pool, x, [case["C"]] * 2)
+    for seq, n in zip(seqs, lens):
+        book = G.Book([0] * 4000, 16, 5, 400)
+        book.resize(n.tolist())
+        assert np.array_equal(seq.page_table.cpu().numpy(), book.table()) and seq.ref.tolist() == book.ref
 
 
 @pytest.mark.parametrize("C", [1, 70])
