@@ -9,7 +9,7 @@
 // element), and a wave a run of neighbouring entries: the sums of whole waves say which one the random number points into, and that one
 // alone adds up its entries in order.
 // Measured: one sequence, 4 tokens that were looked up, vocabulary 32003, 3.7 us and 3.3 (two launches of a chain of fetches each: 8.3 a call);
-// 64 sequences of up to 7, 131072 float32, 12.3 and 5.1 (67 MB in the first: 5.5 TB/s).  One launch, a block a sequence, 16 us where this takes 7.
+// 64 sequences of up to 7, 131072 float32, 12.3 and 5.1 (67 MB in the first: 5.5 TB/s); vocabulary 1000 in one launch 3.3.
 #include <type_traits>
 
 #include "common.hip.h"
@@ -102,9 +102,16 @@ struct Piece {
       for (int e = 0; e < N; ++e) x[e] = v0 + e < V ? row[v0 + e] : T(0);
     }
   }
-  __device__ __forceinline__ double at(int e) const {
-    if constexpr (sizeof(T) == 4) return (double)x[e];
-    else return (double)bf16_bits_to_f32(x[e]);
+  // Values worked out before this line are not kept for use after it (twice as wide as what they come from, they would not fit the registers).
+  __device__ __forceinline__ void forget() {
+    typedef uint32_t four __attribute__((ext_vector_type(4)));
+    four bits = __builtin_bit_cast(four, x);
+    asm volatile("" : "+v"(bits));
+    x = __builtin_bit_cast(vec, bits);
+  }
+  __device__ __forceinline__ float at(int e) const {
+    if constexpr (sizeof(T) == 4) return x[e];
+    else return bf16_bits_to_f32(x[e]);
   }
 };
 
@@ -126,33 +133,37 @@ struct Run {
       for (int j = 0; j < J; ++j) q[j].load(r.q, v0 + j * N * kWave, V);
     }
   }
-  __device__ __forceinline__ double all(int j, int e) const { return weight_of(p[j].at(e)); }
-  __device__ __forceinline__ double left(int j, int e) const {   // what remains of p
-    return weight_of(p[j].at(e) - (has_q ? q[j].at(e) : x == j * N * kWave + e ? 1.0 : 0.0));
+  __device__ __forceinline__ void forget() {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      p[j].forget();
+      q[j].forget();
+    }
   }
-  __device__ __forceinline__ double weight(bool use_left, int j, int e) const { return use_left ? left(j, e) : all(j, e); }
+  __device__ __forceinline__ double all(int j, int e) const { return weight_of(p[j].at(e)); }
+  __device__ __forceinline__ double left(int j, int e) const {   // what remains of p: weight_of((double)p - (double)q)
+    const float from = p[j].at(e), off = has_q ? q[j].at(e) : x == j * N * kWave + e ? 1.f : 0.f;
+    return from > off && from < INFINITY && off > -INFINITY ? (double)from - (double)off : 0.0;
+  }
 
   // The lowest entry of positive weight behind which `before` and the entries up to it are more than `point`; should there be none, the last
   // one of positive weight (sums of two orders may leave the point a rounding past the end); as a place in the row, -1: nothing weighs.
-  __device__ __forceinline__ int find(bool use_left, double before, double point, int first) const {
+  template <typename LEFT>
+  __device__ __forceinline__ int find(LEFT, double before, double point, int first) const {
     const int lane = threadIdx.x & 63;
-    double w[J][N], s[J], incl[J];
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      s[j] = 0.0;
-#pragma unroll
-      for (int e = 0; e < N; ++e) s[j] += w[j][e] = weight(use_left, j, e);
-      incl[j] = wave_incl_scan(s[j]);
-    }
     int last = -1;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      double run = before + (incl[j] - s[j]);
+      double w[N], s = 0.0;
+#pragma unroll
+      for (int e = 0; e < N; ++e) s += w[e] = LEFT::value ? left(j, e) : all(j, e);
+      const double incl = wave_incl_scan(s);
+      double run = before + (incl - s);
       int hit = -1, mine = -1;
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        run += w[j][e];
-        if (w[j][e] > 0.0) {
+        run += w[e];
+        if (w[e] > 0.0) {
           mine = e;
           if (run > point && hit < 0) hit = e;
         }
@@ -162,7 +173,7 @@ struct Run {
       if (hits != 0) return __builtin_amdgcn_readlane(at + hit, (int)__builtin_ctzll(hits));
       const unsigned long long some = __builtin_amdgcn_ballot_w64(mine >= 0);
       if (some != 0) last = __builtin_amdgcn_readlane(at + mine, 63 - (int)__builtin_clzll(some));
-      before += last_lane(incl[j]);
+      before += last_lane(incl);
     }
     return last;
   }
@@ -177,7 +188,7 @@ __device__ __forceinline__ void put_tokens(const VerifyArgs& a, int b, int acc, 
     a.tokens_out[(long long)b * (a.n + 1) + i] = i < acc ? a.tokens[(long long)b * a.n + i] : i == acc ? y : -1;
 }
 
-// Two launches: the sums of parts of kVfPart entries, a wave each; then the part that the random number points into, and the token in it.
+// Longer vocabularies in two launches: the sums of parts of kVfPart entries, a wave each; then the part that the random number points into, and the token in it.
 constexpr int kVfThreads = 256, kVfPart = 1024;
 
 // sums: [b, parts] of what is left and of p
@@ -283,8 +294,51 @@ __global__ __launch_bounds__(kWave) void verify_pick(VerifyArgs a, const double2
     }
     Run<T, J> run;
     run.load(r, part * kVfPart, a.V);
-    y = run.find(use_left, before, point, part * kVfPart);
+    y = use_left ? run.find(std::true_type{}, before, point, part * kVfPart) : run.find(std::false_type{}, before, point, part * kVfPart);
   }
+  put_tokens(a, b, acc, y, lane);
+}
+
+// Short vocabularies in one launch: a block a sequence, a wave a run of J pieces; the entries stay in registers from their sums to the search.
+constexpr int kVoThreads = 1024, kVoWaves = kVoThreads / kWave;
+
+template <typename T, int J>
+__global__ __launch_bounds__(kVoThreads) void verify_one(VerifyArgs a) {
+  constexpr int N = Piece<T>::N, kRun = N * kWave * J;
+  __shared__ double sums[kVoWaves];
+  const int b = blockIdx.x, lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const double u = draw_of(a, b);
+  const int n = drafted(a, b), acc = accepted<T>(a, b, n), first = w * kRun;
+  Run<T, J> run;
+  run.load(rows_of<T>(a, b, n, acc), first, a.V);
+  double total, before;
+  int chosen;   // the wave that the random number points into
+  auto add_up = [&](auto left) __attribute__((always_inline)) {
+    double s = 0.0;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) s += decltype(left)::value ? run.left(j, e) : run.all(j, e);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    s = wave64_sum(s);
+    __syncthreads();
+    if (lane == 0) sums[w] = s;
+    __syncthreads();
+    const double mine = lane < kVoWaves ? sums[lane] : 0.0, incl = wave_incl_scan(mine);
+    total = last_lane(incl);
+    before = incl - mine;
+    const unsigned long long hits = __builtin_amdgcn_ballot_w64(mine > 0.0 && before + mine > u * total), some = __builtin_amdgcn_ballot_w64(mine > 0.0);
+    chosen = hits != 0 ? (int)__builtin_ctzll(hits) : some != 0 ? 63 - (int)__builtin_clzll(some) : 0;
+    run.forget();
+  };
+  add_up(std::true_type{});
+  const bool use_left = total > 0.0 || acc >= n;
+  if (!use_left) add_up(std::false_type{});   // (nothing is left behind a refusal; the same for all waves)
+  if (w != chosen) return;
+  if (lane == 0) a.n_accepted[b] = acc;
+  int y = -1;
+  if (total > 0.0) y = use_left ? run.find(std::true_type{}, lane_of(before, chosen), u * total, first) : run.find(std::false_type{}, lane_of(before, chosen), u * total, first);
   put_tokens(a, b, acc, y, lane);
 }
 
@@ -295,6 +349,22 @@ size_t verify_ws_bytes(int batch, int vocab) { return (size_t)batch * vf_parts(v
 hipError_t launch_verify(const VerifyArgs& a, int dtype, void* ws, hipStream_t st) {
   auto launch = [&](auto one) {
     using T = decltype(one);
+    // One launch up to 24576 float32 entries, 16384 bfloat16 ones (whose pieces have twice as many conversions to 64 bits in them, which are most of
+    // a piece's time: 0.7 us, 1.9).  Us of one and of two launches, 1 to 128 sequences: float32, 4096 entries 3.2 - 4.3 / 6.8 - 8.6, 8000 4.0 - 4.8 / 6.2 -
+    // 8.3, 16000 4.4 - 6.3 / 6.0 - 8.7, 24000 5.5 - 8.3 / 6.6 - 10.3, 32003 (8 pieces) 6.6 - 10.1 / 6.3 - 12.0; bfloat16, 8000 4.2 - 5.0 / 6.8 - 8.5, 16000
+    // 4.9 - 6.5 / 7.0 - 8.5, 24000 (4 pieces) 6.9 - 10.4 / 6.5 - 9.4.
+    constexpr int kStep = Piece<T>::N * kWave * kVoWaves;   // entries of a block whose waves have one piece
+    auto one_launch = [&](auto pieces) {
+      hipLaunchKernelGGL((verify_one<T, decltype(pieces)::value>), dim3(a.b), dim3(kVoThreads), 0, st, a);
+      return hipGetLastError();
+    };
+    using std::integral_constant;
+    if (a.V <= kStep) return one_launch(integral_constant<int, 1>{});
+    if (a.V <= 2 * kStep) return one_launch(integral_constant<int, 2>{});
+    if constexpr (sizeof(T) == 4) {
+      if (a.V <= 4 * kStep) return one_launch(integral_constant<int, 4>{});
+      if (a.V <= 6 * kStep) return one_launch(integral_constant<int, 6>{});
+    }
     const int parts = vf_parts(a.V), waves = kVfThreads / kWave;
     hipLaunchKernelGGL((verify_parts<T>), dim3((parts + waves - 1) / waves, a.b), dim3(kVfThreads), 0, st, a, static_cast<double2*>(ws), parts);
     hipLaunchKernelGGL((verify_pick<T>), dim3(a.b), dim3(kWave), 0, st, a, static_cast<const double2*>(ws), parts);

@@ -305,6 +305,19 @@ def test_verification(b, n, V, lens, lookup, dtype):
         _check_verified(got, p, q, tokens, uniform, lens)
 
 
+@pytest.mark.parametrize("dtype,V", [("f32", V + i) for V in (4096, 8192, 16384, 24576) for i in (0, 1)] +
+                         [("bf16", V + i) for V in (8192, 16384) for i in (0, 1)] + [("f32", 63), ("f32", 257), ("bf16", 1), ("bf16", 4095)])
+@pytest.mark.parametrize("lookup", [False, True])
+def test_verification_of_vocabularies_around_a_blocks_pieces(dtype, V, lookup):
+    rng = np.random.default_rng(V)
+    for lens in (None, [0, 3, 1, 2, 3]):
+        p, q, tokens, uniform = _verify_problem(rng, 5, 3, V, dtype, lookup)
+        uniform[0, :3] = 0.0    # accepts what has any probability
+        uniform[1, :3] = 1.0
+        uniform[:, 3] = [0.0, 1.0, 0.5, 1.0 - 2.0 ** -24, 1e-30]
+        _check_verified(_verified(p, q, tokens, uniform, dtype, lens), p, q, tokens, uniform, lens)
+
+
 @pytest.mark.parametrize("V", [5, 33000])
 def test_verification_of_what_distributions_should_not_hold(V):
     """NaN, infinities, negative entries, rows without any weight, tokens outside the vocabulary, random numbers outside [0, 1)."""
