@@ -14,7 +14,7 @@ LIB = os.path.join(PKG, "libquoka.so")
 
 SOURCES = ["api.hip", "select_queries.hip", "score_keys.hip", "topk_keys.hip", "select_keys.hip", "score_stream.hip", "attn_mfma.hip", "attn_decode.hip", "attn_f32.hip",
            "pages.hip", "paged_attn.hip", "paged_decode.hip", "attn_mfma_paged.hip",
-           "attn_mfma_states.hip", "cross_few.hip", "page_rows.hip", "page_owners.hip", "verify.hip", "probes.hip"]
+           "attn_mfma_states.hip", "cross_few.hip", "cross_rows.hip", "page_rows.hip", "page_owners.hip", "verify.hip", "probes.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

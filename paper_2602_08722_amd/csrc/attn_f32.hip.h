@@ -591,7 +591,7 @@ inline int f32_splits(const Dims& dm, bool sparse) {
 // waves a block take as long, and so do two blocks of four a SIMD with K by way of LDS), the partials' launch 6.  Of shares that take equally
 // long in a batch whose lists are all of `units`, the fewest: shorter lists have fewer, and their other blocks end at once.
 constexpr long long kMostStateParts = 2048;   // partials of 32 rows
-inline int f32_state_units(const Dims& dm) {
+inline int f32_state_units(const Dims& dm, float* us_of = nullptr) {
   const long long blocks = f32_blocks(dm), units = f32_units(dm, false, false), rounds_of_waves = (units + kFaWaves - 1) / kFaWaves;
   long long best = rounds_of_waves;
   float best_us = 1e30f;
@@ -604,6 +604,7 @@ inline int f32_state_units(const Dims& dm) {
       best = waves;
     }
   }
+  if (us_of != nullptr) *us_of = best_us;
   return (int)best * kFaWaves;
 }
 inline int f32_state_shares(const Dims& dm, int per) { return (int)((f32_units(dm, false, false) + per - 1) / per); }

@@ -240,6 +240,7 @@ __global__ __launch_bounds__(64 * WAVES) void cross_few(Dims dm, PagedArgs a) {
 template <int D>
 constexpr int kFewWaves = D == 64 ? 12 : 8;   // as many as LDS has room for
 
+// (One row, and two, over fewer states yet: cross_rows.hip.)
 // Which lists are few, by rounds of tiles and blocks (a compute unit has one at a time); us of this kernel and of the two launches that share
 // lists (paged_decode), all lists equal, and of lists between an eighth of it and the longest.
 //   Few blocks: three rounds (two at d 128).  12 heads, d 64, one or eight sequences of 64 states 5.0 / 7.4, 500 6.3 / 7.8, 1000 7.7 / 8.0,

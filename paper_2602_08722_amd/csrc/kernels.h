@@ -155,6 +155,10 @@ hipError_t launch_paged_decode(const Dims& dm, bool fp8, const PagedArgs& a, flo
 // cross attention of as many, where a sequence's states are few enough for one block
 bool cross_few_applies(const Dims& dm);
 hipError_t launch_cross_few(const Dims& dm, bool fp8, const PagedArgs& a, hipStream_t st);
+// cross attention of up to four query rows per KV head (dtype: of the queries), float32 calls as their times say
+bool cross_rows_take_bf16(const Dims& dm);
+float cross_rows_us(const Dims& dm);
+hipError_t launch_cross_rows(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, hipStream_t st);
 size_t paged_attn_ws_floats(const Dims& dm, int dtype);
 hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float* part, hipStream_t st, bool own = true);
 

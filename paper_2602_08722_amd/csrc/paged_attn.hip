@@ -95,15 +95,26 @@ __global__ __launch_bounds__(kPsThreads) void paged_f32_short(Dims dm, PagedArgs
 // Cross attention: a wave a row or units of 32 states, by what either takes; us, units / a wave a row: 12 heads, d 64, 16 tokens over 1 state
 // 7.6 / 5.2, over 16 7.5 / 6.6, over 32 7.5 / 8.7, 1000 over 1 13.6 / 11.5, over 8 13.4 / 16.6; d 128, 40 tokens over 16 10.4 / 7.4, over 32
 // 10.5 / 10.2; 8 x 4 heads of 8, d 128, 40 over 4 19.8 / 17.7, over 16 19.4 / 26.5.
-static bool states_are_few(const Dims& dm) {
+// Where the query rows are few too (cross_rows, a block a sequence and KV head): that, unless a wave a row takes less, or units less than 1 / 0.85 of it
+// (which its figure is above the measured ones where partials are many): 8 x 4 rows, d 64, 300 states 13.1 -> 8.6 us, of 1000 14.1 (17.3);
+// 12 heads, 1000 states 22.7 -> 11.5, one sequence of 2000 14.1 -> 12.2, of 4000 15.1 (21.8).
+enum StateForm { kWaveARow, kFewRows, kStateUnits };
+static StateForm state_form(const Dims& dm) {
   const float rows = (float)dm.b * (float)dm.n_q * (float)dm.C * 1e-3f, n = (float)dm.T_cap;
-  if (dm.d == 64) return 4.6f + 0.11f * n + rows * (0.55f + 0.05f * n) < 7.5f + 0.7f * rows;
-  return 4.8f + 0.13f * n + rows * (0.92f + 0.075f * n) < 9.8f + 1.06f * rows;
+  const float row_us = dm.d == 64 ? 4.6f + 0.11f * n + rows * (0.55f + 0.05f * n) : 4.8f + 0.13f * n + rows * (0.92f + 0.075f * n);
+  const float few_us = cross_rows_us(dm);
+  // (with rows as few as cross_rows takes, row_us is 1 above what is measured)
+  if (row_us < (dm.d == 64 ? 7.5f + 0.7f * rows : 9.8f + 1.06f * rows) && row_us < few_us + 1.0f) return kWaveARow;
+  float units_us;
+  f32_state_units(dm, &units_us);
+  return few_us < 0.85f * units_us ? kFewRows : kStateUnits;
 }
 
 template <bool FP8, int D, bool OWN>
 static hipError_t launch_paged_f32(const Dims& dm, const PagedArgs& a, float* part, hipStream_t st) {
-  if (OWN ? attn_f32_is_short(dm, a.k_idx != nullptr) : states_are_few(dm)) {
+  const StateForm form = OWN ? kStateUnits : state_form(dm);
+  if (form == kFewRows) return launch_cross_rows(dm, QUOKA_F32, FP8, a, st);
+  if (OWN ? attn_f32_is_short(dm, a.k_idx != nullptr) : form == kWaveARow) {
     const dim3 grid((dm.C + kPsThreads / 64 - 1) / (kPsThreads / 64), dm.n_q, dm.b);
     hipLaunchKernelGGL((paged_f32_short<FP8, D, OWN>), grid, dim3(kPsThreads), 0, st, dm, a);
     return hipGetLastError();
@@ -121,6 +132,7 @@ size_t paged_attn_ws_floats(const Dims& dm, int dtype) {
 
 hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float* part, hipStream_t st, bool own) {
   if (dtype == QUOKA_BF16) {
+    if (!own && cross_rows_take_bf16(dm)) return launch_cross_rows(dm, dtype, fp8, a, st);
     if (attn_decode_applies(dm))
       return !own && cross_few_applies(dm) ? launch_cross_few(dm, fp8, a, st) : launch_paged_decode(dm, fp8, a, part, st, own);
     return own ? launch_paged_attn_bf16(dm, fp8, a, part, st) : launch_cross_attn_bf16(dm, fp8, a, part, st);

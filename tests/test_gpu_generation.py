@@ -96,6 +96,12 @@ CROSS_CASES = [
     dict(dtype="bf16", fp8=False, n_q=12, n_kv=12, d=64, page_len=16, C=1, lens=[(17 * i) % 131 for i in range(70)]),
     dict(dtype="bf16", fp8=True, n_q=40, n_kv=40, d=128, page_len=16, C=1, lens=[33 * i for i in range(24)]),
     dict(dtype="bf16", fp8=False, n_q=520, n_kv=520, d=64, page_len=16, C=1, lens=[2000, 0, 31]),
+    # one and two rows of a KV head over few states, and over more of many sequences
+    dict(dtype="bf16", fp8=False, n_q=12, n_kv=12, d=64, page_len=64, C=1, lens=[600, 1, 0, 31, 32, 33, 256, 257]),
+    dict(dtype="bf16", fp8=True, n_q=5, n_kv=5, d=128, page_len=16, C=2, lens=[50, 15, 16, 17], chunks=[2, 1, 0, 2]),
+    dict(dtype="bf16", fp8=False, n_q=4, n_kv=2, d=64, page_len=8, C=1, lens=[150, 7]),
+    dict(dtype="bf16", fp8=True, n_q=24, n_kv=24, d=64, page_len=32, C=1, lens=[33 * i for i in range(30)]),
+    dict(dtype="bf16", fp8=False, n_q=20, n_kv=10, d=128, page_len=1, C=1, lens=[600 - 17 * i for i in range(28)], chunks=[i % 2 for i in range(28)]),
     # chunks: row blocks of four and eight, shared lists, whole ones
     dict(dtype="bf16", fp8=False, n_q=10, n_kv=10, d=64, page_len=64, C=270, lens=[300 - 23 * i for i in range(13)]),       # four (260 groups of eight)
     dict(dtype="bf16", fp8=True, n_q=10, n_kv=10, d=128, page_len=16, C=270, lens=[20 * i for i in range(13)], chunks=[270 - 20 * i for i in range(13)]),
@@ -129,6 +135,14 @@ CROSS_CASES = [
     dict(dtype="f32", fp8=False, n_q=4, n_kv=2, d=64, page_len=16, C=40, lens=[(97 * i) % 700 for i in range(140)], chunks=[(11 * i) % 41 for i in range(140)]),
     dict(dtype="f32", fp8=False, n_q=2, n_kv=1, d=128, page_len=16, C=3, lens=[9000 - 700 * i for i in range(13)]),
     dict(dtype="f32", fp8=True, n_q=32, n_kv=8, d=64, page_len=16, C=600, lens=[700, 300], chunks=[600, 100]),   # more row blocks than a round
+    # one to four rows of a KV head over many states, of lengths around tiles and pages, more blocks than compute units
+    dict(dtype="f32", fp8=False, n_q=12, n_kv=12, d=64, page_len=64, C=1, lens=[300, 1, 0, 31, 32, 33, 256, 257]),
+    dict(dtype="f32", fp8=True, n_q=5, n_kv=5, d=64, page_len=16, C=3, lens=[1000, 15, 16, 17], chunks=[3, 1, 0, 2]),
+    dict(dtype="f32", fp8=False, n_q=8, n_kv=2, d=128, page_len=8, C=1, lens=[(37 * i) % 300 for i in range(40)]),
+    dict(dtype="f32", fp8=True, n_q=4, n_kv=2, d=128, page_len=128, C=2, lens=[700, 130], chunks=[1, 2]),
+    dict(dtype="f32", fp8=False, n_q=2, n_kv=1, d=128, page_len=1, C=1, lens=[127, 128, 129]),
+    dict(dtype="f32", fp8=False, n_q=24, n_kv=24, d=64, page_len=32, C=1, lens=[60 * i for i in range(30)]),
+    dict(dtype="f32", fp8=True, n_q=10, n_kv=10, d=128, page_len=64, C=4, lens=[2500 - 90 * i for i in range(28)], chunks=[i % 5 for i in range(28)]),
     dict(dtype="f32", fp8=False, n_q=12, n_kv=12, d=128, page_len=16, C=40, lens=[16]),
     dict(dtype="f32", fp8=True, n_q=6, n_kv=2, d=64, page_len=8, C=90, lens=[12, 0, 1, 7], chunks=[90, 5, 0, 61]),
     dict(dtype="f32", fp8=False, n_q=8, n_kv=2, d=128, page_len=16, C=1000, lens=[2, 3], chunks=[1000, 999]),
@@ -148,6 +162,8 @@ def test_cross_attention(case):
     dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=16, C=1, lens=[300, 77]),
     dict(dtype="bf16", fp8=False, n_q=8, n_kv=2, d=64, page_len=16, C=90, lens=[300, 77]),
     dict(dtype="f32", fp8=True, n_q=8, n_kv=2, d=128, page_len=16, C=40, lens=[300, 77]),
+    dict(dtype="f32", fp8=False, n_q=8, n_kv=4, d=64, page_len=16, C=2, lens=[300, 77]),
+    dict(dtype="f32", fp8=True, n_q=8, n_kv=4, d=128, page_len=16, C=1, lens=[300, 77]),
 ], ids=_ids)
 def test_cross_attention_over_other_strides_and_entries(case):
     """Heads inside tokens, gaps between rows, table entries past a sequence's length that name no page, and room for more states."""
@@ -216,10 +232,10 @@ def test_calls_on_two_streams_at_once():
         assert np.array_equal(seq.page_table.cpu().numpy(), book.table()) and seq.ref.tolist() == book.ref
 
 
-@pytest.mark.parametrize("C", [1, 70])
-def test_cross_attention_from_a_graph_as_lengths_move(C):
+@pytest.mark.parametrize("C,dtype", [(1, "bf16"), (70, "bf16"), (1, "f32"), (30, "f32")])
+def test_cross_attention_from_a_graph_as_lengths_move(C, dtype):
     """Recorded once, replayed with other queries and lengths, a length of none among them."""
-    case = dict(dtype="bf16", fp8=True, n_q=8, n_kv=2, d=128, page_len=16, C=C, lens=[400, 90])
+    case = dict(dtype=dtype, fp8=True, n_q=8, n_kv=2, d=128, page_len=16, C=C, lens=[400, 90])
     pool, q, chunks = _cross_problem(case, 43)
     buf = _cross_buffers(case, pool, q)
     side = torch.cuda.Stream()
@@ -232,8 +248,8 @@ def test_cross_attention_from_a_graph_as_lengths_move(C):
         buf.cross_attn()
     whole = [(k, v) for k, v in zip(pool.k, pool.v)]
     for lens in ([400, 90], [17, 0], [0, 33], [399, 90]):
-        q = P.store(np.random.default_rng(sum(lens)).standard_normal(q.shape), "bf16")
-        buf.q.copy_(P.to_dev(q, "bf16", DEV))
+        q = P.store(np.random.default_rng(sum(lens)).standard_normal(q.shape), dtype)
+        buf.q.copy_(P.to_dev(q, dtype, DEV))
         buf.kv_lens.copy_(_ints(lens))
         buf.out.fill_(float("nan"))
         buf.lse.fill_(float("nan"))
