@@ -8,8 +8,8 @@
 // probabilities, the rows).  Lanes take neighbouring pieces of 16 bytes, wherever a row starts (an odd vocabulary's rows are aligned to an
 // element), and a wave a run of neighbouring entries: the sums of whole waves say which one the random number points into, and that one
 // alone adds up its entries in order.
-// Measured: one sequence, 4 tokens that were looked up, vocabulary 32003, 3.7 us and 3.3 (two launches of a chain of fetches each: 8.3 a call);
-// 64 sequences of up to 7, 131072 float32, 12.3 and 5.1 (67 MB in the first: 5.5 TB/s); vocabulary 1000 in one launch 3.3.
+// Measured: one sequence, 4 tokens that were looked up, vocabulary 32003, 3.9 us and 2.7 (two launches of a chain of fetches each: 8.3 a call);
+// 64 sequences of up to 7, 131072 float32, 12.4 and 5.2 (67 MB in the first: 5.4 TB/s); vocabulary 1000 in one launch 3.3.
 #include <type_traits>
 
 #include "common.hip.h"
