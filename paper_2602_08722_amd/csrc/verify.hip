@@ -132,6 +132,7 @@ struct Run {
 #pragma unroll
       for (int j = 0; j < J; ++j) q[j].load(r.q, v0 + j * N * kWave, V);
     }
+    __builtin_amdgcn_sched_barrier(0);   // (all on the way before any is used)
   }
   __device__ __forceinline__ void forget() {
 #pragma unroll
@@ -140,42 +141,62 @@ struct Run {
       q[j].forget();
     }
   }
-  __device__ __forceinline__ double all(int j, int e) const { return weight_of(p[j].at(e)); }
-  __device__ __forceinline__ double left(int j, int e) const {   // what remains of p: weight_of((double)p - (double)q)
-    const float from = p[j].at(e), off = has_q ? q[j].at(e) : x == j * N * kWave + e ? 1.f : 0.f;
+  // What entry e of piece j weighs: p, or (LEFT) what remains of it, weight_of((double)p - (double)q).
+  template <typename LEFT>
+  __device__ __forceinline__ double weight(LEFT, int j, int e) const {
+    const float from = p[j].at(e);
+    if constexpr (!LEFT::value) return weight_of(from);
+    const float off = has_q ? q[j].at(e) : x == j * N * kWave + e ? 1.f : 0.f;
     return from > off && from < INFINITY && off > -INFINITY ? (double)from - (double)off : 0.0;
+  }
+  // This lane's entries of piece j.
+  template <typename LEFT>
+  __device__ __forceinline__ double sum(LEFT left, int j) const {
+    double s = 0.0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) s += weight(left, j, e);
+    return s;
   }
 
   // The lowest entry of positive weight behind which `before` and the entries up to it are more than `point`; should there be none, the last
   // one of positive weight (sums of two orders may leave the point a rounding past the end); as a place in the row, -1: nothing weighs.
+  // s: sums of the pieces, which name the lane; its entries are added up in order.
   template <typename LEFT>
-  __device__ __forceinline__ int find(LEFT, double before, double point, int first) const {
+  __device__ __forceinline__ int find(LEFT left, const double (&s)[J], double before, double point, int first) const {
     const int lane = threadIdx.x & 63;
-    int last = -1;
+    double incl[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) incl[j] = wave_incl_scan(s[j]);
+    int piece = -1, of = 0;   // (the same for all lanes)
+    double start = 0.0;
+    bool found = false;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      double w[N], s = 0.0;
+      const unsigned long long hits = __builtin_amdgcn_ballot_w64(s[j] > 0.0 && before + incl[j] > point), some = __builtin_amdgcn_ballot_w64(s[j] > 0.0);
+      if (!found && some != 0) {
+        found = hits != 0;
+        piece = j;
+        of = found ? (int)__builtin_ctzll(hits) : 63 - (int)__builtin_clzll(some);
+        start = before + (incl[j] - s[j]);
+      }
+      before += last_lane(incl[j]);
+    }
+    if (piece < 0) return -1;
+    int hit = -1, last = 0;
 #pragma unroll
-      for (int e = 0; e < N; ++e) s += w[e] = LEFT::value ? left(j, e) : all(j, e);
-      const double incl = wave_incl_scan(s);
-      double run = before + (incl - s);
-      int hit = -1, mine = -1;
+    for (int j = 0; j < J; ++j) {
+      if (piece != j) continue;
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        run += w[e];
-        if (w[e] > 0.0) {
-          mine = e;
-          if (run > point && hit < 0) hit = e;
+        const double w = weight(left, j, e);
+        start += w;
+        if (w > 0.0) {
+          last = e;
+          if (start > point && hit < 0) hit = e;
         }
       }
-      const int at = first + j * N * kWave + lane * N;
-      const unsigned long long hits = __builtin_amdgcn_ballot_w64(hit >= 0);
-      if (hits != 0) return __builtin_amdgcn_readlane(at + hit, (int)__builtin_ctzll(hits));
-      const unsigned long long some = __builtin_amdgcn_ballot_w64(mine >= 0);
-      if (some != 0) last = __builtin_amdgcn_readlane(at + mine, 63 - (int)__builtin_clzll(some));
-      before += last_lane(incl);
     }
-    return last;
+    return first + piece * N * kWave + __builtin_amdgcn_readlane(lane * N + (hit >= 0 ? hit : last), of);
   }
 };
 
@@ -203,12 +224,10 @@ __global__ __launch_bounds__(kVfThreads) void verify_parts(VerifyArgs a, double2
   run.load(rows_of<T>(a, b, n, acc), part * kVfPart, a.V);
   double left = 0.0, all = 0.0;
 #pragma unroll
-  for (int j = 0; j < J; ++j)
-#pragma unroll
-    for (int e = 0; e < Piece<T>::N; ++e) {
-      left += run.left(j, e);
-      all += run.all(j, e);
-    }
+  for (int j = 0; j < J; ++j) {
+    left += run.sum(std::true_type{}, j);
+    all += run.sum(std::false_type{}, j);
+  }
   left = wave64_sum(left);
   all = wave64_sum(all);
   if ((threadIdx.x & 63) == 0) sums[(size_t)b * parts + part] = make_double2(left, all);
@@ -294,7 +313,13 @@ __global__ __launch_bounds__(kWave) void verify_pick(VerifyArgs a, const double2
     }
     Run<T, J> run;
     run.load(r, part * kVfPart, a.V);
-    y = use_left ? run.find(std::true_type{}, before, point, part * kVfPart) : run.find(std::false_type{}, before, point, part * kVfPart);
+    auto search = [&](auto of) __attribute__((always_inline)) {
+      double pieces[J];
+#pragma unroll
+      for (int j = 0; j < J; ++j) pieces[j] = run.sum(of, j);
+      return run.find(of, pieces, before, point, part * kVfPart);
+    };
+    y = use_left ? search(std::true_type{}) : search(std::false_type{});
   }
   put_tokens(a, b, acc, y, lane);
 }
@@ -311,26 +336,23 @@ __global__ __launch_bounds__(kVoThreads) void verify_one(VerifyArgs a) {
   const int n = drafted(a, b), acc = accepted<T>(a, b, n), first = w * kRun;
   Run<T, J> run;
   run.load(rows_of<T>(a, b, n, acc), first, a.V);
-  double total, before;
-  int chosen;   // the wave that the random number points into
+  double total, before, s[J];   // s: of this lane's pieces
+  int chosen;                   // the wave that the random number points into
   auto add_up = [&](auto left) __attribute__((always_inline)) {
-    double s = 0.0;
+    double mine = 0.0;
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-#pragma unroll
-      for (int e = 0; e < N; ++e) s += decltype(left)::value ? run.left(j, e) : run.all(j, e);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    s = wave64_sum(s);
+    for (int j = 0; j < J; ++j) mine += s[j] = run.sum(left, j);
+    run.forget();
+    mine = wave64_sum(mine);
     __syncthreads();
-    if (lane == 0) sums[w] = s;
+    if (lane == 0) sums[w] = mine;
     __syncthreads();
-    const double mine = lane < kVoWaves ? sums[lane] : 0.0, incl = wave_incl_scan(mine);
+    mine = lane < kVoWaves ? sums[lane] : 0.0;
+    const double incl = wave_incl_scan(mine);
     total = last_lane(incl);
     before = incl - mine;
     const unsigned long long hits = __builtin_amdgcn_ballot_w64(mine > 0.0 && before + mine > u * total), some = __builtin_amdgcn_ballot_w64(mine > 0.0);
     chosen = hits != 0 ? (int)__builtin_ctzll(hits) : some != 0 ? 63 - (int)__builtin_clzll(some) : 0;
-    run.forget();
   };
   add_up(std::true_type{});
   const bool use_left = total > 0.0 || acc >= n;
@@ -338,7 +360,8 @@ __global__ __launch_bounds__(kVoThreads) void verify_one(VerifyArgs a) {
   if (w != chosen) return;
   if (lane == 0) a.n_accepted[b] = acc;
   int y = -1;
-  if (total > 0.0) y = use_left ? run.find(std::true_type{}, lane_of(before, chosen), u * total, first) : run.find(std::false_type{}, lane_of(before, chosen), u * total, first);
+  before = lane_of(before, chosen);
+  if (total > 0.0) y = use_left ? run.find(std::true_type{}, s, before, u * total, first) : run.find(std::false_type{}, s, before, u * total, first);
   put_tokens(a, b, acc, y, lane);
 }
 
@@ -349,10 +372,10 @@ size_t verify_ws_bytes(int batch, int vocab) { return (size_t)batch * vf_parts(v
 hipError_t launch_verify(const VerifyArgs& a, int dtype, void* ws, hipStream_t st) {
   auto launch = [&](auto one) {
     using T = decltype(one);
-    // One launch up to 24576 float32 entries, 16384 bfloat16 ones (whose pieces have twice as many conversions to 64 bits in them, which are most of
-    // a piece's time: 0.7 us, 1.9).  Us of one and of two launches, 1 to 128 sequences: float32, 4096 entries 3.2 - 4.3 / 6.8 - 8.6, 8000 4.0 - 4.8 / 6.2 -
-    // 8.3, 16000 4.4 - 6.3 / 6.0 - 8.7, 24000 5.5 - 8.3 / 6.6 - 10.3, 32003 (8 pieces) 6.6 - 10.1 / 6.3 - 12.0; bfloat16, 8000 4.2 - 5.0 / 6.8 - 8.5, 16000
-    // 4.9 - 6.5 / 7.0 - 8.5, 24000 (4 pieces) 6.9 - 10.4 / 6.5 - 9.4.
+    // One launch up to 24576 float32 entries, 16384 bfloat16 ones, and of 64 sequences or more up to 32768.  Us of one and of two launches, 1 to 128
+    // sequences: float32, 4096 entries 3.2 - 4.3 / 6.8 - 8.6, 8000 3.9 - 4.7 / 6.2 - 8.3, 16000 4.9 - 5.9 / 6.0 - 8.7, 24000 5.8 - 7.4 / 6.6 - 10.3, 32003
+    // 6.9 - 8.2 / 6.5 - 8.0 (8 sequences or fewer), 7.7 - 9.5 / 8.1 - 12.0 (64 and 128); bfloat16, 8000 4.2 - 5.0 / 6.8 - 8.5, 16000 4.9 - 6.1 / 7.0 -
+    // 8.5, 32003 6.9 - 9.3 / 6.8 - 8.2, 8.0 - 9.6 / 8.3 - 10.4.
     constexpr int kStep = Piece<T>::N * kWave * kVoWaves;   // entries of a block whose waves have one piece
     auto one_launch = [&](auto pieces) {
       hipLaunchKernelGGL((verify_one<T, decltype(pieces)::value>), dim3(a.b), dim3(kVoThreads), 0, st, a);
@@ -364,6 +387,9 @@ hipError_t launch_verify(const VerifyArgs& a, int dtype, void* ws, hipStream_t s
     if constexpr (sizeof(T) == 4) {
       if (a.V <= 4 * kStep) return one_launch(integral_constant<int, 4>{});
       if (a.V <= 6 * kStep) return one_launch(integral_constant<int, 6>{});
+      if (a.V <= 8 * kStep && a.b >= 64) return one_launch(integral_constant<int, 8>{});
+    } else {
+      if (a.V <= 4 * kStep && a.b >= 64) return one_launch(integral_constant<int, 4>{});
     }
     const int parts = vf_parts(a.V), waves = kVfThreads / kWave;
     hipLaunchKernelGGL((verify_parts<T>), dim3((parts + waves - 1) / waves, a.b), dim3(kVfThreads), 0, st, a, static_cast<double2*>(ws), parts);

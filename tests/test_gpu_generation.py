@@ -334,6 +334,16 @@ def test_verification_of_vocabularies_around_a_blocks_pieces(dtype, V, lookup):
         _check_verified(_verified(p, q, tokens, uniform, dtype, lens), p, q, tokens, uniform, lens)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [32768, 32769, 25000])
+def test_verification_of_many_sequences(dtype, V):
+    rng = np.random.default_rng(V + 1)
+    lens = [i % 3 for i in range(64)]
+    p, q, tokens, uniform = _verify_problem(rng, 64, 2, V, dtype, False)
+    q[5], uniform[5] = p[5, :2], 1.0   # nothing is left behind a refusal
+    _check_verified(_verified(p, q, tokens, uniform, dtype, lens), p, q, tokens, uniform, lens)
+
+
 @pytest.mark.parametrize("V", [5, 33000])
 def test_verification_of_what_distributions_should_not_hold(V):
     """NaN, infinities, negative entries, rows without any weight, tokens outside the vocabulary, random numbers outside [0, 1)."""
