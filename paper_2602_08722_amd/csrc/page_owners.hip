@@ -9,6 +9,8 @@
 // Bound by the chain: lengths, table, counts' atomics, counts, table.  Measured: a step of 16 sequences over 8192 pages 3 - 4 us, of 256 over 262144
 // 2.7 + 2.5 + 4.3; forks of 16 sequences 6.2, of 256 with 130816 entries 3.4 + 5.3.  (Counts fetched ahead of the scans, whether pages are wanted or not:
 // 0.6 us more for a step that wants none, which most are, otherwise the same.)
+#include <type_traits>
+
 #include "common.hip.h"
 #include "kernels.h"
 
@@ -187,10 +189,10 @@ __global__ __launch_bounds__(kOwThreads) void owners_take(Owners o, ForkArgs f, 
   }
 }
 
-// Free pages counted and handed out by one block.  A thread has the sequence of its number: `need` entries that want a page behind the
-// `start_of` ones in use.
+// Free pages counted and handed out by one block, RUNS times 16 of every thread at once.  A thread has the sequence of its number: `need` entries
+// that want a page behind the `start_of` ones in use.
 constexpr int kOsThreads = 1024;
-template <bool FORK>
+template <bool FORK, int RUNS>
 __device__ __forceinline__ void hand_out(const Owners& o, const ForkArgs& f, int start_of, int need, int32_t* lacking) {
   __shared__ uint32_t scan[kOsThreads / kWave + 1];
   __shared__ int32_t prefix[kOsThreads + 1], start[kOsThreads];
@@ -202,11 +204,20 @@ __device__ __forceinline__ void hand_out(const Owners& o, const ForkArgs& f, int
   if (tid == kOsThreads - 1) prefix[kOsThreads] = (int32_t)wanted;
   __syncthreads();
   uint32_t before = 0;
-  for (int page0 = tid * kOwRun; before < wanted && page0 - tid * kOwRun < o.n_pages; page0 += kOsThreads * kOwRun) {   // block-uniform
-    const uint32_t is = free_pages(o, page0);
-    const uint32_t rank = before + block_excl_scan<kOsThreads>((uint32_t)__popc(is), scan, &total);
-    give_pages(o, page0, is, rank, wanted, prefix, start);
-    before += total;
+  for (int of_block = 0; before < wanted && of_block < o.n_pages; of_block += kOsThreads * kOwRun * RUNS) {   // block-uniform
+    constexpr int kStep = kOsThreads * kOwRun;   // pages of a run of all threads (16 bits hold their number: two runs a scan)
+    uint32_t is[RUNS];
+#pragma unroll
+    for (int i = 0; i < RUNS; ++i) is[i] = free_pages(o, of_block + i * kStep + tid * kOwRun);
+#pragma unroll
+    for (int i = 0; i < RUNS; i += 2) {
+      const uint32_t second = i + 1 < RUNS ? (uint32_t)__popc(is[i + 1]) : 0u;
+      const uint32_t excl = block_excl_scan<kOsThreads>((uint32_t)__popc(is[i]) | second << 16, scan, &total);
+      give_pages(o, of_block + i * kStep + tid * kOwRun, is[i], before + (excl & 0xFFFFu), wanted, prefix, start);
+      before += total & 0xFFFFu;
+      if (i + 1 < RUNS) give_pages(o, of_block + (i + 1) * kStep + tid * kOwRun, is[i + 1], before + (excl >> 16), wanted, prefix, start);
+      before += total >> 16;
+    }
   }
   if (tid < o.b) {
     const int got = min(max((int)(before - mine), 0), need);
@@ -218,7 +229,7 @@ __device__ __forceinline__ void hand_out(const Owners& o, const ForkArgs& f, int
 
 // All of it in one block.  Counts are fetched when the atomics of the first step have reached them, and not from the first-level cache, where a
 // line may be that has table entries of the first step and counts in it.
-template <bool FORK>
+template <bool FORK, int RUNS>
 __global__ __launch_bounds__(kOsThreads) void owners_one(Owners from, Owners o, ForkArgs f, const int32_t* __restrict__ lens,
                                                          int32_t* __restrict__ lacking) {
   __shared__ int32_t starts[kOsThreads], needs[kOsThreads];
@@ -235,35 +246,39 @@ __global__ __launch_bounds__(kOsThreads) void owners_one(Owners from, Owners o, 
   wait_vmcnt<0>();
   __syncthreads();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-  hand_out<FORK>(o, f, tid < o.b ? starts[tid] : 0, tid < o.b ? needs[tid] : 0, lacking);
+  hand_out<FORK, RUNS>(o, f, tid < o.b ? starts[tid] : 0, tid < o.b ? needs[tid] : 0, lacking);
 }
 
 // The second and third step.
-template <bool FORK>
+template <bool FORK, int RUNS>
 __global__ __launch_bounds__(kOsThreads) void owners_rest(Owners o, ForkArgs f, OwWs ws, int32_t* __restrict__ lacking) {
   const int b = min((int)threadIdx.x, o.b - 1);
   const int start = ws.start[b], need = ws.need[b];
-  hand_out<FORK>(o, f, start, (int)threadIdx.x < o.b ? need : 0, lacking);
+  hand_out<FORK, RUNS>(o, f, start, (int)threadIdx.x < o.b ? need : 0, lacking);
 }
 
-// Which launches: one block for all, its last two steps, or many blocks throughout.  Us a call over pools below and above 32768 pages; a resize by 40 tokens, one
-// that gives back or takes every page, a fork: 16 sequences of 260 pages 3.3 / 6.8, 5.5 / 8.5, 8.8 / 11.0; of 1004 pages 3.4 / 6.9, 12.8 / 9.1,
-// 10.4 / 11.8 (two steps in one block; all three 14.7); 64 of 254 4.7 / 7.6, 13.7 / 9.0, 9.4 / 11.0 (all three 16.1); 256 of 67 6.5 / 7.5, 14.5 /
-// 9.2, 11.4 / 11.2.  The step that a generated token takes is what counts, so a resize goes by it; the block's time grows by 0.7 us for
-// every 16384 pages that are looked through, that of the many not.
+// Which launches: one block for all, its last two steps, or many blocks throughout.  Us a call, in one block (the steps that the rule below gives it) and in
+// many; a resize by 40 tokens, one that gives back or takes every page, a fork: 16 sequences of 260 pages 3.3 / 6.8, 5.5 / 8.5, 8.8 / 11.0; of
+// 1004 pages 3.4 / 6.9, 12.8 / 9.1, 10.4 / 11.8 (two steps in one block; all three 14.7); 64 of 254 4.7 / 7.6, 13.7 / 9.0, 9.4 / 11.0 (all three 16.1);
+// 256 of 67 6.5 / 7.5, 14.5 / 9.2, 11.4 / 11.2.  The step that a generated token takes is what counts, so a resize goes by it.  The block's time
+// grows by 0.7 us for every 16384 pages that are looked through (4.4 for 65536), that of the many not: a step over 65536 pages 5.4 - 5.9 / 5.8 - 6.6 us
+// (16 sequences or fewer) and 7.0 / 7.3 (256), over 131072 5.5 - 8.5 / 6.6 by where the free ones are, and where calls are enqueued one by one, at 3 us
+// a launch, 5.5 - 8.7 / 11.0; forks of 16 over 65536 11.8 / 10.4.
+constexpr int kOwSmall = 32768;
 struct OwPlan {
   bool one, rest;
 };
 static OwPlan ow_plan(const Owners& o, bool fork) {
-  const bool small_pool = o.n_pages <= 32768;
+  const bool small_pool = o.n_pages <= (fork ? kOwSmall : 4 * kOwSmall);
   const long long entries = (long long)o.b * o.max_pages;
   return {small_pool && (fork ? o.b <= 64 && entries <= 8192 : o.b <= 128 && entries <= 16384), small_pool && o.b <= kOsThreads};
 }
 
 static hipError_t launch_take(const Owners& o, const ForkArgs& f, const OwWs& w, int32_t* lacking, bool fork, hipStream_t st) {
   if (ow_plan(o, fork).rest) {
-    if (fork) hipLaunchKernelGGL((owners_rest<true>), dim3(1), dim3(kOsThreads), 0, st, o, f, w, lacking);
-    else hipLaunchKernelGGL((owners_rest<false>), dim3(1), dim3(kOsThreads), 0, st, o, f, w, lacking);
+    if (fork) hipLaunchKernelGGL((owners_rest<true, 1>), dim3(1), dim3(kOsThreads), 0, st, o, f, w, lacking);
+    else if (o.n_pages <= kOwSmall) hipLaunchKernelGGL((owners_rest<false, 1>), dim3(1), dim3(kOsThreads), 0, st, o, f, w, lacking);
+    else hipLaunchKernelGGL((owners_rest<false, 4>), dim3(1), dim3(kOsThreads), 0, st, o, f, w, lacking);
     return hipGetLastError();
   }
   const int tiles = ow_tiles(o.n_pages);
@@ -274,7 +289,8 @@ static hipError_t launch_take(const Owners& o, const ForkArgs& f, const OwWs& w,
 
 hipError_t launch_pages_resize(const Owners& o, const int32_t* lens, int32_t* lacking, void* ws, hipStream_t st) {
   if (ow_plan(o, false).one) {
-    hipLaunchKernelGGL((owners_one<false>), dim3(1), dim3(kOsThreads), 0, st, o, o, ForkArgs{}, lens, lacking);
+    if (o.n_pages <= kOwSmall) hipLaunchKernelGGL((owners_one<false, 1>), dim3(1), dim3(kOsThreads), 0, st, o, o, ForkArgs{}, lens, lacking);
+    else hipLaunchKernelGGL((owners_one<false, 4>), dim3(1), dim3(kOsThreads), 0, st, o, o, ForkArgs{}, lens, lacking);
     return hipGetLastError();
   }
   const OwWs w = ow_ws(o, ws);
@@ -284,7 +300,7 @@ hipError_t launch_pages_resize(const Owners& o, const int32_t* lens, int32_t* la
 
 hipError_t launch_pages_fork(const Owners& from, const Owners& o, const ForkArgs& f, int32_t* lacking, void* ws, hipStream_t st) {
   if (ow_plan(o, true).one) {
-    hipLaunchKernelGGL((owners_one<true>), dim3(1), dim3(kOsThreads), 0, st, from, o, f, nullptr, lacking);
+    hipLaunchKernelGGL((owners_one<true, 1>), dim3(1), dim3(kOsThreads), 0, st, from, o, f, nullptr, lacking);
     return hipGetLastError();
   }
   const OwWs w = ow_ws(o, ws);

@@ -407,7 +407,8 @@ def _same(seqs, book, lacking, what):
 
 
 @pytest.mark.parametrize("n_pages,page_len,batch,max_pages", [(1, 1, 1, 1), (40, 16, 5, 9), (300, 64, 70, 6), (5000, 16, 33, 150), (9000, 1, 300, 60),
-                                                              (70000, 32, 9, 9000), (4096, 256, 1, 4096), (20000, 16, 1500, 12)])
+                                                              (70000, 32, 9, 9000), (4096, 256, 1, 4096), (20000, 16, 1500, 12),
+                                                              (32769, 16, 40, 300), (131072, 8, 150, 200), (131073, 16, 3, 50)])
 def test_pages_that_come_and_go(n_pages, page_len, batch, max_pages):
     """Calls of every kind in a row, more than there are pages for among them; the table's entries hold anything beforehand."""
     pk, rng = _pk(), np.random.default_rng(n_pages)
@@ -476,6 +477,29 @@ def test_children_with_less_room_than_their_parents(batch, kids, n_pages):
     child.resize(torch.zeros(kids, dtype=torch.int32, device=DEV))
     theirs.resize([0] * kids)
     _same(seqs, book, 0, "")
+
+
+@pytest.mark.parametrize("n_pages,batch,max_pages", [(20000, 30, 100), (32769, 30, 100), (65536, 300, 20), (131072, 100, 40), (140000, 30, 100)])
+@pytest.mark.parametrize("busy", [0.5, 0.99])
+def test_free_pages_among_others_pages(n_pages, batch, max_pages, busy):
+    """Pages that other tables hold, here and there, at the pool's start and nearly everywhere; some calls want more than there are."""
+    rng = np.random.default_rng(n_pages)
+    seqs = _pk().PagedSequences.allocate(n_pages, 16, batch, max_pages)
+    ref = (rng.random(n_pages) < busy).astype(np.int64) * rng.integers(1, 4, n_pages)
+    ref[:n_pages // 3] = 1
+    seqs.ref.copy_(_ints(ref.tolist()))
+    book = G.Book(ref.tolist(), 16, batch, max_pages)
+    for step in range(4):
+        lens = rng.integers(0, 16 * max_pages + 40, batch)
+        lacking = book.resize(lens.tolist())
+        seqs.resize(_ints(lens.tolist()))
+        _same(seqs, book, lacking, step)
+    kids, kid_book = seqs.another(batch), G.Book(book.ref, 16, batch, max_pages)
+    parents = rng.integers(-1, batch, batch)
+    first, got, lacking = kid_book.fork(book, parents.tolist(), lens.tolist())
+    kids.fork(seqs, _ints(parents.tolist()), _ints(lens.tolist()))
+    _same(kids, kid_book, lacking, "fork")
+    assert kids.first.tolist() == first and kids.lens.tolist() == got
 
 
 def test_owners_that_hold_nonsense_stay_inside_the_arrays():
