@@ -232,6 +232,21 @@ def test_calls_on_two_streams_at_once():
         assert np.array_equal(seq.page_table.cpu().numpy(), book.table()) and seq.ref.tolist() == book.ref
 
 
+@pytest.mark.parametrize("case", [
+    dict(dtype=dtype, fp8=fp8, n_q=n_q, n_kv=8, d=128, page_len=64, C=C, lens=[T])
+    for dtype, fp8, n_q, C, T in (("bf16", False, 8, 1, 300), ("bf16", True, 16, 1, 50), ("bf16", False, 32, 1, 400), ("bf16", True, 32, 1, 5000),
+                                  ("bf16", False, 32, 70, 700), ("bf16", True, 32, 300, 300), ("f32", False, 8, 1, 700), ("f32", True, 32, 1, 300),
+                                  ("f32", False, 32, 40, 300), ("f32", True, 8, 3, 5))
+], ids=_ids)
+def test_cross_attention_beyond_four_gib_of_a_pool(case):
+    row = 1 if case["fp8"] else 2 if case["dtype"] == "bf16" else 4
+    pool, q, chunks = _cross_problem(case, 47, n_pages=3 * (1 << 31) // (8 * 64 * 128 * row))   # (pages from all over it)
+    buf = _cross_buffers(case, pool, q)
+    buf.cross_attn()
+    torch.cuda.synchronize()
+    _check_cross(case, buf, pool, q, chunks)
+
+
 @pytest.mark.parametrize("C,dtype", [(1, "bf16"), (70, "bf16"), (1, "f32"), (30, "f32")])
 def test_cross_attention_from_a_graph_as_lengths_move(C, dtype):
     """Recorded once, replayed with other queries and lengths, a length of none among them."""
@@ -342,6 +357,22 @@ def test_verification_of_many_sequences(dtype, V):
     p, q, tokens, uniform = _verify_problem(rng, 64, 2, V, dtype, False)
     q[5], uniform[5] = p[5, :2], 1.0   # nothing is left behind a refusal
     _check_verified(_verified(p, q, tokens, uniform, dtype, lens), p, q, tokens, uniform, lens)
+
+
+@pytest.mark.parametrize("V", [1000, 40000])
+def test_verification_of_rows_far_apart(V):
+    """Strides past 32 bits: sequences more than 2^31 elements from each other, at an odd element."""
+    rng = np.random.default_rng(9)
+    p, q, tokens, uniform = _verify_problem(rng, 2, 2, V, "bf16", False)
+    far = (1 << 31) + 12345
+    base = torch.zeros(far + 6 * V + 7, dtype=torch.bfloat16, device=DEV)
+    target, draft = (base.as_strided(x.shape, (far, V + 1, 1), at) for x, at in ((p, 1), (q, 3 * V + 5)))
+    target.copy_(P.to_dev(p, "bf16", DEV))
+    draft.copy_(P.to_dev(q, "bf16", DEV))
+    buf = _pk().DraftBuffers(target, _ints(tokens.tolist()), torch.from_numpy(uniform).to(DEV), draft=draft)
+    got = buf.verify()
+    torch.cuda.synchronize()
+    _check_verified([x.cpu().numpy() for x in got], p, q, tokens, uniform)
 
 
 @pytest.mark.parametrize("V", [5, 33000])
