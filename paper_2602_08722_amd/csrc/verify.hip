@@ -1,6 +1,6 @@
 // Verification of drafted tokens against the target's probabilities (quoka_verify_draft).
 //
-// Token i of a sequence is accepted while u_i q_i(x_i) < p_i(x_i), a positive number; the product of two float32 numbers is exact in 64 bits.  The token after
+// Token i of a sequence is accepted while u_i q_i(x_i) < p_i(x_i), a positive number, and q_i(x_i) is finite; the product of two float32 numbers is exact in 64 bits.  The token after
 // the a accepted ones is the lowest v of positive weight w_v with w_0 + ... + w_v > u_n (w_0 + w_1 + ...), w = max(p_a - q_a, 0) behind a refusal
 // (p_a, should nothing be left of it), else p_a.  Sums are in 64 bits: a token's part of that line is as narrow as its probability.
 //
@@ -60,7 +60,7 @@ __device__ __forceinline__ int accepted(const VerifyArgs& a, int b, int n) {
       if (x >= 0 && x < a.V) {
         const double p = Elem<T>::load1(static_cast<const T*>(a.target) + b * a.ts[0] + i * a.ts[1] + x);
         const double q = a.draft == nullptr ? 1.0 : Elem<T>::load1(static_cast<const T*>(a.draft) + b * a.ds[0] + i * a.ds[1] + x);
-        good = u * q < p && weight_of(p) > 0.0;   // (a NaN compares false)
+        good = u * q < p && weight_of(p) > 0.0 && fabs(q) < (double)INFINITY;   // (a NaN compares false)
       }
     }
     const unsigned long long stops = __builtin_amdgcn_ballot_w64(!good);

@@ -34,7 +34,8 @@ def verify(p, q, tokens, uniform, n):
     a = 0
     while a < n:
         x = int(tokens[a])
-        if not 0 <= x < V or not (float(u[a]) * (1.0 if q is None else float(q[a][x])) < p[a][x] and 0 < p[a][x] < np.inf):
+        drawn = 1.0 if q is None or not 0 <= x < V else float(q[a][x])
+        if not 0 <= x < V or not (float(u[a]) * drawn < p[a][x] and 0 < p[a][x] < np.inf and np.isfinite(drawn)):
             break
         out[a] = x
         a += 1

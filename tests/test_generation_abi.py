@@ -279,6 +279,13 @@ def test_the_plain_verification_draws_from_the_target():
     assert np.allclose(counts, p, atol=1e-12)
 
 
+@pytest.mark.parametrize("value", [-np.inf, np.inf, np.nan])
+@pytest.mark.parametrize("u", [0.5, 0.0, -0.5, np.inf, -np.inf, np.nan])
+def test_the_plain_verification_refuses_tokens_whose_draft_probability_is_no_number(value, u):
+    a, out = G.verify([[0.75, 0.25], [0.5, 0.5]], [[value, 0.0]], [0], [u, 0.5], 1)
+    assert a == 0 and out.tolist() == [1, -1]
+
+
 def test_the_plain_book_keeps_its_counts():
     ref = [0] * 10
     a = G.Book(ref, 4, 2, 5)

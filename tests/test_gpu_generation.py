@@ -418,6 +418,25 @@ def test_borders_of_a_verification(V):
         assert got[0][0] == a and got[1][0, a] == (0 if a == 1 else 1)   # (refused: nothing is left at 0)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [8, 40000])
+def test_tokens_drafted_with_a_probability_that_is_no_number_are_refused(V, dtype):
+    """q is -inf, inf or NaN at the drafted token, whatever the random number: not accepted, and the token weighs nothing behind it.  (All of p
+    lies on tokens 1, the drafted one, and 3: what is drawn is 3.)  A second token that could be accepted stays unread."""
+    p, q = np.zeros((1, 3, V), np.float32), np.zeros((1, 2, V), np.float32)
+    p[0, :, 1], p[0, :, 3] = 0.75, 0.25
+    q[0, :, 1] = 0.5
+    tokens = np.array([[1, 1]], dtype=np.int64)
+    for value in (-np.inf, np.inf, np.nan):
+        for u in (0.5, 1.0, 2.0 ** -40, 0.0, -0.5, np.inf, -np.inf, np.nan):
+            q[0, 0, 1] = value
+            n_accepted, out = _verified(p, q, tokens, np.array([[u, 0.25, 0.5]], np.float32), dtype)
+            assert n_accepted.tolist() == [0] and out.tolist() == [[3, -1, -1]], (value, u)
+    q[0, 0, 1] = 0.5   # (and with a number in its place: u q < p)
+    n_accepted, out = _verified(p, q, tokens, np.array([[0.5, 0.25, 0.5]], np.float32), dtype)
+    assert n_accepted.tolist() == [2] and out.tolist() == [[1, 1, 1]]
+
+
 def test_verification_takes_distributions_that_sequences_share():
     """Strides of zero: one target for all sequences of the batch."""
     rng = np.random.default_rng(8)
