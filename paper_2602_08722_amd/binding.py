@@ -554,8 +554,9 @@ class PagedCache:
 
     def compact(self, source, k_idx, k_cnt):
         """The rows that k_idx [b, n_KV, B_max] lists, k_cnt [b, n_KV] of them, from the pages of `source`, another PagedCache of the same
-        batch, one behind the other into the pages of this one."""
-        _, n_kv, d, _ = self._rows
+        batch, one behind the other into the pages of this one.  Entries are cut to the positions of the source's table, and to as many as a
+        cache that is attended may have (2^24 - 1; float32 rows of 128: 2^23 - 1)."""
+        dtype, n_kv, d, _ = self._rows
         lists, b, dev = k_idx.shape, self._batch, self._device
         if (k_idx.dtype != torch.int32 or k_cnt.dtype != torch.int32 or len(lists) != 3 or lists[0] != b or lists[1] != n_kv or
                 k_cnt.shape != (b, n_kv) or not k_idx.is_contiguous() or not k_cnt.is_contiguous()):
@@ -564,9 +565,9 @@ class PagedCache:
             raise ValueError("key lists are on the pages' device")
         if source._batch != b:
             raise ValueError("caches that rows move between are of one batch")
-        # (the positions that the source's table has, as far as there are such caches)
+        # (the positions that the source's table has, as far as any call may have them: quoka_shape's limits, in the dtype that _moves gives it)
         theirs = source.pages
-        room = min(theirs.max_pages * theirs.page_len, (1 << 24) - 1, (1 << 32) // (4 * d) - 1)
+        room = min(theirs.max_pages * theirs.page_len, (1 << 24) - 1, (1 << 32) // ((4 if dtype == torch.float32 else 2) * d) - 1)
         quoka_cache_compact(self._moves(source, room, lists[2]), theirs, self.pages, k_idx, k_cnt)
 
     def copy(self, source, parents=None, first=None, lens=None, max_rows=None):

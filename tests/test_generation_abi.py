@@ -224,6 +224,24 @@ def test_moves_refuse_caches_that_do_not_fit():
         pk.PagedBuffers(cache, [1, 2], 60).cross_attn()
 
 
+@pytest.mark.parametrize("dtype,d,most", [(torch.float8_e4m3fn, 128, 2 ** 24 - 1), (torch.bfloat16, 128, 2 ** 24 - 1), (torch.bfloat16, 64, 2 ** 24 - 1),
+                                          (torch.float32, 64, 2 ** 24 - 1), (torch.float32, 128, 2 ** 23 - 1)])
+def test_lists_reach_every_position_that_a_call_may_have(dtype, d, most, monkeypatch):
+    """Of a table with room for more: as many as attention and selection take, which refuse one more."""
+    table = torch.zeros(1, 1 << 10, dtype=torch.int32)
+    there, pool = torch.zeros(1, 1, 16, d, dtype=dtype), torch.empty_strided((1, 1, 1 << 15, d), (0, 0, d, 1), dtype=dtype)
+    scales = [torch.zeros(1, 1, n, dtype=torch.uint8) for n in (1 << 15, 16)] if dtype == torch.float8_e4m3fn else [None, None]
+    cache, to = pk.PagedCache(pool, pool, table, *[scales[0]] * 2), pk.PagedCache(there, there, table[:, :4].contiguous(), *[scales[1]] * 2)
+    shapes = []
+    monkeypatch.setattr(pk.binding, "quoka_cache_compact", lambda shape, *a: shapes.append(shape))
+    to.compact(cache, torch.zeros(1, 1, 5, dtype=torch.int32), torch.zeros(1, 1, dtype=torch.int32))
+    s, n = shapes[0], ctypes.c_size_t(0)
+    assert s.max_kv_len == most
+    for t, code in ((most, 0), (most + 1, 2)):
+        s.max_kv_len = t
+        assert pk.load_library().quoka_paged_workspace_bytes(ctypes.byref(s), ctypes.byref(n)) == code
+
+
 def test_drafts_refuse_tensors_that_do_not_fit():
     p, q = torch.zeros(2, 4, 100), torch.zeros(2, 3, 100)
     x, u = torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 4)

@@ -679,6 +679,31 @@ def test_listed_rows_move_between_pools_and_page_lengths():
     assert bool((there.k_pages.view(torch.uint8)[[1, 3]] == 0x7F).all())
 
 
+@pytest.mark.parametrize("dtype", [torch.float8_e4m3fn, torch.bfloat16])
+def test_listed_rows_of_the_longest_caches_move(dtype):
+    """Positions up to the last that a cache of 2^24 - 1 tokens has, through a table that repeats a few pages; rows of different bits."""
+    pk, page_len, d = _pk(), 65536, 128
+    table = torch.zeros(1, 256, dtype=torch.int32, device=DEV)
+    table[0, 128], table[0, 255] = 1, 2
+    cache = pk.PagedCache.allocate(3, page_len, 1, d, table, dtype=dtype)
+    for i, x in enumerate((cache.k_pages, cache.v_pages)):
+        bits = x.view(torch.uint8) if x.element_size() == 1 else x.view(torch.int16)
+        bits.copy_(torch.randint(0, 100, bits.shape, device=DEV, generator=torch.Generator(DEV).manual_seed(i)).to(bits.dtype))
+    for x in (cache.k_scale, cache.v_scale):
+        if x is not None:
+            x.copy_(torch.randint(100, 150, x.shape, device=DEV).to(torch.uint8))
+    to = pk.PagedCache.allocate(1, 16, 1, d, torch.zeros(1, 1, dtype=torch.int32, device=DEV), dtype=dtype)
+    at = [2 ** 23 - 3, 2 ** 23 - 2, 2 ** 23 - 1, 2 ** 23, 2 ** 23 + 77, 2 ** 24 - 65537, 2 ** 24 - 65536, 2 ** 24 - 2]
+    to.compact(cache, _ints([[at]]), _ints([[len(at)]]))
+    pages = table[0].tolist()
+    for src, dst in ((cache.k_pages, to.k_pages), (cache.v_pages, to.v_pages), (cache.k_scale, to.k_scale), (cache.v_scale, to.v_scale)):
+        if src is None:
+            continue
+        for j, t in enumerate(at):
+            x, y = (z.reshape(-1).view(torch.uint8) for z in (dst[0, 0, j].clone(), src[pages[t // page_len], 0, t % page_len].clone()))
+            assert torch.equal(x, y), (j, t)
+
+
 @pytest.mark.parametrize("layout", ["heads", "tokens"])
 @pytest.mark.parametrize("case", MOVE_CASES, ids=_ids)
 def test_copied_rows_keep_their_positions(case, layout):
