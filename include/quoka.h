@@ -283,7 +283,8 @@ quoka_status quoka_paged_attn(const quoka_shape* shape, const quoka_pages* pages
  * several sequences share -- written by quoka_cache_write like any others.  For q-head h (KV head kv) and chunk position i < chunk_lens[b]:
  *   O[b,h,i] = sum_t softmax_t(<Q[b,h,i], K_t> / sqrt(d)) V_t over the positions t < kv_lens[b], without a mask.
  * Rows i >= chunk_lens[b], and all rows of a sequence of kv_lens[b] == 0, are written as zeros, their lse as -infinity.
- * Arguments, workspace (quoka_paged_workspace_bytes), limits and arithmetic as in quoka_paged_attn. */
+ * Arguments, workspace (quoka_paged_workspace_bytes is enough for either call; in float32 each takes what it needs itself), limits and
+ * arithmetic as in quoka_paged_attn. */
 quoka_status quoka_cross_attn(const quoka_shape* shape, const quoka_pages* pages, const void* q, const int32_t* kv_lens,
                               const int32_t* chunk_lens, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -576,8 +576,8 @@ inline long long f32_units(const Dims& dm, bool sparse, bool own = true) {   // 
   const long long units = ((long long)attended_cap(dm, sparse) + 31) / 32 + (own ? (dm.C + 31) / 32 : 0);
   return units > 0 ? units : 1;   // (of states without length nothing is split)
 }
-inline int f32_most_splits(const Dims& dm, bool sparse, bool own = true) {
-  const long long n = (f32_units(dm, sparse, own) + kFaWaves - 1) / kFaWaves;
+inline int f32_most_splits(const Dims& dm, bool sparse) {
+  const long long n = (f32_units(dm, sparse) + kFaWaves - 1) / kFaWaves;
   return (int)(n > kFaMaxSplits ? kFaMaxSplits : n);
 }
 inline int f32_splits(const Dims& dm, bool sparse) {
@@ -608,10 +608,6 @@ inline int f32_state_units(const Dims& dm, float* us_of = nullptr) {
   return (int)best * kFaWaves;
 }
 inline int f32_state_shares(const Dims& dm, int per) { return (int)((f32_units(dm, false, false) + per - 1) / per); }
-inline size_t cross_f32_ws_floats(const Dims& dm) {
-  const long long most = f32_blocks(dm) * f32_most_splits(dm, false, false);
-  return (size_t)(most < kMostStateParts ? most : kMostStateParts) * 32 * (dm.d + 2);
-}
 
 template <int D, int SRC = kContiguous>
 static hipError_t launch_f32_units(const Dims& dm, const attn_args<SRC>& a, float* part, hipStream_t st) {

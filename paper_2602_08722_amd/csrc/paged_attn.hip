@@ -125,8 +125,15 @@ static hipError_t launch_paged_f32(const Dims& dm, const PagedArgs& a, float* pa
   return launch_f32_units<D, SRC>(dm, aa, part, st);
 }
 
-size_t paged_attn_ws_floats(const Dims& dm, int dtype) {
-  if (dtype != QUOKA_BF16) return attn_f32_ws_floats(dm) > cross_f32_ws_floats(dm) ? attn_f32_ws_floats(dm) : cross_f32_ws_floats(dm);
+// Partials of cross attention: of the shares that the launch has (kMostStateParts at most).
+static size_t cross_f32_ws_floats(const Dims& dm) {
+  if (state_form(dm) != kStateUnits) return 0;
+  const int shares = f32_state_shares(dm, f32_state_units(dm));
+  return shares > 1 ? (size_t)(f32_blocks(dm) * shares) * 32 * (dm.d + 2) : 0;
+}
+
+size_t paged_attn_ws_floats(const Dims& dm, int dtype, bool own) {
+  if (dtype != QUOKA_BF16) return own ? attn_f32_ws_floats(dm) : cross_f32_ws_floats(dm);
   return attn_decode_applies(dm) ? paged_decode_ws_floats(dm) : paged_attn_bf16_ws_floats(dm);
 }
 

@@ -97,6 +97,29 @@ def test_bad_pointers_and_arguments_are_refused():
     assert lib.quoka_cache_compact(ctypes.byref(_shape(pk, max_budget=0)), a, b, None, AT, None) == 0
 
 
+# quoka_paged_attn in float32: partials of 32 rows of d outputs and two sums each, one for every row block and eight units of 32 keys, at most 512
+def _attn_bytes(s):
+    blocks = s.batch * s.n_kv_heads * -(-s.chunk_len * (s.n_q_heads // s.n_kv_heads) // 32)
+    shares = min(-(-(-(-s.max_kv_len // 32) + -(-s.chunk_len // 32)) // 8), 64)
+    return -(-min(blocks * shares, 512) * 32 * (s.head_dim + 2) * 4 // 256) * 256
+
+
+@pytest.mark.parametrize("kw,parts", [
+    (dict(), 0), (dict(batch=8, chunk_len=1, max_kv_len=40000, head_dim=64), 0), (dict(n_q_heads=32, n_kv_heads=8, chunk_len=512, max_kv_len=8192), 0),
+    (dict(chunk_len=540, max_kv_len=5000), 680), (dict(batch=2, chunk_len=270, max_kv_len=5000, head_dim=64), 680),
+])
+def test_a_float32_workspace_is_as_large_as_its_call_wants(kw, parts):
+    """parts: of cross attention, where they are more than those of attention over the chunk's own rows too."""
+    lib, shape, n = pk.load_library(), _shape(pk, dtype=pk.QUOKA_F32, **kw), ctypes.c_size_t(0)
+    s, need = ctypes.byref(shape), max(_attn_bytes(shape), parts * 32 * (shape.head_dim + 2) * 4)
+    assert lib.quoka_paged_workspace_bytes(s, ctypes.byref(n)) == 0 and n.value == need
+    pages = ctypes.byref(_pages(max_pages=1 << 16))
+    less = ctypes.c_size_t(_attn_bytes(shape) - 1)
+    assert lib.quoka_paged_attn(s, pages, AT, AT, None, None, None, AT, None, WS, less, None) == 3
+    if parts:
+        assert lib.quoka_cross_attn(s, pages, AT, AT, None, AT, None, WS, ctypes.c_size_t(need - 1), None) == 3
+
+
 # ---- who holds the pages ----------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("kw,code", [

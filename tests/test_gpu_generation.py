@@ -275,6 +275,29 @@ def test_cross_attention_from_a_graph_as_lengths_move(C, dtype):
         float(torch.randn(1 << 16, device=DEV).sum())
 
 
+@pytest.mark.parametrize("d,C,lens", [(64, 270, [5000, 4000]), (128, 270, [5000, 2500])])
+def test_float32_attention_over_pages_in_its_own_workspace(d, C, lens):
+    """Where cross attention wants more partials: the call that does not takes what it needs, and leaves what lies behind."""
+    pk = _pk()
+    case = dict(dtype="f32", fp8=False, n_q=8, n_kv=2, d=d, page_len=16, C=C, lens=[n + C for n in lens])
+    pool, q, chunks = _cross_problem(case, 48)
+    buf = _cross_buffers(dict(case, lens=lens), pool, q)
+    want, lse = buf.attn().clone(), buf.lse.clone()
+    need = 512 * 32 * (d + 2) * 4   # at most 512 partials of 32 rows
+    assert buf.workspace.numel() > need
+    whole, buf.workspace = buf.workspace, buf.workspace[:need]
+    whole.fill_(0xFF)
+    buf.out.fill_(float("nan"))
+    buf.attn()
+    torch.cuda.synchronize()
+    assert torch.equal(buf.out, want) and torch.equal(buf.lse, lse) and bool((whole[need:] == 0xFF).all())
+    for i, n in enumerate(lens):
+        out, _, weight = P.attention(q[i].astype(np.float64), pool.k[i], pool.v[i], n)
+        assert np.all(np.abs(buf.out[i].cpu().numpy() - out) <= 1e-4 * weight + 1e-7)
+    with pytest.raises(pk.QuokaError):
+        buf.cross_attn()
+
+
 # ---- verification ------------------------------------------------------------------------------------------------------
 
 def _softmax(z):
