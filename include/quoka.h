@@ -340,7 +340,8 @@ quoka_status quoka_pages_resize(const quoka_page_owners* owners, const int32_t* 
  *   lens        in   [from->batch] int32;  parents  in  [children->batch] int32, repeated ones too
  *   first       out  [children->batch]: the first position of a row that is to be copied (the whole pages' end)
  *   child_lens  out  [children->batch]: cached tokens; where the last page is lacking, those of the whole pages
- *   workspace   of quoka_pages_workspace_bytes(children) */
+ *   workspace   of quoka_pages_workspace_bytes(children)
+ * No output shares memory with an input, with an array of either batch or with another output: such calls are refused. */
 quoka_status quoka_pages_fork(const quoka_page_owners* from, const quoka_page_owners* children, const int32_t* parents, const int32_t* lens,
                               int32_t* first, int32_t* child_lens, int32_t* lacking, void* workspace, size_t workspace_bytes,
                               void* stream);

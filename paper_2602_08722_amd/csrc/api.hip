@@ -801,9 +801,21 @@ quoka_status quoka_pages_fork(const quoka_page_owners* from, const quoka_page_ow
   auto overlap = [](const int32_t* x, long long n, const int32_t* y, long long m) { return x < y + m && y < x + n; };
   if (overlap(p.table, (long long)p.b * p.max_pages, o.table, (long long)o.b * o.max_pages) || overlap(p.held, p.b, o.held, o.b)) return QUOKA_EINVAL;
   if (parents == nullptr || lens == nullptr || first == nullptr || child_lens == nullptr || lacking == nullptr) return QUOKA_EINVAL;
-  if (overlap(child_lens, o.b, lens, p.b) || overlap(first, o.b, lens, p.b)) return QUOKA_EINVAL;   // (children of one parent read what another wrote)
   st = check_owners_ws(o, workspace, workspace_bytes);
   if (st != QUOKA_OK) return st;
+  // (children of one parent would read what another wrote, and the waves of a child's block what one of them wrote)
+  const struct {
+    const int32_t* at;
+    long long n;
+  } outs[3] = {{first, o.b}, {child_lens, o.b}, {lacking, 1}},
+    ins[7] = {{parents, o.b}, {lens, p.b}, {o.ref, o.n_pages}, {p.table, (long long)p.b * p.max_pages}, {o.table, (long long)o.b * o.max_pages},
+              {p.held, p.b}, {o.held, o.b}};
+  for (int i = 0; i < 3; ++i) {
+    for (const auto& in : ins)
+      if (overlap(outs[i].at, outs[i].n, in.at, in.n)) return QUOKA_EINVAL;
+    for (int k = 0; k < i; ++k)
+      if (overlap(outs[i].at, outs[i].n, outs[k].at, outs[k].n)) return QUOKA_EINVAL;
+  }
   quoka::ForkArgs f;
   f.parents = parents;
   f.lens = lens;

@@ -158,6 +158,24 @@ def test_owners_that_do_not_belong_together_and_bad_pointers_are_refused():
     assert lib.quoka_pages_fork(at, child, AT, AT, OTHER, OTHER, AT, WS, ctypes.c_size_t(8), None) == 3
 
 
+def test_outputs_of_a_fork_over_its_inputs_or_each_other_are_refused():
+    """Of three children from two sequences: any of the three outputs that shares a word with the parents, the lengths, the three arrays of
+    either batch, or another output.  (In batches of more than a block's, threads read some of them after others wrote.)"""
+    lib, n = pk.load_library(), ctypes.c_size_t(0)
+    source, kids = _owners(ref=0x100000, page_table=0x200000, held=0x300000, batch=2), _owners(ref=0x100000, page_table=0x400000, held=0x500000)
+    assert lib.quoka_pages_workspace_bytes(ctypes.byref(kids), ctypes.byref(n)) == 0
+    arrays = dict(parents=(0x600000, 3), lens=(0x700000, 2), first=(0x800000, 3), child_lens=(0x900000, 3), lacking=(0xA00000, 1))
+    others = dict(arrays, ref=(0x100000, 100), table=(0x200000, 2 * 8), kids_table=(0x400000, 3 * 8), held=(0x300000, 2), kids_held=(0x500000, 3))
+    for out in ("first", "child_lens", "lacking"):
+        for name, (start, words) in others.items():
+            if name == out:
+                continue
+            for at in (start, start + 4 * (words - 1), start - 4 * (arrays[out][1] - 1)):   # on it, over its end, over its start
+                a = {k: ctypes.c_void_p(at if k == out else v[0]) for k, v in arrays.items()}
+                assert lib.quoka_pages_fork(ctypes.byref(source), ctypes.byref(kids), a["parents"], a["lens"], a["first"], a["child_lens"], a["lacking"],
+                                            WS, n, None) == 1, (out, name, hex(at))
+
+
 # ---- verification -----------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("kw,code", [
