@@ -355,7 +355,8 @@ quoka_status quoka_pages_fork(const quoka_page_owners* from, const quoka_page_ow
  *   w_v = max(p_a(v) - q_a(v), 0) for a < n, or p_a(v) should all of these be 0;   w_v = p_n(v) for a == n.
  * So the tokens are distributed as the target's, whatever drafted them.  Distributions need not add up to 1.  A w_v that is no positive
  * number (NaN, an infinity) weighs nothing; a token whose p_i(x_i) is none, whose q_i(x_i) is NaN or an infinity, or that is outside
- * [0, vocab) is not accepted.  All of it is in float64.  No output is an input.
+ * [0, vocab) is not accepted.  All of it is in float64.  No output shares memory with an input or with the other (refused for tokens, random
+ * numbers and lengths).
  *   target      in   [b, n_draft + 1, vocab] (dtype), the last axis contiguous, others by strides (elements, may be 0)
  *   draft       in   [b, n_draft, vocab] (dtype); NULL: q_i is 1 at x_i (tokens that were looked up)
  *   tokens      in   [b, n_draft] int32;  uniform  in  [b, n_draft + 1] float32

@@ -754,6 +754,11 @@ quoka_status quoka_cache_copy(const quoka_shape* shape, const quoka_pages* src, 
   return from_hip(quoka::launch_move_rows(a, dm.b, row_bytes, src->format == QUOKA_PAGES_FP8, static_cast<hipStream_t>(stream)));
 }
 
+// Whether n words from x on and m from y on share any.
+static bool overlap(const void* x, long long n, const void* y, long long m) {
+  return static_cast<const int32_t*>(x) < static_cast<const int32_t*>(y) + m && static_cast<const int32_t*>(y) < static_cast<const int32_t*>(x) + n;
+}
+
 // ---- who holds the pages -------------------------------------------------------------------------------------------
 static quoka_status check_owners(const quoka_page_owners* o, quoka::Owners* out) {
   if (o == nullptr || o->ref == nullptr || o->page_table == nullptr || o->held == nullptr) return QUOKA_EINVAL;
@@ -798,7 +803,6 @@ quoka_status quoka_pages_fork(const quoka_page_owners* from, const quoka_page_ow
   st = check_owners(children, &o);
   if (st != QUOKA_OK) return st;
   if (p.ref != o.ref || p.n_pages != o.n_pages || p.shift != o.shift) return QUOKA_EINVAL;
-  auto overlap = [](const int32_t* x, long long n, const int32_t* y, long long m) { return x < y + m && y < x + n; };
   if (overlap(p.table, (long long)p.b * p.max_pages, o.table, (long long)o.b * o.max_pages) || overlap(p.held, p.b, o.held, o.b)) return QUOKA_EINVAL;
   if (parents == nullptr || lens == nullptr || first == nullptr || child_lens == nullptr || lacking == nullptr) return QUOKA_EINVAL;
   st = check_owners_ws(o, workspace, workspace_bytes);
@@ -850,10 +854,18 @@ quoka_status quoka_verify_draft(const quoka_draft_shape* shape, const void* targ
   if (st != QUOKA_OK) return st;
   if (target == nullptr || tokens == nullptr || uniform == nullptr || n_accepted == nullptr || tokens_out == nullptr || workspace == nullptr)
     return QUOKA_EINVAL;
-  if (n_accepted == draft_lens) return QUOKA_EINVAL;   // (waves read the one after others wrote the other)
   const uintptr_t es = shape->dtype == QUOKA_BF16 ? 2 : 4;
   if (reinterpret_cast<uintptr_t>(target) % es != 0 || reinterpret_cast<uintptr_t>(draft) % es != 0) return QUOKA_EINVAL;
   if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0 || workspace_bytes < need) return QUOKA_EWORKSPACE;
+  // (waves would read the one after others wrote the other)
+  const long long b = shape->batch, words = b * (shape->n_draft + 1);
+  if (overlap(n_accepted, b, tokens_out, words)) return QUOKA_EINVAL;
+  for (const bool counts : {true, false}) {
+    const void* out = counts ? n_accepted : tokens_out;
+    const long long n = counts ? b : words;
+    if (overlap(out, n, tokens, b * shape->n_draft) || overlap(out, n, uniform, words) || (draft_lens != nullptr && overlap(out, n, draft_lens, b)))
+      return QUOKA_EINVAL;
+  }
   quoka::VerifyArgs a;
   a.target = target;
   a.draft = draft;

@@ -204,6 +204,22 @@ def test_bad_pointers_of_a_verification_are_refused():
         assert lib.quoka_verify_draft(s, AT, AT, AT, AT, None, AT, AT, ws, size, None) == code
 
 
+def test_outputs_of_a_verification_over_its_inputs_or_each_other_are_refused():
+    """Two sequences of three drafted tokens: counts and tokens that come out share no word with drafted tokens, random numbers, lengths or each
+    other.  (Blocks of one sequence would read what those of another wrote.)"""
+    lib, n, s = pk.load_library(), ctypes.c_size_t(0), ctypes.byref(_drafts())
+    assert lib.quoka_verify_workspace_bytes(s, ctypes.byref(n)) == 0
+    arrays = dict(tokens=(0x600000, 6), uniform=(0x700000, 8), draft_lens=(0x800000, 2), n_accepted=(0x900000, 2), tokens_out=(0xA00000, 8))
+    for out in ("n_accepted", "tokens_out"):
+        for name, (start, words) in arrays.items():
+            if name == out:
+                continue
+            for at in (start, start + 4 * (words - 1), start - 4 * (arrays[out][1] - 1)):   # on it, over its end, over its start
+                a = {k: ctypes.c_void_p(at if k == out else v[0]) for k, v in arrays.items()}
+                assert lib.quoka_verify_draft(s, AT, AT, a["tokens"], a["uniform"], a["draft_lens"], a["n_accepted"], a["tokens_out"], WS, n, None) == 1, \
+                    (out, name, hex(at))
+
+
 # ---- the binding ------------------------------------------------------------------------------------------------------
 
 def _ints(*x):
