@@ -279,8 +279,8 @@ quoka_status quoka_paged_attn(const quoka_shape* shape, const quoka_pages* pages
                               const int32_t* chunk_lens, const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse,
                               void* workspace, size_t workspace_bytes, void* stream);
 
-/* Cross attention: attention of a chunk's queries over cached rows that are not the chunk's own -- an encoder's states, or a prefix that
- * several sequences share -- written by quoka_cache_write like any others.  For q-head h (KV head kv) and chunk position i < chunk_lens[b]:
+/* Cross attention: attention of a chunk's queries over cached rows that are not the chunk's own (an encoder's states), written by
+ * quoka_cache_write like any others.  For q-head h (KV head kv) and chunk position i < chunk_lens[b]:
  *   O[b,h,i] = sum_t softmax_t(<Q[b,h,i], K_t> / sqrt(d)) V_t over the positions t < kv_lens[b], without a mask.
  * Rows i >= chunk_lens[b], and all rows of a sequence of kv_lens[b] == 0, are written as zeros, their lse as -infinity.
  * Arguments, workspace (quoka_paged_workspace_bytes is enough for either call; in float32 each takes what it needs itself), limits and

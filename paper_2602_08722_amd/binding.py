@@ -597,7 +597,7 @@ class PagedBuffers:
         buf.write()        the chunk's rows into the pages
         buf.attn()         attention over all cached rows and the chunk's       (the chunk's rows have been written)
         buf.sparse_attn()  over the listed rows and the chunk's
-        buf.cross_attn()   over all cached rows and no others: kv_lens states of an encoder (or a prefix) that the cache holds
+        buf.cross_attn()   over all cached rows and no others: kv_lens states of an encoder that the cache holds
         buf.chunk_attn()   the method's step over pages: write, read K back, select keys, sparse_attn
         buf.read(k, v)     the cached rows as contiguous tensors; either may be None
     """

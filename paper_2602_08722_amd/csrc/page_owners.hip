@@ -4,11 +4,13 @@
 // Pages are handed out lowest first, in the order of the sequences and of their entries, so that a call's result depends on nothing but its
 // arguments: counts are changed by integer atomics, whose order does not matter, and the rank of a free page among the free ones names the
 // entry that gets it.  Three steps, each of which uses what the one before has completed: entries that go or are shared, free pages counted
-// beside the sum of what the sequences lack, free pages to entries.  Small pools and batches take them in one launch of one block, others in
-// three launches (a block a sequence, a tile of pages a block).
+// beside the sum of what the sequences lack, free pages to entries.  Small pools and batches take them in one launch of one block, small pools of
+// larger batches in two (a block a sequence, then one block), others in three (a block a sequence, a tile of pages a block twice).
 // Bound by the chain: lengths, table, counts' atomics, counts, table.  Measured: a step of 16 sequences over 8192 pages 3 - 4 us, of 256 over 262144
-// 2.7 + 2.5 + 4.3; forks of 16 sequences 6.2, of 256 with 130816 entries 3.4 + 5.3.  (Counts fetched ahead of the scans, whether pages are wanted or not:
-// 0.6 us more for a step that wants none, which most are, otherwise the same.)
+// 2.7 + 2.5 + 4.3; forks that change only last pages, of 16 sequences 6.2, of 256 with tables of 130816 entries 3.3 + 5.1 (a call 9.9, and 10.5 where nearly
+// every entry changes; of the 16 the same).  With many tiles, each block of the last launch adds up the counts of those before its own, which grows with the
+// square of the pool: steps that want nothing, over 2^18 and 2^22 pages 11.6 us, 2^26 101, 2^28 1012, 2^30 13500.  (Counts fetched ahead of the scans,
+// whether pages are wanted or not: 0.6 us more for a step that wants none, which most are, otherwise the same.)
 #include <type_traits>
 
 #include "common.hip.h"

@@ -1,15 +1,15 @@
 // Verification of drafted tokens against the target's probabilities (quoka_verify_draft).
 //
-// Token i of a sequence is accepted while u_i q_i(x_i) < p_i(x_i), a positive number, and q_i(x_i) is finite; the product of two float32 numbers is exact in 64 bits.  The token after
-// the a accepted ones is the lowest v of positive weight w_v with w_0 + ... + w_v > u_n (w_0 + w_1 + ...), w = max(p_a - q_a, 0) behind a refusal
+// Token i of a sequence is accepted while u_i q_i(x_i) < p_i(x_i), a positive number, and q_i(x_i) is finite; the product of two float32 numbers is
+// exact in 64 bits.  The token after the a accepted ones is the lowest v of positive weight w_v with w_0 + ... + w_v > u_n (w_0 + w_1 + ...), w = max(p_a - q_a, 0) behind a refusal
 // (p_a, should nothing be left of it), else p_a.  Sums are in 64 bits: a token's part of that line is as narrow as its probability.
 //
 // Bound by memory where there are many sequences (two rows of the vocabulary each), by a chain of fetches where there are few (tokens, their
 // probabilities, the rows).  Lanes take neighbouring pieces of 16 bytes, wherever a row starts (an odd vocabulary's rows are aligned to an
 // element), and a wave a run of neighbouring entries: the sums of whole waves say which one the random number points into, and that one
 // alone adds up its entries in order.
-// Measured: one sequence, 4 tokens that were looked up, vocabulary 32003, 3.9 us and 2.7 (two launches of a chain of fetches each: 8.3 a call);
-// 64 sequences of up to 7, 131072 float32, 12.4 and 5.2 (67 MB in the first: 5.4 TB/s); vocabulary 1000 in one launch 3.3.
+// Measured: one sequence, 4 tokens that were looked up, vocabulary 32003, 4.0 us and 3.4 (two launches of a chain of fetches each: 8.3 a call);
+// 64 sequences of up to 7, 131072 float32, 12.8 and 4.6 (67 MB in the first: 5.2 TB/s); vocabulary 1000 in one launch 3.3.
 #include <type_traits>
 
 #include "common.hip.h"
