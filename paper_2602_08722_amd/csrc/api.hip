@@ -650,9 +650,8 @@ quoka_status quoka_cache_read(const quoka_shape* shape, const quoka_pages* pages
                                            static_cast<hipStream_t>(stream)));
 }
 
-// (own: the chunk's own rows are attended too)
-static size_t paged_ws_bytes(const Dims& dm, int dtype, bool own) {
-  const size_t bytes = round_up(quoka::paged_attn_ws_floats(dm, dtype, own) * sizeof(float), kAlign);
+static size_t paged_ws_bytes(const quoka::PagedPlan& plan) {
+  const size_t bytes = round_up(plan.ws_floats * sizeof(float), kAlign);
   return bytes > 0 ? bytes : kAlign;
 }
 
@@ -661,11 +660,13 @@ quoka_status quoka_paged_workspace_bytes(const quoka_shape* shape, size_t* out_b
   const quoka_status st = check_shape(shape, &dm);
   if (st != QUOKA_OK) return st;
   if (out_bytes == nullptr) return QUOKA_EINVAL;
-  const size_t with_own = paged_ws_bytes(dm, shape->dtype, true), without = paged_ws_bytes(dm, shape->dtype, false);
+  const size_t with_own = paged_ws_bytes(quoka::paged_attn_plan(dm, shape->dtype, true)),
+               without = paged_ws_bytes(quoka::paged_attn_plan(dm, shape->dtype, false));
   *out_bytes = with_own > without ? with_own : without;   // (either call)
   return QUOKA_OK;
 }
 
+// (own: the chunk's own rows are attended too)
 static quoka_status paged_common(const quoka_shape* shape, const quoka_pages* pages, const void* q, const int32_t* kv_lens,
                                  const int32_t* chunk_lens, const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse,
                                  void* workspace, size_t workspace_bytes, void* stream, bool own) {
@@ -680,7 +681,8 @@ static quoka_status paged_common(const quoka_shape* shape, const quoka_pages* pa
   // (kernels number the keys of all sequences together, in tiles of 32, with 32 bits)
   if ((long long)dm.b * ((long long)dm.T_max + dm.C + 32) >= 1ll << 36) return QUOKA_EUNSUPPORTED;
   if (workspace == nullptr) return QUOKA_EINVAL;
-  if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0 || workspace_bytes < paged_ws_bytes(dm, shape->dtype, own)) return QUOKA_EWORKSPACE;
+  const quoka::PagedPlan plan = quoka::paged_attn_plan(dm, shape->dtype, own);
+  if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0 || workspace_bytes < paged_ws_bytes(plan)) return QUOKA_EWORKSPACE;
   a.q = q;
   a.kv_lens = kv_lens;
   a.chunk_lens = chunk_lens;
@@ -689,7 +691,7 @@ static quoka_status paged_common(const quoka_shape* shape, const quoka_pages* pa
   a.k_cnt = k_cnt;
   a.out = out;
   a.lse = lse;
-  return from_hip(quoka::launch_paged_attn(dm, shape->dtype, pages->format == QUOKA_PAGES_FP8, a, static_cast<float*>(workspace),
+  return from_hip(quoka::launch_paged_attn(dm, shape->dtype, pages->format == QUOKA_PAGES_FP8, a, plan, static_cast<float*>(workspace),
                                            static_cast<hipStream_t>(stream), own));
 }
 

@@ -159,8 +159,15 @@ hipError_t launch_cross_few(const Dims& dm, bool fp8, const PagedArgs& a, hipStr
 bool cross_rows_take_bf16(const Dims& dm);
 float cross_rows_us(const Dims& dm);
 hipError_t launch_cross_rows(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, hipStream_t st);
-size_t paged_attn_ws_floats(const Dims& dm, int dtype, bool own);
-hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float* part, hipStream_t st, bool own = true);
+// what a call's shape decides, worked out once a call: its workspace, and in float32 the kernel of cross attention
+enum StateForm { kWaveARow, kFewRows, kStateUnits };
+struct PagedPlan {
+  size_t ws_floats = 0;
+  StateForm form = kStateUnits;
+  int units = 0;   // kStateUnits: of a share
+};
+PagedPlan paged_attn_plan(const Dims& dm, int dtype, bool own);
+hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, const PagedPlan& plan, float* part, hipStream_t st, bool own);
 
 // rows of pages into other pages (page_rows.hip): the listed ones of every KV head (list), or first .. lens - 1 of the parents
 struct MoveArgs {

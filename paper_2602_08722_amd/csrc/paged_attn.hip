@@ -98,46 +98,45 @@ __global__ __launch_bounds__(kPsThreads) void paged_f32_short(Dims dm, PagedArgs
 // Where the query rows are few too (cross_rows, a block a sequence and KV head): that, unless a wave a row takes less, or units less than 1 / 0.85 of it
 // (which its figure is above the measured ones where partials are many): 8 x 4 rows, d 64, 300 states 13.1 -> 8.6 us, of 1000 14.1 (17.3);
 // 12 heads, 1000 states 22.7 -> 11.5, one sequence of 2000 14.1 -> 12.2, of 4000 15.1 (21.8).
-enum StateForm { kWaveARow, kFewRows, kStateUnits };
-static StateForm state_form(const Dims& dm) {
+static PagedPlan state_plan(const Dims& dm) {
   const float rows = (float)dm.b * (float)dm.n_q * (float)dm.C * 1e-3f, n = (float)dm.T_cap;
   const float row_us = dm.d == 64 ? 4.6f + 0.11f * n + rows * (0.55f + 0.05f * n) : 4.8f + 0.13f * n + rows * (0.92f + 0.075f * n);
   const float few_us = cross_rows_us(dm);
   // (with rows as few as cross_rows takes, row_us is 1 above what is measured)
-  if (row_us < (dm.d == 64 ? 7.5f + 0.7f * rows : 9.8f + 1.06f * rows) && row_us < few_us + 1.0f) return kWaveARow;
+  if (row_us < (dm.d == 64 ? 7.5f + 0.7f * rows : 9.8f + 1.06f * rows) && row_us < few_us + 1.0f) return {0, kWaveARow, 0};
   float units_us;
-  f32_state_units(dm, &units_us);
-  return few_us < 0.85f * units_us ? kFewRows : kStateUnits;
+  const int units = f32_state_units(dm, &units_us);
+  if (few_us < 0.85f * units_us) return {0, kFewRows, 0};
+  const int shares = f32_state_shares(dm, units);   // (partials of these and no more: kMostStateParts at most)
+  return {shares > 1 ? (size_t)(f32_blocks(dm) * shares) * 32 * (dm.d + 2) : 0, kStateUnits, units};
 }
 
 template <bool FP8, int D, bool OWN>
-static hipError_t launch_paged_f32(const Dims& dm, const PagedArgs& a, float* part, hipStream_t st) {
-  const StateForm form = OWN ? kStateUnits : state_form(dm);
-  if (form == kFewRows) return launch_cross_rows(dm, QUOKA_F32, FP8, a, st);
-  if (OWN ? attn_f32_is_short(dm, a.k_idx != nullptr) : form == kWaveARow) {
+static hipError_t launch_paged_f32(const Dims& dm, const PagedArgs& a, const PagedPlan& plan, float* part, hipStream_t st) {
+  if (plan.form == kFewRows) return launch_cross_rows(dm, QUOKA_F32, FP8, a, st);
+  if (OWN ? attn_f32_is_short(dm, a.k_idx != nullptr) : plan.form == kWaveARow) {
     const dim3 grid((dm.C + kPsThreads / 64 - 1) / (kPsThreads / 64), dm.n_q, dm.b);
     hipLaunchKernelGGL((paged_f32_short<FP8, D, OWN>), grid, dim3(kPsThreads), 0, st, dm, a);
     return hipGetLastError();
   }
   constexpr int SRC = OWN ? FP8 ? kFp8Pages : kRawPages : FP8 ? kFp8States : kRawStates;
   PagedAttnArgs aa = paged_attn_args(a, part);
-  if constexpr (!OWN) aa.slots = f32_state_units(dm);
+  if constexpr (!OWN) aa.slots = plan.units;
   return launch_f32_units<D, SRC>(dm, aa, part, st);
 }
 
-// Partials of cross attention: of the shares that the launch has (kMostStateParts at most).
-static size_t cross_f32_ws_floats(const Dims& dm) {
-  if (state_form(dm) != kStateUnits) return 0;
-  const int shares = f32_state_shares(dm, f32_state_units(dm));
-  return shares > 1 ? (size_t)(f32_blocks(dm) * shares) * 32 * (dm.d + 2) : 0;
+PagedPlan paged_attn_plan(const Dims& dm, int dtype, bool own) {
+  PagedPlan plan;
+  if (dtype != QUOKA_BF16) {
+    if (!own) return state_plan(dm);
+    plan.ws_floats = attn_f32_ws_floats(dm);
+  } else {
+    plan.ws_floats = attn_decode_applies(dm) ? paged_decode_ws_floats(dm) : paged_attn_bf16_ws_floats(dm);
+  }
+  return plan;
 }
 
-size_t paged_attn_ws_floats(const Dims& dm, int dtype, bool own) {
-  if (dtype != QUOKA_BF16) return own ? attn_f32_ws_floats(dm) : cross_f32_ws_floats(dm);
-  return attn_decode_applies(dm) ? paged_decode_ws_floats(dm) : paged_attn_bf16_ws_floats(dm);
-}
-
-hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, float* part, hipStream_t st, bool own) {
+hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArgs& a, const PagedPlan& plan, float* part, hipStream_t st, bool own) {
   if (dtype == QUOKA_BF16) {
     if (!own && cross_rows_take_bf16(dm)) return launch_cross_rows(dm, dtype, fp8, a, st);
     if (attn_decode_applies(dm))
@@ -146,8 +145,8 @@ hipError_t launch_paged_attn(const Dims& dm, int dtype, bool fp8, const PagedArg
   }
   auto launch = [&](auto own_rows) {
     constexpr bool OWN = decltype(own_rows)::value;
-    if (dm.d == 64) return fp8 ? launch_paged_f32<true, 64, OWN>(dm, a, part, st) : launch_paged_f32<false, 64, OWN>(dm, a, part, st);
-    return fp8 ? launch_paged_f32<true, 128, OWN>(dm, a, part, st) : launch_paged_f32<false, 128, OWN>(dm, a, part, st);
+    if (dm.d == 64) return fp8 ? launch_paged_f32<true, 64, OWN>(dm, a, plan, part, st) : launch_paged_f32<false, 64, OWN>(dm, a, plan, part, st);
+    return fp8 ? launch_paged_f32<true, 128, OWN>(dm, a, plan, part, st) : launch_paged_f32<false, 128, OWN>(dm, a, plan, part, st);
   };
   return own ? launch(std::true_type{}) : launch(std::false_type{});
 }

@@ -296,6 +296,14 @@ def test_float32_attention_over_pages_in_its_own_workspace(d, C, lens):
         assert np.all(np.abs(buf.out[i].cpu().numpy() - out) <= 1e-4 * weight + 1e-7)
     with pytest.raises(pk.QuokaError):
         buf.cross_attn()
+    wide = torch.full((whole.numel() + 65536,), 0xFF, dtype=torch.uint8, device=DEV)   # what cross attention asks for, and no more
+    buf.workspace = wide[:whole.numel()]
+    buf.out.fill_(float("nan"))
+    buf.cross_attn()
+    torch.cuda.synchronize()
+    pool.k, pool.v = ([x[:n] for x, n in zip(y, lens)] for y in (pool.k, pool.v))
+    _check_cross(case, buf, pool, q, chunks)
+    assert bool((wide[whole.numel():] == 0xFF).all())
 
 
 # ---- verification ------------------------------------------------------------------------------------------------------
